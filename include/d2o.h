@@ -320,6 +320,84 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
                        int32_t* n_evi, int32_t* target_pos, double* u_star, uint8_t* passed,
                        void* stream);
 
+/* ---- Windowed prompt attention, and caches in pages -------------------------------------
+ * The two cache policies that the paper compares D2O with, in the form a server runs them: a window
+ * of recent tokens plus a few first ones, and pure eviction by accumulated attention (Eq. 6-8
+ * without Eq. 9-12), over a cache that lies in pages of a pool shared by all sequences.  No
+ * context is needed: the caller owns pools, page table, lengths and workspace.  All of these calls
+ * enqueue only, allocate nothing, keep nothing between calls and may be captured into a graph.
+ * A workspace (16-byte aligned) belongs to one call at a time: calls that overlap in time need one each. */
+
+/* Causal prompt attention in which query i sees the keys j <= i with j > i - window or j < n_sink:
+ * O = softmax(Q K^T / sqrt(d)) V over those.  window = 0: no window (every j <= i).
+ * Q, O: [B][Hq][n][d]; K, V: [B][Hkv][n][d]; O in `dtype`.  lens: device [B], the tokens of each sequence
+ * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
+ * its keys behind the end are never looked at.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
+ * INVALID_ARG, UNSUPPORTED, CAPACITY (workspace smaller than d2o_window_workspace_bytes says), HIP. */
+int d2o_window_workspace_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                               size_t* bytes);
+int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                      d2o_view Q, d2o_view K, d2o_view V, const int32_t* lens, int32_t window, int32_t n_sink,
+                      d2o_view O, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A cache in pages.  Entry s of sequence b is row s % page_size of page page_table[b][s / page_size], for every
+ * KV head.  A page id outside [0, n_pages) stands for no page: entries there are as if absent (never attended to, written
+ * or moved; evictions rank them below all others).  A page that a call writes must belong to one sequence; pages that are
+ * only attended to, with no scores, may be shared. */
+typedef struct {
+  int32_t batch;       /* B: sequences, rows of page_table                                  */
+  int32_t n_q_heads;   /* Hq, a multiple of n_kv_heads with Hq / Hkv <= 16                  */
+  int32_t n_kv_heads;  /* Hkv                                                               */
+  int32_t head_dim;    /* d: 64 or 128                                                      */
+  int32_t dtype;       /* d2o_dtype of q, k, v and out, and of the rows unless cache_fp8    */
+  int32_t cache_fp8;   /* 1: a row is d E4M3 codes and one power of two, as in d2o_config   */
+  int32_t page_size;   /* rows of a page: a power of two, 1 to 1024                         */
+  int32_t n_pages;     /* pages of the pool                                                 */
+  int32_t max_pages;   /* columns of page_table                                             */
+  d2o_view K, V;       /* the pool: stride_b between pages, stride_h between KV heads,      */
+                       /* stride_n between rows, in elements (bytes when cache_fp8)         */
+  int8_t* K_exp;       /* [n_pages][Hkv][page_size] powers of two of fp8 rows, else NULL    */
+  int8_t* V_exp;
+  float* score;        /* [n_pages][Hkv][page_size] accumulated attention, NULL: not kept   */
+  int32_t* pos;        /* [n_pages][Hkv][page_size] token position of an entry, NULL: entry */
+                       /* s has position s                                                  */
+  const int32_t* page_table; /* [B][max_pages]                                              */
+} d2o_pages;
+
+/* Bytes of the workspace that the three calls below need while no sequence (fill: no prompt) has more than
+ * max_len entries.  Errors: INVALID_ARG, UNSUPPORTED. */
+int d2o_pages_workspace_bytes(const d2o_pages* pages, int32_t max_len, size_t* bytes);
+
+/* Prompts into pages.  Of the lens[b] tokens of sequence b (NULL: n each; taken within [0, n]) every KV head keeps the
+ * first n_sink, the last `recent` and, of those between, the budget - n_sink - recent with the highest scores (equal scores: the lower
+ * position; NaN ranks highest); min(lens[b], budget) entries are written from entry 0 in rising position, with score (0 where scores is
+ * NULL) and position where the pages keep them.  K, V: [B][Hkv][n][d] in `dtype`; scores: device [B][Hkv][n] fp32, NULL only
+ * if budget >= n.  Rows of the pages behind the last entry are left as they were.
+ * Errors: INVALID_ARG (budget < max(1, n_sink + recent), scores missing), UNSUPPORTED, CAPACITY (pages or workspace too small), HIP. */
+int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, const int32_t* lens, const float* scores,
+                   int32_t budget, int32_t recent, int32_t n_sink, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One generation step over pages.  lens: device [B], entries of every sequence INCLUDING the new token, whose row
+ * (k_new, v_new) is stored as entry lens[b] - 1 with score 0 and position positions[b]; then q attends over the
+ * entries with position > positions[b] - window or position < n_sink (window = 0: all) and, where the pages keep scores,
+ * the softmax rows of the Hq / Hkv query heads are added to the entries' scores (Eq. 6).  positions: device
+ * [B], NULL: lens[b] - 1.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
+ * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
+ * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_len beyond the page table, workspace too small), HIP. */
+int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view v_new, const int32_t* lens,
+                   const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Evicts in place.  Every KV head of a sequence with lens[b] > budget entries (device [B], read only) keeps `budget` of
+ * them: the positions below n_sink and above the newest position - recent, then the highest scores (equal scores: the lower
+ * position, then the lower entry; NaN ranks highest).  Kept entries below `budget` stay where they are; the i-th given-up entry below
+ * it takes row, score and position of the i-th kept one behind it.  Afterwards the sequence has min(lens[b], budget)
+ * entries; the rows behind are left as they were.  pages->score must not be NULL, and pages->pos not either (an entry moves, its position with it).
+ * max_len as for d2o_pages_step.  Errors: INVALID_ARG (budget < max(1, n_sink + recent)), UNSUPPORTED, CAPACITY, HIP. */
+int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int32_t max_len, int32_t budget, int32_t recent,
+                    int32_t n_sink, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Kernel timing aid for benchmarks (not part of the method).  While enabled (on >= 1), launches
  * of the kernels below are bracketed by two HIP events recorded on the launch stream: every
  * launch of the prompt-phase kernels and of the split closing kernels, and every on-th launch of

@@ -23,6 +23,8 @@ EXPORTS = [
     "d2o_decode_step_static", "d2o_append_chunk", "d2o_append_events",
     "d2o_layer_reserve", "d2o_cache_export", "d2o_cache_import", "d2o_last_events",
     "d2o_prefill_events", "d2o_timing_enable", "d2o_timing_read",
+    "d2o_window_workspace_bytes", "d2o_window_attend", "d2o_pages_workspace_bytes", "d2o_pages_fill",
+    "d2o_pages_step", "d2o_pages_evict",
 ]
 
 
@@ -42,6 +44,14 @@ class d2o_config(C.Structure):
 class d2o_view(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64),
                 ("stride_n", C.c_int64)]
+
+
+class d2o_pages(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("cache_fp8", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("K", d2o_view), ("V", d2o_view), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p),
+                ("score", C.c_void_p), ("pos", C.c_void_p), ("page_table", C.c_void_p)]
 
 
 _lib = None
@@ -89,6 +99,14 @@ def load_library() -> C.CDLL:
     lib.d2o_prefill_events.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.d2o_timing_enable.argtypes = [vp, i32]
     lib.d2o_timing_read.argtypes = [vp, i32, P(C.c_double), P(C.c_int64), vp]
+    sz = C.c_size_t
+    lib.d2o_window_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, P(sz)]
+    lib.d2o_window_attend.argtypes = [i32, i32, i32, i32, i32, i32, d2o_view, d2o_view, d2o_view, vp, i32, i32, d2o_view,
+                                      vp, sz, vp]
+    lib.d2o_pages_workspace_bytes.argtypes = [P(d2o_pages), i32, P(sz)]
+    lib.d2o_pages_fill.argtypes = [P(d2o_pages), d2o_view, d2o_view, i32, vp, vp, i32, i32, i32, vp, sz, vp]
+    lib.d2o_pages_step.argtypes = [P(d2o_pages), d2o_view, d2o_view, d2o_view, vp, vp, i32, i32, i32, d2o_view, vp, sz, vp]
+    lib.d2o_pages_evict.argtypes = [P(d2o_pages), vp, i32, i32, i32, i32, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("d2o_destroy", "d2o_last_error"):
             getattr(lib, name).restype = C.c_int
@@ -384,6 +402,172 @@ class D2O:
                     "d2o_prefill_events")
         r, e = nr.value, ne.value
         return ret[:r], evi[:e], tgt[:e], us[:e], ps[:e].astype(bool)
+
+
+# ---- windowed prompt attention and caches in pages ------------------------------------------
+
+_DTYPE_CODES = {torch.bfloat16: D2O_BF16, torch.float32: D2O_F32}
+_STATUS = {-1: "invalid argument", -2: "not supported", -3: "too small a cache or workspace", -4: "call order",
+           -5: "HIP error"}
+
+
+def _need(ok, what):
+    if not ok:
+        raise D2OError(what)
+
+
+def _ok(rc, what):
+    if rc != 0:
+        raise D2OError(f"{what} failed with {rc} ({_STATUS.get(rc, 'unknown')})")
+
+
+def _view_of(t: torch.Tensor, batch_dim=0, head_dim_=1, row_dim=2) -> d2o_view:
+    # (a dimension of size one may have any stride: it takes no part)
+    s, n = t.stride(), t.shape
+    return d2o_view(t.data_ptr(), s[batch_dim] if n[batch_dim] > 1 else 0, s[head_dim_] if n[head_dim_] > 1 else 0,
+                    s[row_dim] if row_dim is not None and n[row_dim] > 1 else 0)
+
+
+def _tensor_ok(t, shape, dtype, device, what):
+    _need(isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape)
+          and (t.numel() == 0 or t.stride(-1) == 1 or t.shape[-1] == 1),
+          f"{what}: a tensor of shape {tuple(shape)} and type {dtype} on {device}, with its last dimension contiguous, "
+          "is needed")
+
+
+def _vector_ok(t, shape, dtype, device, what):
+    _tensor_ok(t, shape, dtype, device, what)
+    _need(t.is_contiguous(), f"{what} must be contiguous")
+
+
+class _on:
+    """Makes `device` the current one for a call (nothing to do in the usual case that it is)."""
+
+    def __init__(self, device):
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return int(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=None):
+    """Causal prompt attention over the last `window` tokens and the first n_sink (window 0: all).  Q [B, Hq, n, d],
+    K, V [B, Hkv, n, d]; lens: int32 [B] tokens of a padded batch; O: output, made here if None (rows behind a sequence's end
+    are then zero).  Returns O."""
+    lib = load_library()
+    _need(isinstance(Q, torch.Tensor) and Q.is_cuda and Q.dim() == 4 and Q.dtype in _DTYPE_CODES and isinstance(K, torch.Tensor)
+          and K.dim() == 4, "Q and K: four-dimensional float32 or bfloat16 tensors on a GPU are needed")
+    B, Hq, n, d = Q.shape
+    dev, dt, Hkv = Q.device, Q.dtype, K.shape[1]
+    _tensor_ok(Q, Q.shape, dt, dev, "Q")
+    _tensor_ok(K, (B, Hkv, n, d), dt, dev, "K")
+    _tensor_ok(V, (B, Hkv, n, d), dt, dev, "V")
+    if lens is not None:
+        _vector_ok(lens, (B,), torch.int32, dev, "lens")
+    need = C.c_size_t()
+    _ok(lib.d2o_window_workspace_bytes(B, n, Hkv, d, _DTYPE_CODES[dt], C.byref(need)), "d2o_window_workspace_bytes")
+    with _on(dev) as stream:
+        if O is None:
+            O = torch.empty(Q.shape, dtype=dt, device=dev) if lens is None else torch.zeros(Q.shape, dtype=dt, device=dev)
+        else:
+            _tensor_ok(O, Q.shape, dt, dev, "O")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        _ok(lib.d2o_window_attend(B, n, Hq, Hkv, d, _DTYPE_CODES[dt], _view_of(Q), _view_of(K), _view_of(V),
+                                  lens.data_ptr() if lens is not None else None, window, n_sink, _view_of(O),
+                                  ws.data_ptr(), need.value, stream), "d2o_window_attend")
+    return O
+
+
+class Pages:
+    """A cache in pages over the caller's tensors, and the workspace of the calls on it.
+
+    K, V: pools [n_pages, Hkv, page_size, d], float32 or bfloat16, or uint8 codes with int8 K_exp, V_exp
+    [n_pages, Hkv, page_size] (8-bit rows of bfloat16 tensors); page_table int32 [B, max_pages]; score float32 and pos int32
+    [n_pages, Hkv, page_size] where accumulated attention and token positions are kept.  max_len: the most entries a sequence
+    (or tokens a prompt) will have in any call, the page table's capacity if None.  Calls on one object
+    share its workspace: on streams that overlap in time, use an object each."""
+
+    def __init__(self, K, V, page_table, n_q_heads, K_exp=None, V_exp=None, score=None, pos=None, max_len=None):
+        self.lib = load_library()
+        _need(isinstance(K, torch.Tensor) and K.is_cuda and K.dim() == 4, "K: a pool [n_pages, Hkv, page_size, d] on a GPU is needed")
+        fp8 = K.dtype == torch.uint8
+        _need(fp8 or K.dtype in _DTYPE_CODES, "pools hold float32 or bfloat16 rows, or uint8 codes")
+        self.device, self.dtype = K.device, torch.bfloat16 if fp8 else K.dtype
+        n_pages, Hkv, page_size, d = K.shape
+        _tensor_ok(K, K.shape, K.dtype, self.device, "K")
+        _tensor_ok(V, K.shape, K.dtype, self.device, "V")
+        _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table: an int32 tensor [B, max_pages] is needed")
+        _vector_ok(page_table, page_table.shape, torch.int32, self.device, "page_table")
+        per_row = (n_pages, Hkv, page_size)
+        _need((K_exp is not None and V_exp is not None) == fp8 and (fp8 or (K_exp is None and V_exp is None)),
+              "K_exp and V_exp belong to pools of uint8 codes")
+        for t, dt, what in ((K_exp, torch.int8, "K_exp"), (V_exp, torch.int8, "V_exp"), (score, torch.float32, "score"),
+                            (pos, torch.int32, "pos")):
+            if t is not None:
+                _vector_ok(t, per_row, dt, self.device, what)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        B, max_pages = page_table.shape
+        self.tensors = (K, V, page_table, K_exp, V_exp, score, pos)
+        self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = B, n_q_heads, Hkv, d
+        self.max_len = max_pages * page_size if max_len is None else int(max_len)
+        self.desc = d2o_pages(B, n_q_heads, Hkv, d, _DTYPE_CODES[self.dtype], 1 if fp8 else 0, page_size, n_pages,
+                              max_pages, _view_of(K), _view_of(V), ptr(K_exp), ptr(V_exp), ptr(score), ptr(pos),
+                              page_table.data_ptr())
+        self.capacity = max_pages * page_size
+        need = C.c_size_t()
+        _ok(self.lib.d2o_pages_workspace_bytes(C.byref(self.desc), self.max_len, C.byref(need)),
+            "d2o_pages_workspace_bytes")
+        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self._ws = (self.workspace.data_ptr(), need.value)
+
+    def _lens(self, lens, what="lens"):
+        _vector_ok(lens, (self.batch,), torch.int32, self.device, what)
+        return lens.data_ptr()
+
+    def d2o_pages_fill(self, K, V, budget, recent=0, n_sink=0, score=None, lens=None):
+        """Prompts K, V [B, Hkv, n, d] into the pages; score: float32 [B, Hkv, n] accumulated attention."""
+        _need(isinstance(K, torch.Tensor) and K.dim() == 4, "K: a tensor [B, Hkv, n, d] is needed")
+        n = K.shape[2]
+        shape = (self.batch, self.n_kv_heads, n, self.head_dim)
+        _tensor_ok(K, shape, self.dtype, self.device, "K")
+        _tensor_ok(V, shape, self.dtype, self.device, "V")
+        if score is not None:
+            _vector_ok(score, shape[:3], torch.float32, self.device, "score")
+        with _on(self.device) as stream:
+            _ok(self.lib.d2o_pages_fill(C.byref(self.desc), _view_of(K), _view_of(V), n,
+                                        None if lens is None else self._lens(lens),
+                                        None if score is None else score.data_ptr(), budget, recent, n_sink, *self._ws,
+                                        stream), "d2o_pages_fill")
+
+    def d2o_pages_step(self, q, k_new, v_new, lens, out, positions=None, window=0, n_sink=0):
+        """One new token per sequence: q, out [B, Hq, d]; k_new, v_new [B, Hkv, d], or None: attention only; lens int32
+        [B], the new token included."""
+        shape = (self.batch, self.n_q_heads, self.head_dim)
+        new = (self.batch, self.n_kv_heads, self.head_dim)
+        _tensor_ok(q, shape, self.dtype, self.device, "q")
+        _tensor_ok(out, shape, self.dtype, self.device, "out")
+        _need((k_new is None) == (v_new is None), "k_new and v_new come together")
+        if k_new is not None:
+            _tensor_ok(k_new, new, self.dtype, self.device, "k_new")
+            _tensor_ok(v_new, new, self.dtype, self.device, "v_new")
+        with _on(self.device) as stream:
+            _ok(self.lib.d2o_pages_step(C.byref(self.desc), _view_of(q, row_dim=None),
+                                        _NULL_VIEW if k_new is None else _view_of(k_new, row_dim=None),
+                                        _NULL_VIEW if v_new is None else _view_of(v_new, row_dim=None), self._lens(lens),
+                                        None if positions is None else self._lens(positions, "positions"),
+                                        min(self.max_len, self.capacity), window, n_sink, _view_of(out, row_dim=None), *self._ws, stream), "d2o_pages_step")
+
+    def d2o_pages_evict(self, lens, budget, recent=0, n_sink=0):
+        """Every head of a sequence with more than `budget` entries goes back to that many, in place."""
+        with _on(self.device) as stream:
+            _ok(self.lib.d2o_pages_evict(C.byref(self.desc), self._lens(lens), min(self.max_len, self.capacity), budget,
+                                         recent, n_sink, *self._ws, stream), "d2o_pages_evict")
 
 
 KERNEL_IDS = {"attn_fwd": 0, "colsum": 1, "select": 2, "match_filter": 3, "match_refine": 4,

@@ -1,0 +1,218 @@
+"""Windowed prompt attention with sink tokens against its 64-bit form, at tile edges, odd sizes, strides and values
+where it can go wrong."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_13035_amd import binding
+
+from . import pages_ref as ref
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def inputs(dtype, B, Hq, Hkv, n, d, seed=0, qscale=1.5):
+    g = torch.Generator().manual_seed(1000 + seed)
+    r = lambda h, s=1.0: (torch.randn((B, h, n, d), generator=g) * s).to(dtype)  # noqa: E731
+    return r(Hq, qscale), r(Hkv), r(Hkv)
+
+
+def check(Q, K, V, O, window, n_sink, lens=None):
+    """O (on the CPU) against the definition; rows behind a sequence's end are not looked at here."""
+    B, Hq, n, d = Q.shape
+    G = Hq // K.shape[1]
+    for b in range(B):
+        m = n if lens is None else int(lens[b])
+        if m == 0:
+            continue
+        seen = ref.window_seen(m, window, n_sink)
+        for h in range(Hq):
+            q, k, v = (x[b, i, :m].double() for x, i in ((Q, h), (K, h // G), (V, h // G)))
+            o, p = ref.attend64(q, k, v, seen)
+            got = O[b, h, :m].double()
+            fine = torch.isfinite(o)
+            assert torch.equal(torch.isfinite(got), fine), (b, h)
+            assert torch.equal(got.isnan(), o.isnan()) and torch.equal(got[got.isinf()], o[o.isinf()])
+            # (columns without an infinity or NaN: these have no bound)
+            vf = torch.where(torch.isfinite(v), v, torch.zeros_like(v))
+            tol = ref.bound(q, k, vf, seen, torch.where(fine, o, torch.zeros_like(o)), p, Q.dtype, Q.dtype == BF16)
+            err = torch.where(fine, (got - o).abs(), torch.zeros_like(o))
+            assert bool((err <= tol).all()), (b, h, float((err / tol).max()))
+
+
+def run(Q, K, V, window, n_sink, lens=None, O=None):
+    dev = "cuda:0"
+    O = binding.d2o_window_attend(Q.to(dev), K.to(dev), V.to(dev), window, n_sink, None if lens is None else lens.to(dev), O)
+    torch.cuda.synchronize()
+    return O.cpu()
+
+
+SIZES = [  # B, Hq, Hkv, n, window, n_sink
+    (1, 1, 1, 1, 0, 0), (1, 2, 1, 2, 1, 0), (2, 4, 2, 5, 3, 1), (1, 4, 4, 31, 8, 2), (1, 3, 1, 33, 1, 0),
+    (1, 4, 1, 63, 17, 4), (1, 2, 2, 64, 64, 0), (1, 8, 1, 65, 33, 40), (1, 16, 1, 96, 0, 0), (2, 6, 2, 127, 64, 3),
+    (1, 2, 2, 128, 63, 64), (1, 2, 1, 129, 65, 65), (1, 5, 5, 200, 100, 150), (1, 4, 2, 257, 129, 1), (1, 2, 2, 256, 300, 7),
+    (1, 1, 1, 513, 2, 130), (1, 2, 1, 700, 350, 0), (1, 2, 2, 641, 0, 4), (3, 2, 1, 300, 1, 1), (1, 2, 2, 1100, 64, 4),
+    (1, 1, 1, 2000, 1031, 77),
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "b%d_q%d_kv%d_n%d_w%d_t%d" % s)
+def test_window_attend(dtype, d, size):
+    B, Hq, Hkv, n, window, n_sink = size
+    Q, K, V = inputs(dtype, B, Hq, Hkv, n, d, seed=n)
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_padded_batch(dtype):
+    """Sequences of different lengths, one of them empty: their rows are right, the rows behind them untouched, and what lies
+    in the padding - infinities and NaN - takes no part."""
+    B, Hq, Hkv, n, d = 5, 4, 2, 300, 128
+    lens = torch.tensor([300, 0, 1, 130, 257], dtype=torch.int32)
+    Q, K, V = inputs(dtype, B, Hq, Hkv, n, d)
+    for b in range(B):
+        K[b, :, lens[b]:] = math.nan
+        V[b, :, lens[b]:] = math.inf
+        Q[b, :, lens[b]:] = math.nan
+    O = torch.full(Q.shape, 7.0, dtype=dtype, device="cuda:0")
+    got = run(Q, K, V, 100, 3, lens, O)
+    check(Q, K, V, got, 100, 3, lens)
+    for b in range(B):
+        assert bool((got[b, :, lens[b]:] == 7.0).all())
+    fresh = run(Q, K, V, 100, 3, lens)
+    for b in range(B):
+        assert torch.equal(fresh[b, :, :lens[b]], got[b, :, :lens[b]]) and bool((fresh[b, :, lens[b]:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_lengths_beyond_the_tensor_are_cut(dtype):
+    Q, K, V = inputs(dtype, 2, 2, 1, 70, 64)
+    got = run(Q, K, V, 20, 1, torch.tensor([1 << 30, -5], dtype=torch.int32))
+    check(Q, K, V, got, 20, 1, [70, 0])
+    assert bool((got[1] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_strided_views(dtype):
+    """Token-major tensors with padded rows and heads in the middle of a wider one."""
+    B, Hq, Hkv, n, d = 2, 4, 2, 150, 64
+    Q, K, V = inputs(dtype, B, Hq, Hkv, n, d)
+    wide = torch.zeros((B, n, Hq + 2 * Hkv + 1, d + 16), dtype=dtype, device="cuda:0")
+    q, k, v = wide[:, :, :Hq, :d], wide[:, :, Hq:Hq + Hkv, :d], wide[:, :, Hq + Hkv:Hq + 2 * Hkv, :d]
+    for x, y in ((q, Q), (k, K), (v, V)):
+        x.copy_(y.transpose(1, 2))
+    out = torch.full((B, n, Hq, d + 16), 7.0, dtype=dtype, device="cuda:0")
+    binding.d2o_window_attend(q.transpose(1, 2), k.transpose(1, 2), v.transpose(1, 2), 40, 5, O=out[..., :d].transpose(1, 2))
+    want = run(Q, K, V, 40, 5)
+    assert torch.equal(out[..., :d].transpose(1, 2).cpu(), want)
+    assert bool((out[..., d:] == 7.0).all())
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_values_that_are_not_finite_reach_only_who_sees_them(dtype, value):
+    Q, K, V = inputs(dtype, 1, 2, 1, 300, 64)
+    for j, c in ((0, 3), (70, 5), (128, 0), (200, 63), (255, 17), (299, 9)):
+        V[0, 0, j, c] = value
+    check(Q, K, V, run(Q, K, V, 50, 2), 50, 2)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_both_infinities_of_a_column_cancel_to_nan_where_both_are_seen(dtype):
+    Q, K, V = inputs(dtype, 1, 1, 1, 200, 128)
+    V[0, 0, 100, 7], V[0, 0, 130, 7] = math.inf, -math.inf
+    check(Q, K, V, run(Q, K, V, 64, 0), 64, 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_keys_that_are_not_finite_reach_only_who_sees_them(dtype):
+    """A NaN key makes the rows that see it NaN, whole; the others are as if it were any other key."""
+    Q, K, V = inputs(dtype, 1, 1, 1, 260, 64)
+    K[0, 0, 100] = math.nan
+    got = run(Q, K, V, 40, 0)
+    hit = torch.zeros(260, dtype=torch.bool)
+    hit[100:140] = True
+    assert bool(got[0, 0, hit].isnan().all()) and bool(torch.isfinite(got[0, 0, ~hit]).all())
+    K[0, 0, 100] = 0.0
+    clean = run(Q, K, V, 40, 0)
+    assert torch.equal(got[0, 0, ~hit], clean[0, 0, ~hit])
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-6, 1e6, 1e30])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_values_of_any_magnitude(dtype, scale):
+    Q, K, V = inputs(dtype, 1, 2, 2, 200, 128)
+    V = (V.float() * scale).to(dtype)
+    check(Q, K, V, run(Q, K, V, 70, 4), 70, 4)
+
+
+def test_values_whose_magnitude_changes_along_the_prompt():
+    """Every eighth token's values are larger or smaller by powers of two: each output is dominated by the large ones it sees."""
+    Q, K, V = inputs(BF16, 1, 2, 1, 400, 64)
+    e = torch.randint(-40, 40, (50,), generator=torch.Generator().manual_seed(5)).repeat_interleave(8)
+    V = torch.ldexp(V.float(), e[None, None, :, None]).to(BF16)
+    check(Q, K, V, run(Q, K, V, 60, 3), 60, 3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_sharp_and_flat_attention(dtype):
+    """Logits in the hundreds (one key takes all), and all equal (the mean of what is seen)."""
+    Q, K, V = inputs(dtype, 1, 2, 1, 260, 128, qscale=60.0)
+    check(Q, K, V, run(Q, K, V, 90, 2), 90, 2)
+    Q = torch.zeros_like(Q)
+    check(Q, K, V, run(Q, K, V, 90, 2), 90, 2)
+
+
+def test_two_runs_and_another_stream_give_the_same_bits():
+    Q, K, V = (x.cuda() for x in inputs(BF16, 2, 8, 2, 900, 128))
+    first = binding.d2o_window_attend(Q, K, V, 300, 4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        second = binding.d2o_window_attend(Q, K, V, 300, 4)
+    s.synchronize()
+    assert torch.equal(first, second)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_and_replayed(dtype):
+    Q, K, V = (x.cuda() for x in inputs(dtype, 1, 4, 2, 333, 128))
+    lens = torch.tensor([333], dtype=torch.int32, device="cuda:0")
+    O = torch.zeros_like(Q)
+    binding.d2o_window_attend(Q, K, V, 77, 4, lens, O)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        binding.d2o_window_attend(Q, K, V, 77, 4, lens, O)
+    for seed, m in ((1, 333), (2, 200), (3, 1)):
+        for x, y in zip((Q, K, V), inputs(dtype, 1, 4, 2, 333, 128, seed)):
+            x.copy_(y)
+        lens.fill_(m)
+        O.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        want = binding.d2o_window_attend(Q, K, V, 77, 4, lens)
+        assert torch.equal(O, want) and bool((O[:, :, :m] != 0).any())
+
+
+def test_wrong_arguments_are_refused():
+    Q, K, V = (x.cuda() for x in inputs(BF16, 2, 4, 2, 10, 64))
+    bad = [
+        lambda: binding.d2o_window_attend(Q.cpu(), K, V, 4),
+        lambda: binding.d2o_window_attend(Q, K.float(), V, 4),
+        lambda: binding.d2o_window_attend(Q, K, V[:, :, :9], 4),
+        lambda: binding.d2o_window_attend(Q, K[:, :1].expand(2, 3, 10, 64), V[:, :1].expand(2, 3, 10, 64), 4),
+        lambda: binding.d2o_window_attend(Q, K, V, -1),
+        lambda: binding.d2o_window_attend(Q, K, V, 4, -1),
+        lambda: binding.d2o_window_attend(Q, K, V, 4, lens=torch.tensor([1, 2], device="cuda:0")),
+        lambda: binding.d2o_window_attend(Q, K, V, 4, O=torch.empty(2, 4, 10, 64, device="cuda:0")),
+        lambda: binding.d2o_window_attend(Q[..., :32], K[..., :32], V[..., :32], 4),
+        lambda: binding.d2o_window_attend(Q.transpose(2, 3), K.transpose(2, 3), V.transpose(2, 3), 4),
+    ]
+    for call in bad:
+        with pytest.raises(binding.D2OError):
+            call()
