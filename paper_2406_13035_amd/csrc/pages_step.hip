@@ -1,6 +1,8 @@
 // One generation step over a cache in pages (d2o_pages_step): the new token's row is stored, every query head attends
 // over the entries that its window shows, and the softmax rows are added to the entries' scores.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "pages.h"
 
@@ -23,7 +25,7 @@ int check_pages(const d2o_pages* p, PagePool* out) {
   if (p->cache_fp8 != 0 && p->cache_fp8 != 1) return D2O_ERR_INVALID_ARG;
   if (p->cache_fp8 && p->dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
   if (p->page_size < 1 || p->page_size > 1024 || (p->page_size & (p->page_size - 1))) return D2O_ERR_INVALID_ARG;
-  if (int64_t(p->max_pages) * p->page_size > 0x7FFFFFFF) return D2O_ERR_INVALID_ARG;
+  if (int64_t(p->max_pages) * p->page_size > 0x7FFF0000) return D2O_ERR_INVALID_ARG;
   if (int64_t(p->batch) * p->n_q_heads > 0x3FFFFFFF) return D2O_ERR_INVALID_ARG;
   const int es = p->cache_fp8 ? 1 : p->dtype == D2O_BF16 ? 2 : 4;
   if (!dense_view_ok(p->K, es, true) || !dense_view_ok(p->V, es, true)) return D2O_ERR_INVALID_ARG;
@@ -54,137 +56,483 @@ int check_pages(const d2o_pages* p, PagePool* out) {
 
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaves = 4;       // wavefronts of a workgroup
+constexpr int kTile = 16;       // entries of a tile: the rows of one matrix operand
+constexpr int kRowBcast = 0x150;  // lane i of each row of 16 lanes to all of the row (data-parallel primitive, + i)
+
 struct StepArgs {
   PagePool pool;
   View q, kn, vn, out;
   const int32_t* lens;
   const int32_t* positions;
-  float* logits;  // [B][Hq][max_len]
-  int32_t Hq, G, max_len, window, n_sink;
+  float* logits;   // [B][Hq][pad] base-2 logits of the entries that are seen (scores kept)
+  float* part_o;   // [B * Hkv][splits][G][D] outputs of a share, not normalised
+  float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum
+  int32_t Hq, G, max_len, window, n_sink, pad, splits;
 };
 
-template <typename CT>
-__device__ __forceinline__ float value_at(const uint8_t* row, int i) {
-  return Elem<CT>::to_f32(reinterpret_cast<const CT*>(row)[i]);
+// The tiles of a sequence that hold what a step sees: those of the first tokens, then those from the window's start.  (Where the
+// pages keep positions, entries lie in any order and all tiles are looked at.)
+struct TileList {
+  int n, sink_tiles, rest0, tiles, share;  // entries, tiles of the first tokens, first tile behind them, tiles in all, tiles per workgroup
+  int64_t last;                            // the new token's position
+  __device__ __forceinline__ TileList(const StepArgs& a, int b, int least) {
+    n = min(a.lens[b], a.max_len);
+    if (n <= 0) {
+      n = tiles = share = sink_tiles = rest0 = 0;
+      last = 0;
+      return;
+    }
+    last = a.positions ? a.positions[b] : n - 1;
+    const int all = (n + kTile - 1) / kTile;
+    sink_tiles = rest0 = 0;
+    if (a.window != 0 && !a.pool.pos) {
+      const int64_t lo = last - a.window + 1;  // first entry of the window
+      sink_tiles = (min(a.n_sink, n) + kTile - 1) / kTile;
+      rest0 = int(min(max(lo / kTile, int64_t(sink_tiles)), int64_t(all)));
+      if (lo < 0) rest0 = sink_tiles;
+    }
+    tiles = sink_tiles + all - rest0;
+    if (tiles == 0) {  // nothing is seen: the last tile, whose entries are all masked
+      rest0 = all - 1;
+      tiles = 1;
+    }
+    share = max((tiles + a.splits - 1) / a.splits, least);
+  }
+  __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
+  __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }
+};
+
+// f(0), f(1) .. f(N - 1) with the number as a constant.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, const F& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(const F& f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
-// T: type of q, k, v and out; CT: of the cache's rows.  One workgroup per (sequence, KV head).
+template <int L>
+__device__ __forceinline__ float row_bcast(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kRowBcast + L, 0xF, 0xF, true));
+}
+// v + the same of the lanes 16 and 32 away: every lane gets the sum over the four rows of 16.
+__device__ __forceinline__ float sum_rows(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+  v = __int_as_float(a[0]) + __int_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return __int_as_float(b[0]) + __int_as_float(b[1]);
+}
+
+// What a lane holds of rows of type CT with D elements.  K: lane l has row l % 16 of a tile, chunks of 16 bytes that the four rows of
+// lanes take in turn; V: the 16 lanes of a row of lanes share a row of V, D / 16 elements each.
+template <typename CT, int D>
+struct Rows;
+template <int D>
+struct Rows<uint16_t, D> {
+  static constexpr int kK = D / 32, kE = D / 16;  // 16-byte chunks of K per lane; elements of V per lane
+  typedef std::conditional_t<D == 128, u32x4, u32x2> VReg;
+  bf16x8 q[kK];
+  __device__ __forceinline__ void load_q(const uint16_t* row, int g) {
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+      q[i] = row ? *reinterpret_cast<const bf16x8*>(row + i * 32 + g * 8) : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  }
+  __device__ __forceinline__ f32x4 logits(const u32x4* k, float) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kK; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i]), q[i], s, 0, 0, 0);
+    return s;
+  }
+  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return reinterpret_cast<const VReg*>(row)[c]; }
+  static __device__ __forceinline__ int column(int c, int e) { return c * kE + e; }
+  static __device__ __forceinline__ void values(const VReg& v, float, float* f) {
+#pragma unroll
+    for (int i = 0; i < kE / 2; ++i) {
+      f[2 * i] = __uint_as_float(v[i] << 16);
+      f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+    }
+  }
+};
+template <int D>
+struct Rows<float, D> {
+  static constexpr int kK = D / 16, kE = D / 16;
+  struct VReg {
+    f32x4 x[D / 64];
+  };
+  f32x4 q[kK];
+  __device__ __forceinline__ void load_q(const float* row, int g) {
+#pragma unroll
+    for (int i = 0; i < kK; ++i) q[i] = row ? *reinterpret_cast<const f32x4*>(row + i * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ f32x4 logits(const u32x4* k, float) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kK; ++i) {
+      const f32x4 x = __builtin_bit_cast(f32x4, k[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], q[i][j], s, 0, 0, 0);
+    }
+    return s;
+  }
+  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) {
+    VReg v;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) v.x[i] = reinterpret_cast<const f32x4*>(row)[i * 16 + c];
+    return v;
+  }
+  static __device__ __forceinline__ int column(int c, int e) { return (e / 4) * 64 + c * 4 + e % 4; }
+  static __device__ __forceinline__ void values(const VReg& v, float, float* f) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) f[e] = v.x[e / 4][e % 4];
+  }
+};
+// 8-bit codes: K as bf16 with the row's power of two (exact: four significant bits), V in fp32.
+template <int D>
+struct Rows<uint8_t, D> {
+  static constexpr int kK = D / 64, kE = D / 16;
+  typedef std::conditional_t<D == 128, u32x2, uint32_t> VReg;
+  bf16x8 q[2 * kK];
+  __device__ __forceinline__ void load_q(const uint16_t* row, int g) {
+#pragma unroll
+    for (int i = 0; i < 2 * kK; ++i)
+      q[i] = row ? *reinterpret_cast<const bf16x8*>(row + i / 2 * 64 + g * 16 + i % 2 * 8)
+                 : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  }
+  __device__ __forceinline__ f32x4 logits(const u32x4* k, float scale) const {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 2 * kK; ++i) {
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t w = k[i / 2][i % 2 * 2 + j];
+        x[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+        x[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
+      }
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), q[i], s, 0, 0, 0);
+    }
+    return s;
+  }
+  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return reinterpret_cast<const VReg*>(row)[c]; }
+  static __device__ __forceinline__ int column(int c, int e) { return c * kE + e; }
+  static __device__ __forceinline__ void values(const VReg& v, float scale, float* f) {
+#pragma unroll
+    for (int i = 0; i < kE / 4; ++i) {
+      uint32_t w;
+      if constexpr (D == 128)
+        w = v[i];
+      else
+        w = v;
+      const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false);
+      const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
+      f[4 * i] = lo[0];
+      f[4 * i + 1] = lo[1];
+      f[4 * i + 2] = hi[0];
+      f[4 * i + 3] = hi[1];
+    }
+  }
+};
+
+// out[h] of a (sequence, KV head) from joined partials.
+template <typename T>
+__device__ __forceinline__ void store_out(const StepArgs& a, int b, int hq, int col, float o) {
+  (static_cast<T*>(a.out.ptr) + b * a.out.sb + hq * a.out.sh)[col] = Elem<T>::from_f32(o);
+}
+
+// The new token's row into its page: two wavefronts, one for K and one for V.
 template <typename T, typename CT, int D>
-__global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
-  __shared__ float red[4];
-  __shared__ float qs[D];
-  constexpr float kLog2e = 1.4426950408889634f;
-  const int Hkv = a.pool.Hkv, b = blockIdx.x / Hkv, hk = blockIdx.x % Hkv, tid = threadIdx.x;
-  const int n = min(a.lens[b], a.max_len);
-  T* out = static_cast<T*>(a.out.ptr) + b * a.out.sb;
-  if (n <= 0) {
-    for (int i = tid; i < a.G * D; i += 256) out[(hk * a.G + i / D) * a.out.sh + i % D] = Elem<T>::from_f32(0.f);
+__device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int page, int s, int64_t position) {
+  const int tid = threadIdx.x;
+  const int64_t at = a.pool.at(page, hk, s);
+  if (tid < 128) {
+    const int which = tid >> 6, lane = tid & 63;
+    const View& x = which ? a.vn : a.kn;
+    const T* src = static_cast<const T*>(x.ptr) + b * x.sb + hk * x.sh;
+    CT* dst = reinterpret_cast<CT*>(which ? a.pool.v_at(page, hk, s) : a.pool.k_at(page, hk, s));
+    if constexpr (sizeof(CT) == 1) {
+      float m = 0.f;
+      for (int i = lane; i < D; i += 64) m = fmaxf(m, fabsf(Elem<T>::to_f32(src[i])));
+      const int e = fp8_row_exponent(wave_max(m));
+      for (int i = lane; i < D; i += 64) dst[i] = fp8_code(Elem<T>::to_f32(src[i]), e);
+      if (lane == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at] = int8_t(e);
+    } else {
+      for (int i = lane; i < D; i += 64) dst[i] = src[i];
+    }
+  }
+  if (tid == 0) {
+    if (a.pool.score) a.pool.score[at] = 0.f;
+    if (a.pool.pos) a.pool.pos[at] = int32_t(position);
+  }
+}
+
+// One workgroup per (sequence, KV head, share of its tiles).  U tiles of 16 entries per wavefront and round: the logits of all
+// query heads of the group come from the matrix core (heads are its columns, padded to 16), straight from rows in registers: lane l
+// holds 16 bytes of row l % 16 at a time, and the order of the products' terms is free.  A lane of the result has head
+// l % 16 and four entries of its row of lanes, and that row of lanes reads the rows of V of just these entries: every row of lanes keeps a
+// softmax of its own over the entries it meets, with nothing exchanged in the loop; a probability reaches the lanes of
+// its row by a register broadcast.  P V runs on the vector ALU in fp32 (a rounding of P would cost more bits than the products
+// save: the loads bound the kernel up to 16 heads per group).
+template <typename T, typename CT, int D, int GM, int U>
+__global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
+  typedef Rows<CT, D> R;
+  constexpr int E = R::kE;
+  __shared__ float so[kWaves][GM][D];
+  __shared__ float sml[kWaves][GM][2];
+  const int Hkv = a.pool.Hkv, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const TileList list(a, b, kWaves * U);
+  const int t0 = blockIdx.x * list.share, t1 = min(t0 + list.share, list.tiles);
+  if (list.n == 0) {
+    if (blockIdx.x == 0)
+      for (int i = tid; i < a.G * D; i += 64 * kWaves) store_out<T>(a, b, hk * a.G + i / D, i % D, 0.f);
     return;
   }
-  const int64_t P = a.positions ? a.positions[b] : n - 1;
-  if (a.kn.ptr && a.lens[b] <= a.max_len) {
+  if (t0 >= t1) return;
+  const int n = list.n;
+  // the workgroup of the last tile stores the new token before it reads the tile
+  if (a.kn.ptr && t1 == list.tiles && a.lens[b] <= a.max_len) {
     const int page = a.pool.page_of(b, n - 1);
-    if (page >= 0) {
-      const T* src[2] = {static_cast<const T*>(a.kn.ptr) + b * a.kn.sb + hk * a.kn.sh,
-                         static_cast<const T*>(a.vn.ptr) + b * a.vn.sb + hk * a.vn.sh};
-      const int64_t at = a.pool.at(page, hk, n - 1);
-      if (tid < 128) {
-        const int which = tid >> 6, lane = tid & 63;
-        CT* dst = reinterpret_cast<CT*>(which ? a.pool.v_at(page, hk, n - 1) : a.pool.k_at(page, hk, n - 1));
-        if constexpr (sizeof(CT) == 1) {
-          float m = 0.f;
-          for (int i = lane; i < D; i += 64) m = fmaxf(m, fabsf(Elem<T>::to_f32(src[which][i])));
-          const int e = fp8_row_exponent(wave_max(m));
-          for (int i = lane; i < D; i += 64) dst[i] = fp8_code(Elem<T>::to_f32(src[which][i]), e);
-          if (lane == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at] = int8_t(e);
-        } else {
-          for (int i = lane; i < D; i += 64) dst[i] = src[which][i];
+    if (page >= 0) store_new<T, CT, D>(a, b, hk, page, n - 1, list.last);
+    __threadfence_block();
+    __syncthreads();
+  }
+  R rows;
+  rows.load_q(c < a.G ? static_cast<const T*>(a.q.ptr) + b * a.q.sb + (hk * a.G + c) * a.q.sh : nullptr, g);
+  const float scale2 = kLog2e / sqrtf(float(D));
+  const bool ordered = a.window != 0 && !a.pool.pos, by_pos = a.window != 0 && a.pool.pos;
+  const int64_t lo64 = a.window == 0 ? INT64_MIN : list.last - a.window + 1;  // first position of the window
+  float m = -3.402823466e38f, l = 0.f, acc[GM][E] = {};
+  float* lg = a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
+  const bool big_pages = a.pool.shift >= 4;
+  for (int t = t0 + w * U; t < t1; t += kWaves * U) {
+    u32x4 k[U][R::kK];
+    typename R::VReg v[U][4];
+    float ke[U], ve[U][4];
+    uint32_t seen[U];  // bit i: entry i of the tile is seen
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s0 = t + u < t1 ? list.slot(t + u) : n;  // (a tile behind the share: no entry)
+      const int s = s0 + c;
+      int pk = -1, pv[4];
+      if (big_pages) {  // a tile lies in one page
+        if (s0 < n) pk = a.pool.page_of(b, s0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pv[r] = pk;
+      } else {
+        if (s < n) pk = a.pool.page_of(b, s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pv[r] = __shfl(pk, 4 * g + r, 64);
+      }
+      bool ok = s < n && pk >= 0;
+      if (ordered) ok = ok && (s >= lo64 || s < a.n_sink);
+      if (by_pos && ok) {
+        const int p = a.pool.pos[a.pool.at(pk, hk, s)];
+        ok = p >= lo64 || p < a.n_sink;
+      }
+      seen[u] = uint32_t(__ballot(ok)) & 0xFFFFu;
+      // (rows that are not seen: the first row of the pool instead, whose values are not used)
+      const uint8_t* kr = ok ? a.pool.k_at(pk, hk, s) : a.pool.K;
+#pragma unroll
+      for (int i = 0; i < R::kK; ++i) k[u][i] = reinterpret_cast<const u32x4*>(kr)[i * 4 + g];
+      if constexpr (sizeof(CT) == 1) ke[u] = ok ? pow2_f32(a.pool.k_exp[a.pool.at(pk, hk, s)]) : 1.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int sv = s0 + 4 * g + r;
+        const bool okv = seen[u] >> (4 * g + r) & 1;
+        v[u][r] = R::load_v(okv ? a.pool.v_at(pv[r], hk, sv) : a.pool.V, c);
+        if constexpr (sizeof(CT) == 1) ve[u][r] = okv ? pow2_f32(a.pool.v_exp[a.pool.at(pv[r], hk, sv)]) : 1.f;
+      }
+    }
+    f32x4 s[U];
+    float mx = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = rows.logits(k[u], ke[u]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[u][r] *= scale2;
+        if (!(seen[u] >> (4 * g + r) & 1)) s[u][r] = -INFINITY;
+        mx = fmaxf(mx, s[u][r]);
+      }
+      if (lg && c < a.G && t + u < t1) *reinterpret_cast<f32x4*>(lg + list.slot(t + u) + 4 * g) = s[u];
+    }
+    if (__any(mx > m)) {
+      const float f = __builtin_amdgcn_exp2f(m - mx);
+      m = mx;
+      l *= f;
+      each<GM>([&](auto h) {
+        const float fh = row_bcast<h>(f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[h][e] *= fh;
+      });
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool whole = seen[u] == 0xFFFFu;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(s[u][r] - m);
+        l += p;
+        float f[E];
+        R::values(v[u][r], ve[u][r], f);
+        if (!whole) {
+          const bool okv = seen[u] >> (4 * g + r) & 1;
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[e] = okv ? f[e] : 0.f;
         }
-      }
-      if (tid == 0) {
-        if (a.pool.score) a.pool.score[at] = 0.f;
-        if (a.pool.pos) a.pool.pos[at] = int32_t(P);
+        each<GM>([&](auto h) {
+          const float ph = row_bcast<h>(p);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[h][e] = fmaf(ph, f[e], acc[h][e]);
+        });
       }
     }
-    __threadfence_block();
-    __syncthreads();
   }
-  auto seen = [&](int s, int page) {
-    if (page < 0) return false;
-    if (a.window == 0) return true;
-    const int64_t p = a.pool.pos ? a.pool.pos[a.pool.at(page, hk, s)] : s;
-    return p > P - a.window || p < a.n_sink;
-  };
-  for (int g = 0; g < a.G; ++g) {
-    const int hq = hk * a.G + g;
-    const T* q = static_cast<const T*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh;
-    float* lg = a.logits + (int64_t(b) * a.Hq + hq) * a.max_len;
-    __syncthreads();
-    if (tid < D) qs[tid] = Elem<T>::to_f32(q[tid]) * (kLog2e / sqrtf(float(D)));
-    __syncthreads();
-    float m = -INFINITY;
-    for (int s = tid; s < n; s += 256) {
-      const int page = a.pool.page_of(b, s);
-      float x = -INFINITY;
-      if (seen(s, page)) {
-        const uint8_t* row = a.pool.k_at(page, hk, s);
-        x = 0.f;
-        for (int i = 0; i < D; ++i) x = fmaf(qs[i], value_at<CT>(row, i), x);
-        if constexpr (sizeof(CT) == 1) x = ldexpf(x, a.pool.k_exp[a.pool.at(page, hk, s)]);
-      }
-      lg[s] = x;
-      m = fmaxf(m, x);
+  // join the four rows of lanes, then the wavefronts
+  float mw = fmaxf(m, __shfl_xor(m, 16, 64));
+  mw = fmaxf(mw, __shfl_xor(mw, 32, 64));
+  const float f = __builtin_amdgcn_exp2f(m - mw);
+  l = sum_rows(l * f);
+  each<GM>([&](auto h) {
+    const float fh = row_bcast<h>(f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float o = sum_rows(acc[h][e] * fh);
+      if (g == h % 4) so[w][h][R::column(c, e)] = o;
     }
-    m = wave_max(m);
-    if ((tid & 63) == 0) red[tid >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    __syncthreads();
-    float l = 0.f;
-    for (int s = tid; s < n; s += 256) {
-      const float p = seen(s, a.pool.page_of(b, s)) ? exp2f(lg[s] - m) : 0.f;
-      lg[s] = p;
-      l += p;
-    }
-    l = wave_sum(l);
-    if ((tid & 63) == 0) red[tid >> 6] = l;
-    __threadfence_block();
-    __syncthreads();
-    l = (red[0] + red[1]) + (red[2] + red[3]);
-    bool any = false;
-    if (tid < D) {
-      float o = 0.f;
-      for (int s = 0; s < n; ++s) {
-        const int page = a.pool.page_of(b, s);
-        if (!seen(s, page)) continue;
-        any = true;
-        float v = value_at<CT>(a.pool.v_at(page, hk, s), tid);
-        if constexpr (sizeof(CT) == 1) v = ldexpf(v, a.pool.v_exp[a.pool.at(page, hk, s)]);
-        o = fmaf(lg[s], v, o);
-      }
-      out[hq * a.out.sh + tid] = Elem<T>::from_f32(any ? o / l : 0.f);
-    }
-    if (a.pool.score)
-      for (int s = tid; s < n; s += 256) {
-        const int page = a.pool.page_of(b, s);
-        if (seen(s, page)) a.pool.score[a.pool.at(page, hk, s)] += lg[s] / l;
-      }
+  });
+  if (lane < GM) {
+    sml[w][lane][0] = mw;
+    sml[w][lane][1] = l;
   }
+  __syncthreads();
+  const bool single = list.shares() == 1, lg_kept = a.pool.score != nullptr;
+  for (int i = tid; i < a.G * D; i += 64 * kWaves) {
+    const int h = i / D, col = i % D;
+    float M = sml[0][h][0];
+#pragma unroll
+    for (int x = 1; x < kWaves; ++x) M = fmaxf(M, sml[x][h][0]);
+    float L = 0.f, o = 0.f;
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      const float fx = __builtin_amdgcn_exp2f(sml[x][h][0] - M);
+      L = fmaf(sml[x][h][1], fx, L);
+      o = fmaf(so[x][h][col], fx, o);
+    }
+    const int64_t at = (int64_t(bh) * a.splits + blockIdx.x) * a.G + h;
+    if (single)
+      store_out<T>(a, b, hk * a.G + h, col, L == 0.f ? 0.f : o / L);
+    else
+      a.part_o[at * D + col] = o;
+    if (col == 0 && (lg_kept || !single)) {
+      a.part_ml[at * 2] = M;
+      a.part_ml[at * 2 + 1] = L;
+    }
+  }
+}
+
+// Joins the shares of a (sequence, query head): one workgroup each, a thread per column.
+template <typename T, int D>
+__global__ __launch_bounds__(D) void step_join(StepArgs a, int least) {
+  const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, bh = b * a.pool.Hkv + hq / a.G, h = hq % a.G;
+  const TileList list(a, b, least);
+  const int ns = list.shares();
+  if (ns <= 1) return;
+  const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2;
+  const float* po = a.part_o + (int64_t(bh) * a.splits * a.G + h) * D + threadIdx.x;
+  float M = -3.402823466e38f;
+  for (int i = 0; i < ns; ++i) M = fmaxf(M, ml[int64_t(i) * a.G * 2]);
+  float L = 0.f, o = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < ns; ++i) {
+    const float f = __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M);
+    L = fmaf(ml[int64_t(i) * a.G * 2 + 1], f, L);
+    o = fmaf(po[int64_t(i) * a.G * D], f, o);
+  }
+  store_out<T>(a, b, hq, threadIdx.x, L == 0.f ? 0.f : o / L);
+}
+
+// Adds the softmax rows to the scores (Eq. 6): a thread per entry, the group's query heads in rising order.
+constexpr int kScoreThreads = 256;
+__global__ __launch_bounds__(kScoreThreads) void step_scores(StepArgs a, int least) {
+  __shared__ float M[16], inv[16];
+  const int Hkv = a.pool.Hkv, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv, tid = threadIdx.x;
+  const TileList list(a, b, least);
+  const int first = blockIdx.x * kScoreThreads;
+  if (first >= list.tiles * kTile) return;
+  const int ns = list.shares();
+  if (tid < a.G) {
+    const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + tid) * 2;
+    float m = -3.402823466e38f, L = 0.f;
+    for (int i = 0; i < ns; ++i) m = fmaxf(m, ml[int64_t(i) * a.G * 2]);
+    for (int i = 0; i < ns; ++i) L = fmaf(ml[int64_t(i) * a.G * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - m), L);
+    M[tid] = m;
+    inv[tid] = 1.f / L;
+  }
+  __syncthreads();
+  const int i = first + tid;
+  if (i >= list.tiles * kTile) return;
+  const int s = list.slot(i / kTile) + i % kTile;
+  if (s >= list.n) return;
+  const float* lg = a.logits + (int64_t(b) * a.Hq + hk * a.G) * a.pad + s;
+  float add = 0.f;
+  for (int h = 0; h < a.G; ++h) {
+    const float x = lg[int64_t(h) * a.pad];
+    if (x != -INFINITY) add += __builtin_amdgcn_exp2f(x - M[h]) * inv[h];
+  }
+  if (add != 0.f) {
+    const int page = a.pool.page_of(b, s);
+    if (page >= 0) a.pool.score[a.pool.at(page, hk, s)] += add;
+  }
+}
+
+// Tiles per wavefront and round: 8 KB of rows in flight, half of it where the outputs of 16 heads fill the registers.
+template <typename CT, int D, int GM>
+constexpr int tiles_per_round() {
+  constexpr int u = (GM > 8 ? 8192 : 16384) / (kTile * 2 * D * int(sizeof(CT)));
+  return u < 1 ? 1 : u > 4 ? 4 : u;
+}
+
+template <typename T, typename CT, int D, int GM>
+void launch_step(const StepArgs& a, int batch, hipStream_t s) {
+  constexpr int U = tiles_per_round<CT, D, GM>();
+  const int bh = batch * a.pool.Hkv;
+  step_part<T, CT, D, GM, U><<<dim3(a.splits, bh), 64 * kWaves, 0, s>>>(a);
+  if (a.splits > 1) step_join<T, D><<<dim3(batch * a.Hq), D, 0, s>>>(a, kWaves * U);
+  if (a.pool.score) step_scores<<<dim3((a.pad + kScoreThreads - 1) / kScoreThreads, bh), kScoreThreads, 0, s>>>(a, kWaves * U);
+}
+
+template <typename T, typename CT, int D>
+void launch_step(const StepArgs& a, int batch, hipStream_t s) {
+  if (a.G == 1) launch_step<T, CT, D, 1>(a, batch, s);
+  else if (a.G == 2) launch_step<T, CT, D, 2>(a, batch, s);
+  else if (a.G <= 4) launch_step<T, CT, D, 4>(a, batch, s);
+  else if (a.G <= 8) launch_step<T, CT, D, 8>(a, batch, s);
+  else launch_step<T, CT, D, 16>(a, batch, s);
 }
 
 template <typename T, typename CT>
 void launch_step(const StepArgs& a, int batch, int D, hipStream_t s) {
-  const dim3 grid(batch * a.pool.Hkv);
-  if (D == 64)
-    step_kernel<T, CT, 64><<<grid, 256, 0, s>>>(a);
-  else
-    step_kernel<T, CT, 128><<<grid, 256, 0, s>>>(a);
+  if (D == 64) launch_step<T, CT, 64>(a, batch, s);
+  else launch_step<T, CT, 128>(a, batch, s);
+}
+
+int step_splits(int64_t bh, int max_len) {
+  const int64_t tiles = (int64_t(max_len) + kTile - 1) / kTile;
+  const int64_t want = std::max<int64_t>(1, 1024 / bh);
+  return int(std::max<int64_t>(1, std::min<int64_t>(want, tiles / (2 * kWaves))));
 }
 
 }  // namespace
 
 size_t pages_step_bytes(const d2o_pages* p, int32_t max_len) {
-  return round256(size_t(p->batch) * p->n_q_heads * max_len * sizeof(float));
+  const size_t bh = size_t(p->batch) * p->n_kv_heads, hq = size_t(p->batch) * p->n_q_heads, pad = (size_t(max_len) + kTile - 1) / kTile * kTile;
+  const size_t splits = step_splits(bh, max_len);
+  return round256(p->score ? hq * pad * sizeof(float) : 0) + round256(hq * splits * p->head_dim * sizeof(float)) +
+         round256(hq * splits * 2 * sizeof(float));
 }
 
 }  // namespace d2o
@@ -219,7 +567,16 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   a.out = to_view(out);
   a.lens = lens;
   a.positions = positions;
-  a.logits = static_cast<float*>(workspace);
+  const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads, hq = int64_t(pages->batch) * pages->n_q_heads;
+  if (bh > 65535) return D2O_ERR_UNSUPPORTED;
+  a.pad = (max_len + kTile - 1) / kTile * kTile;
+  a.splits = step_splits(bh, max_len);
+  char* ws = static_cast<char*>(workspace);
+  a.logits = reinterpret_cast<float*>(ws);
+  ws += round256(pages->score ? size_t(hq) * a.pad * sizeof(float) : 0);
+  a.part_o = reinterpret_cast<float*>(ws);
+  ws += round256(size_t(hq) * a.splits * pages->head_dim * sizeof(float));
+  a.part_ml = reinterpret_cast<float*>(ws);
   a.Hq = pages->n_q_heads;
   a.G = pages->n_q_heads / pages->n_kv_heads;
   a.max_len = max_len;
