@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <type_traits>
+#include <utility>
 
 namespace d2o {
 
@@ -16,6 +17,16 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) double f64x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+// f(0), f(1) .. f(N - 1) with the number as a constant.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, const F& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(const F& f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
 
 // Storage element traits: float and bf16 (held as uint16_t).
 template <typename T>

@@ -1,8 +1,6 @@
 // One generation step over a cache in pages (d2o_pages_step): the new token's row is stored, every query head attends
 // over the entries that its window shows, and the softmax rows are added to the entries' scores.
 #include <algorithm>
-#include <type_traits>
-#include <utility>
 
 #include "pages.h"
 
@@ -103,16 +101,6 @@ struct TileList {
   __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
   __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }
 };
-
-// f(0), f(1) .. f(N - 1) with the number as a constant.
-template <typename F, int... I>
-__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, const F& f) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, typename F>
-__device__ __forceinline__ void each(const F& f) {
-  each_of(std::make_integer_sequence<int, N>{}, f);
-}
 
 template <int L>
 __device__ __forceinline__ float row_bcast(float v) {

@@ -1,61 +1,582 @@
 // Causal prompt attention over a window of recent tokens and a few first ones (d2o_window_attend).
+//
+// Query i sees the keys j <= i with j > i - window or j < n_sink.  A workgroup owns a block of query rows and walks the 64-key (bf16)
+// or 32-key (fp32) tiles that any of its rows sees: those of the first tokens, then those from its first row's window start to its
+// last row.  Both kernels keep S^T = K Q^T in the matrix core's accumulator layout, where a lane owns one query, so that a row's
+// maximum and sum are taken in registers, and choose the keys' order such that these registers are the operand of
+// O^T = V^T P^T as they are.
 #include <algorithm>
+#include <type_traits>
 
 #include "pages.h"
 
 namespace d2o {
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kFloor = -1e30f;  // exponent reference before a row has seen a key
+
 struct WindowArgs {
   View q, k, v, o;
   const int32_t* lens;
   int32_t n, Hq, G, window, n_sink;  // window: at least 1, INT32_MAX without one
+  // bf16: transposed values and a record per tile of 64 keys
+  uint16_t* vt;  // [B][Hkv][tiles][D][64] fp16, every group of eight keys scaled by a power of two of its own
+  float* rec;    // [B][Hkv][tiles][kRec]: exponents of the groups (of the even ones, then of the odd ones), a flag
+  int32_t tiles, blocks, reverse;
+};
+constexpr int kRec = 16;  // floats per record
+
+// The tiles of BN keys that the rows [r0, r1] see: `sinks` tiles of first tokens, then those from `rest0`.
+struct Tiles {
+  int sinks, rest0, count;
+  __device__ __forceinline__ Tiles(const WindowArgs& a, int r0, int r1, int BN) {
+    const int lo = max(0, r0 + 1 - a.window);
+    sinks = (min(a.n_sink, r1 + 1) + BN - 1) / BN;
+    rest0 = max(lo / BN, sinks);
+    const int end = r1 / BN + 1;
+    rest0 = min(rest0, end);
+    sinks = min(sinks, end);
+    count = sinks + end - rest0;
+  }
+  __device__ __forceinline__ int tile(int t) const { return t < sinks ? t : rest0 + t - sinks; }
 };
 
-// One wavefront per query: 64 keys at a time, a key per lane for the logits, D / 64 columns per lane for the output.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void window_row(WindowArgs a) {
-  constexpr float kLog2e = 1.4426950408889634f;
-  __shared__ float qs[D];
-  const int i = blockIdx.x, hq = blockIdx.y % a.Hq, b = blockIdx.y / a.Hq, hk = hq / a.G, lane = threadIdx.x;
+__device__ __forceinline__ bool sees(const WindowArgs& a, int i, int j) {
+  return j <= i && (j > i - a.window || j < a.n_sink);
+}
+// Whether any of the rows [r0, r1] sees any of the keys [k0, k1], and whether each sees all of them.
+__device__ __forceinline__ bool any_seen(const WindowArgs& a, int r0, int r1, int k0, int k1) {
+  return k0 <= r1 && (k1 > r0 - a.window || k0 < a.n_sink);
+}
+__device__ __forceinline__ bool all_seen(const WindowArgs& a, int r0, int r1, int k0, int k1) {
+  return k1 <= r0 && (k0 > r1 - a.window || k1 < a.n_sink);
+}
+
+// Workgroup number -> (block of rows, head and sequence).  Workgroups go to the chip's eight XCDs, each with an L2 of its own, in
+// turn; here each XCD gets a contiguous run of (head, block), so that blocks that share most of their window meet in one L2.
+// Without a window (reverse) the work grows with the block's position: the longest blocks of all heads first.
+__device__ __forceinline__ void place(const WindowArgs& a, int heads, int& block, int& hz) {
+  constexpr int kXcd = 8;
+  const int total = a.blocks * heads, lin = blockIdx.x;
+  if (a.reverse) {
+    block = a.blocks - 1 - lin / heads;
+    hz = lin % heads;
+    return;
+  }
+  const int xcd = lin % kXcd, q = total / kXcd, r = total % kXcd, at = xcd * q + min(xcd, r) + lin / kXcd;
+  hz = at / a.blocks;
+  block = at % a.blocks;
+}
+
+__device__ __forceinline__ float max_halves(float v) {  // with the lane 32 away
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return fmaxf(__int_as_float(s[0]), __int_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return __int_as_float(s[0]) + __int_as_float(s[1]);
+}
+
+// ---- bf16 ----------------------------------------------------------------------------------
+// The product with V runs in fp16: probabilities rounded to bf16 would cost 2^-8 each, as much as the output's own rounding; in
+// fp16 they cost 2^-11.  V is converted once, in a transposing pass, each group of eight keys divided by a power of two 2^e that
+// brings its largest magnitude to [2^13, 2^14) (exact: bf16 has eight significant bits), and the probabilities of the group
+// are multiplied by 2^e in the exponent.  (One e for the head would lose rows whose window holds small values
+// only.)  A group less than 2^12 below its tile's largest keeps the tile's e, so that nearly every tile has one e.  Infinities and NaN of V count as zero here and are added to the rows that see them at the end.
+
+constexpr int kGroupLd = 512 + 32;  // LDS elements from one group of rows (1 KB, one load instruction) to the next
+// A tile's rows of 256 (128) bytes lie four (eight) to a group; chunk k (16 bytes) of a row sits at k ^ x within its four, x from the row:
+// the 16 lanes of a 128-bit access phase then meet all banks once.
+__device__ __forceinline__ int swz(int chunk, int x) { return ((chunk & ~3) << 3) + (((chunk & 3) ^ x) << 3); }
+__device__ __forceinline__ int at256(int row, int chunk) { return (row >> 2) * kGroupLd + (row & 3) * 128 + swz(chunk, row & 3); }
+__device__ __forceinline__ int at128(int row, int chunk) { return (row >> 3) * kGroupLd + (row & 7) * 64 + swz(chunk, (row >> 1) & 3); }
+
+constexpr float kPShift = 12.f;  // probabilities are formed as 2^12 * p before the fp16 rounding
+constexpr float kLazy = 3.f;     // log2 of the growth the exponent reference tolerates before it moves
+
+// MFMA row -> key offset inside 32 keys, such that accumulator registers 8 kb .. 8 kb + 7 of lane half h hold the keys 16 kb + 8 h .. + 7.
+__device__ __forceinline__ int perm_key(int m) { return (m & ~0xC) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+// V [b][h][n][D] -> vt and rec.  One workgroup per tile.
+template <int D>
+__global__ __launch_bounds__(256) void window_values(WindowArgs a) {
+  __shared__ uint16_t t[64][D + 2];
+  __shared__ uint32_t top[8];
+  __shared__ int odd;
+  const int tile = blockIdx.x, Hkv = a.Hq / a.G, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv, tid = threadIdx.x;
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
-  if (i >= n) return;
-  const T* q = static_cast<const T*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh + i * a.q.sn;
-  const T* k = static_cast<const T*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
-  const T* v = static_cast<const T*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
-  for (int c = lane; c < D; c += 64) qs[c] = Elem<T>::to_f32(q[c]) * (kLog2e / sqrtf(float(D)));
-  __syncthreads();
-  const int lo = max(0, int(int64_t(i) + 1 - a.window)), sinks = min(a.n_sink, lo), seen = sinks + i + 1 - lo;
-  float m = -1e30f, l = 0.f, o[D / 64] = {};
-  for (int t0 = 0; t0 < seen; t0 += 64) {
-    const int t = t0 + lane, j = t < sinks ? t : lo + t - sinks;
-    float s = -INFINITY;
-    if (t < seen) {
-      s = 0.f;
-      for (int c = 0; c < D; ++c) s = fmaf(qs[c], Elem<T>::to_f32(k[j * a.k.sn + c]), s);
+  if (tile * 64 >= n) return;
+  constexpr int kChunks = D / 8, kRows = 256 / kChunks, kRound = 64 / kRows;  // chunks per row, rows per round, rounds
+  const uint16_t* src = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
+  if (tid < 8) top[tid] = 0;
+  if (tid == 8) odd = 0;
+  u32x4 v[kRound];
+  uint32_t m[kRound];
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < kRound; ++u) {
+    const int row = u * kRows + tid / kChunks, col = tid % kChunks * 8;
+    v[u] = u32x4{0, 0, 0, 0};
+    if (tile * 64 + row < n) v[u] = *reinterpret_cast<const u32x4*>(src + int64_t(tile * 64 + row) * a.v.sn + col);
+    m[u] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((v[u][i] & 0x7F800000u) == 0x7F800000u) v[u][i] &= 0x0000FFFFu, bad = true;
+      if ((v[u][i] & 0x7F80u) == 0x7F80u) v[u][i] &= 0xFFFF0000u, bad = true;
+      m[u] = max(m[u], max(v[u][i] & 0x7FFF0000u, v[u][i] << 16 & 0x7FFF0000u));
     }
-    const float mn = fmaxf(m, wave_max(s)), p = t < seen ? exp2f(s - mn) : 0.f, f = exp2f(m - mn);
-    m = mn;
-    l = l * f + wave_sum(p);
-    for (int c = 0; c < D / 64; ++c) o[c] *= f;
-    for (int u = 0; u < min(64, seen - t0); ++u) {
-      const float pu = __shfl(p, u, 64);
-      const int64_t ju = __shfl(j, u, 64);
-      for (int c = 0; c < D / 64; ++c) o[c] = fmaf(pu, Elem<T>::to_f32(v[ju * a.v.sn + c * 64 + lane]), o[c]);
+    // the lanes of eight rows: at most a wavefront
+#pragma unroll
+    for (int o = 1; o < kChunks; o <<= 1) m[u] = max(m[u], uint32_t(__shfl_xor(int(m[u]), o, 64)));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kRound; ++u)
+    if (tid % kChunks == 0) atomicMax(&top[(u * kRows + tid / kChunks) / 8], m[u]);
+  if (bad) odd = 1;
+  __syncthreads();
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) all = max(all, top[i]);
+  // exponent of the largest magnitude, brought to 13 (biased exponents; subnormal values count as the lowest)
+  auto exponent = [](uint32_t bits) { return max(int(bits >> 23), 1) - 127 - 13; };
+  const int e_tile = all ? exponent(all) : 0;
+  auto group_exponent = [&](int gr) __attribute__((always_inline)) {
+    const int e = top[gr] ? exponent(top[gr]) : e_tile;
+    return e < e_tile - 12 ? e : e_tile;
+  };
+  float* rec = a.rec + (int64_t(bh) * a.tiles + tile) * kRec;
+  if (tid < 8) rec[(tid & 1) * 4 + tid / 2] = float(group_exponent(tid));
+  if (tid == 8) rec[8] = odd ? 1.f : 0.f;
+#pragma unroll
+  for (int u = 0; u < kRound; ++u) {
+    const int row = u * kRows + tid / kChunks, col = tid % kChunks * 8, e = group_exponent(row / 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const _Float16 lo = (_Float16)ldexpf(__uint_as_float(v[u][i] << 16), -e);
+      const _Float16 hi = (_Float16)ldexpf(__uint_as_float(v[u][i] & 0xFFFF0000u), -e);
+      *reinterpret_cast<uint32_t*>(&t[row][col + 2 * i]) = __builtin_bit_cast(uint16_t, lo) | uint32_t(__builtin_bit_cast(uint16_t, hi)) << 16;
     }
   }
-  T* out = static_cast<T*>(a.o.ptr) + b * a.o.sb + hq * a.o.sh + i * a.o.sn;
-  for (int c = 0; c < D / 64; ++c) out[c * 64 + lane] = Elem<T>::from_f32(o[c] / l);
+  __syncthreads();
+  uint16_t* dst = a.vt + (int64_t(bh) * a.tiles + tile) * D * 64;
+  for (int c = tid; c < D * 8; c += 256) {
+    const int dd = c >> 3, kc = (c & 7) * 8;
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = t[kc + 2 * i][dd] | uint32_t(t[kc + 2 * i + 1][dd]) << 16;
+    *reinterpret_cast<u32x4*>(dst + dd * 64 + kc) = o;
+  }
+}
+
+template <int D>
+constexpr int tile_elems() { return D / 8 * kGroupLd; }  // a tile of K, and of V^T, in LDS
+
+// NW wavefronts of 32 query rows.  K and V^T tiles are double-buffered in LDS, filled straight from memory; the two halves of the
+// wavefronts run half a tile apart, one forming its probabilities on the vector ALU while the other runs P V of its tile and
+// Q K^T of the next on the matrix core.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_bf16(WindowArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+  constexpr int kElems = tile_elems<D>(), kDC = D / 32, kKS = D / 16, BM = 32 * NW;
+  uint16_t* Ks = smem;               // [2][kElems]
+  uint16_t* Vs = smem + 2 * kElems;  // [2][kElems]
+  const int Hkv = a.Hq / a.G;
+  int blk, hz;
+  place(a, gridDim.x / a.blocks, blk, hz);
+  const int hq = hz % a.Hq, b = hz / a.Hq, hk = hq / a.G;
+  const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
+  const int r0 = blk * BM;
+  if (r0 >= n) return;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, m = lane & 31, h = lane >> 5;
+  const float scale2 = kLog2e / sqrtf(float(D));
+  const Tiles tl(a, r0, min(r0 + BM, n) - 1, 64);
+  const int ntile = tl.count;
+  const uint16_t* kbase = static_cast<const uint16_t*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
+  const int64_t vt0 = (int64_t(b) * Hkv + hk) * a.tiles;
+  const uint16_t* vtbase = a.vt + vt0 * D * 64;
+  const float* rec = a.rec + vt0 * kRec;
+  // a tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB
+  auto load_k = [&](int t) __attribute__((always_inline)) {
+    constexpr int kPer = 512 / D;  // rows per instruction
+    const int k0 = tl.tile(t) * 64;
+#pragma unroll
+    for (int i = 0; i < 64 / kPer / NW; ++i) {
+      const int lr = (w * (64 / kPer / NW) + i) * kPer + lane / (D / 8);
+      const int row = (lr & 32) | perm_key(lr & 31);
+      const int sw = D == 128 ? swz(lane & 15, lr & 3) : swz(lane & 7, (lr >> 1) & 3);
+      load_lds16(kbase + int64_t(min(k0 + row, n - 1)) * a.k.sn + sw, Ks + (t & 1) * kElems + (w * (64 / kPer / NW) + i) * kGroupLd);
+    }
+  };
+  auto load_v = [&](int t) __attribute__((always_inline)) {
+    const uint16_t* src = vtbase + int64_t(tl.tile(t)) * D * 64;
+#pragma unroll
+    for (int i = 0; i < D / 8 / NW; ++i) {
+      const int row = (w * (D / 8 / NW) + i) * 8 + (lane >> 3);
+      load_lds16(src + row * 64 + swz(lane & 7, (row >> 1) & 3), Vs + (t & 1) * kElems + (w * (D / 8 / NW) + i) * kGroupLd);
+    }
+  };
+  const int wr0 = r0 + w * 32, q_row = wr0 + m;
+  bf16x8 bq[kKS];
+  load_k(0);
+  {
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh + int64_t(min(q_row, n - 1)) * a.q.sn;
+#pragma unroll
+    for (int ks = 0; ks < kKS; ++ks) bq[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16 + h * 8);
+  }
+  load_v(0);
+  if (ntile > 1) load_k(1);
+  auto exps_of = [&](int t) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(rec + int64_t(tl.tile(t)) * kRec + h * 4); };
+  f32x4 ex = exps_of(0), ex_next = ex;
+
+  f32x16 o[kDC];
+#pragma unroll
+  for (int i = 0; i < kDC; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  // mrun: exponent reference of o; el: the sum is kept relative to mrun - el
+  float mrun = kFloor, el = 0.f, lsum = 0.f;
+  f32x16 s[2];
+  f16x8 pb[2][2];
+  auto active = [&](int t) __attribute__((always_inline)) {
+    const int k0 = tl.tile(t) * 64;
+    return any_seen(a, wr0, wr0 + 31, k0, k0 + 63);
+  };
+  // probabilities of one group of eight registers (sub-tile st, half kb) with exponent reference c
+  auto form = [&](int st, int kb, float c) __attribute__((always_inline)) {
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[st][8 * kb + r], scale2, -c));
+      sum += p;
+      pb[st][kb][r] = (_Float16)p;
+    }
+    return sum;
+  };
+  auto softmax = [&](int t) __attribute__((always_inline)) {
+    const int k0 = tl.tile(t) * 64;
+    if (!all_seen(a, wr0, wr0 + 31, k0, k0 + 63)) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + st * 32 + (r >> 3) * 16 + h * 8 + (r & 7);
+          if (!sees(a, q_row, key)) s[st][r] = -INFINITY;
+        }
+    }
+    float mx[4];
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        float x = s[st][8 * kb];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) x = fmaxf(x, s[st][8 * kb + r]);
+        mx[st * 2 + kb] = x;
+      }
+    const float e0 = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(ex[0])));
+    const bool one = __all(ex[0] == e0 && ex[1] == e0 && ex[2] == e0 && ex[3] == e0);
+    float top;
+    if (one)
+      top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), scale2, e0);
+    else
+      top = fmaxf(fmaxf(fmaf(mx[0], scale2, ex[0]), fmaf(mx[1], scale2, ex[1])),
+                  fmaxf(fmaf(mx[2], scale2, ex[2]), fmaf(mx[3], scale2, ex[3])));
+    const float cand = max_halves(top) - kPShift;
+    const bool grew = cand > mrun + kLazy;
+    if (__any(grew)) {  // wavefront-uniform: no rescale when no row's maximum moved
+      const float mnew = grew ? cand : mrun, enew = grew ? e0 : el;
+      const float f = __builtin_amdgcn_exp2f(mrun - mnew);
+      lsum *= __builtin_amdgcn_exp2f((mrun - mnew) - (el - enew));
+      mrun = mnew;
+      el = enew;
+#pragma unroll
+      for (int i = 0; i < kDC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= f;
+    }
+    if (one) {
+      const float c = mrun - e0;
+      float sum = form(0, 0, c);
+      sum += form(0, 1, c);
+      sum += form(1, 0, c);
+      sum += form(1, 1, c);
+      lsum += ldexpf(sum, int(el - e0));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lsum += ldexpf(form(i >> 1, i & 1, mrun - ex[i]), int(el - ex[i]));
+    }
+  };
+  // o += V^T P^T of tile t, then S^T = K Q^T of tile t + 1; LDS operands are fetched two batches of four ahead
+  constexpr int kPV = 4 * kDC, kQK = 2 * kKS;
+  auto operand = [&](int t, auto i) __attribute__((always_inline)) -> u32x4 {
+    constexpr int idx = decltype(i)::value;
+    if constexpr (idx < kPV) {
+      constexpr int st = idx / (2 * kDC), kb = idx / kDC % 2, dc = idx % kDC;
+      return *reinterpret_cast<const u32x4*>(&Vs[(t & 1) * kElems + at128(dc * 32 + m, st * 4 + kb * 2 + h)]);
+    }
+    const int st = (idx - kPV) & 1, ks = (idx - kPV) >> 1, row = st * 32 + m, chunk = ks * 2 + h;
+    return *reinterpret_cast<const u32x4*>(&Ks[((t + 1) & 1) * kElems + (D == 128 ? at256(row, chunk) : at128(row, chunk))]);
+  };
+  auto issue = [&](auto i, const u32x4& x) __attribute__((always_inline)) {
+    constexpr int idx = decltype(i)::value;
+    if constexpr (idx < kPV) {
+      constexpr int st = idx / (2 * kDC), kb = idx / kDC % 2, dc = idx % kDC;
+      o[dc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), pb[st][kb], o[dc], 0, 0, 0);
+    } else {
+      constexpr int st = (idx - kPV) & 1, ks = (idx - kPV) >> 1;
+      const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      s[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), bq[ks], ks == 0 ? zero : s[st], 0, 0, 0);
+    }
+  };
+  auto products = [&](int t, auto first, auto last) __attribute__((always_inline)) {
+    constexpr int i0 = decltype(first)::value, NB = (decltype(last)::value - i0) / 4;
+    u32x4 A[2][4];
+    each<8>([&](auto i) { A[i / 4][i % 4] = operand(t, std::integral_constant<int, i0 + i>{}); });
+    each<NB>([&](auto bt) {
+      __builtin_amdgcn_sched_barrier(0);
+      each<4>([&](auto i) { issue(std::integral_constant<int, i0 + 4 * bt + i>{}, A[bt & 1][i]); });
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (bt + 2 < NB)
+        each<4>([&](auto i) { A[bt & 1][i] = operand(t, std::integral_constant<int, i0 + 4 * (bt + 2) + i>{}); });
+    });
+  };
+  typedef std::integral_constant<int, 0> P0;
+  typedef std::integral_constant<int, kPV> P1;
+  typedef std::integral_constant<int, kPV + kQK> P2;
+  auto matrix = [&](int t, bool pv, bool qk) __attribute__((always_inline)) {  // the wavefront in its matrix phase issues first
+    __builtin_amdgcn_s_setprio(1);
+    if (pv && qk)
+      products(t, P0{}, P2{});
+    else if (pv)
+      products(t, P0{}, P1{});
+    else if (qk)
+      products(t, P1{}, P2{});
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  const bool late = w >= NW / 2;
+#pragma unroll
+  for (int ks = 0; ks < kKS; ++ks) asm volatile("" ::"v"(bq[ks]));  // the queries have arrived
+  wait_vm<0>();
+  __syncthreads();
+  bool now = active(0);
+  if (now) {
+    products(-1, P1{}, P2{});  // S of tile 0
+    if (!late) softmax(0);
+  }
+  __syncthreads();
+  for (int t = 0; t < ntile; ++t) {
+    const bool more = t + 1 < ntile, next = more && active(t + 1);
+    if (t + 2 < ntile) load_k(t + 2);
+    if (more) {
+      load_v(t + 1);
+      ex_next = exps_of(t + 1);
+    }
+    if (late) {
+      if (now) softmax(t);
+      matrix(t, now, next);
+    } else {
+      matrix(t, now, next);
+    }
+    ex = ex_next;
+    if (!late && next) softmax(t + 1);
+    now = next;
+    wait_vm<0>();  // this wavefront's part of the next tiles is in LDS
+    __syncthreads();
+  }
+  // infinities and NaN of V, which counted as zero above: a row that sees one takes it as it is, whatever its weight
+  for (int t0 = 0; t0 < ntile; t0 += 64) {
+    const int t = t0 + lane;
+    uint64_t flagged = __ballot(t < ntile && rec[int64_t(tl.tile(min(t, ntile - 1))) * kRec + 8] != 0.f);
+    while (flagged) {
+      const int k0 = tl.tile(t0 + __builtin_ctzll(flagged)) * 64;
+      flagged &= flagged - 1;
+      const uint16_t* vsrc = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
+      for (int j = k0; j < min(k0 + 64, n); ++j) {
+        if (!sees(a, q_row, j)) continue;
+        const uint16_t* row = vsrc + int64_t(j) * a.v.sn;
+        each<kDC>([&](auto dc) {
+          each<16>([&](auto r) {
+            const float x = Elem<uint16_t>::to_f32(row[dc * 32 + (r >> 2) * 8 + h * 4 + (r & 3)]);
+            if (!(fabsf(x) < INFINITY)) o[dc][decltype(r)::value] += x;
+          });
+        });
+      }
+    }
+  }
+  const float inv = 1.f / sum_of_halves(lsum);
+  if (q_row >= n) return;
+  // registers 4 rg .. 4 rg + 3 hold columns 32 dc + 8 rg + 4 h + 0..3: the lanes of a row swap halves of a register pair, so that
+  // each stores eight consecutive columns
+  const int ie = int(el);
+  uint16_t* out = static_cast<uint16_t*>(a.o.ptr) + b * a.o.sb + hq * a.o.sh + int64_t(q_row) * a.o.sn;
+#pragma unroll
+  for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = Elem<uint16_t>::from_f32(ldexpf(o[dc][8 * h2 + 2 * i] * inv, ie)) |
+               uint32_t(Elem<uint16_t>::from_f32(ldexpf(o[dc][8 * h2 + 2 * i + 1] * inv, ie))) << 16;
+      const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+      *reinterpret_cast<u32x4*>(out + dc * 32 + h2 * 16 + h * 8) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+    }
+}
+
+// ---- fp32 ----------------------------------------------------------------------------------
+// Four wavefronts of 16 query rows, tiles of 32 keys, all products on the fp32 matrix instruction (16 x 16 x 4): S^T of 16 keys
+// leaves the four keys 4 g + r in register r of lane row g, and register r is the operand of the product whose V rows are
+// 4 g + r.  Tiles pass through registers on their way to LDS; an infinity or NaN of V counts as zero there and is added at the end.
+template <int D>
+__global__ __launch_bounds__(256) void window_f32(WindowArgs a) {
+  constexpr int BN = 32, BM = 64, kLd = D + 4, kLoads = BN * D / 4 / 256;
+  __shared__ __attribute__((aligned(16))) float Ks[2][BN * kLd], Vs[2][BN * kLd];
+  __shared__ int odd;
+  int blk, hz;
+  place(a, gridDim.x / a.blocks, blk, hz);
+  const int hq = hz % a.Hq, b = hz / a.Hq, hk = hq / a.G;
+  const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
+  const int r0 = blk * BM;
+  if (r0 >= n) return;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const float scale2 = kLog2e / sqrtf(float(D));
+  const Tiles tl(a, r0, min(r0 + BM, n) - 1, BN);
+  const float* kbase = static_cast<const float*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
+  const float* vbase = static_cast<const float*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
+  f32x4 kr[kLoads], vr[kLoads];
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    const int k0 = tl.tile(t) * BN;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = tid + 256 * i, row = x / (D / 4), col = x % (D / 4) * 4;
+      const int64_t j = min(k0 + row, n - 1);
+      kr[i] = *reinterpret_cast<const f32x4*>(kbase + j * a.k.sn + col);
+      vr[i] = *reinterpret_cast<const f32x4*>(vbase + j * a.v.sn + col);
+    }
+  };
+  auto stage = [&](int buf) __attribute__((always_inline)) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = tid + 256 * i, row = x / (D / 4), col = x % (D / 4) * 4;
+      *reinterpret_cast<f32x4*>(&Ks[buf][row * kLd + col]) = kr[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!(fabsf(vr[i][j]) < INFINITY)) vr[i][j] = 0.f, bad = true;
+      *reinterpret_cast<f32x4*>(&Vs[buf][row * kLd + col]) = vr[i];
+    }
+    if (bad) odd = 1;
+  };
+  const int wr0 = r0 + w * 16, q_row = wr0 + c;
+  f32x4 q[D / 16];
+  fetch(0);
+  const float* qp = static_cast<const float*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh + int64_t(min(q_row, n - 1)) * a.q.sn;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const f32x4*>(qp + i * 16 + g * 4);
+  if (tid == 0) odd = 0;
+  __syncthreads();
+  stage(0);
+  __syncthreads();
+  float m = kFloor, l = 0.f;
+  f32x4 o[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < tl.count; ++t) {
+    if (t + 1 < tl.count) fetch(t + 1);
+    const float *Kt = Ks[t & 1], *Vt = Vs[t & 1];
+    const int k0 = tl.tile(t) * BN;
+#pragma unroll
+    for (int st = 0; st < BN / 16; ++st) {
+      const int j0 = k0 + st * 16;
+      if (!any_seen(a, wr0, wr0 + 15, j0, j0 + 15)) continue;
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&Kt[(st * 16 + c) * kLd + i * 16 + g * 4]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], q[i][j], s, 0, 0, 0);
+      }
+      const bool whole = all_seen(a, wr0, wr0 + 15, j0, j0 + 15);
+      float mx = m;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[r] *= scale2;
+        if (!whole && !sees(a, q_row, j0 + 4 * g + r)) s[r] = -INFINITY;
+        mx = fmaxf(mx, s[r]);
+      }
+      const auto x16 = __builtin_amdgcn_permlane16_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+      mx = max_halves(fmaxf(__int_as_float(x16[0]), __int_as_float(x16[1])));
+      if (__any(mx > m)) {
+        const float f = __builtin_amdgcn_exp2f(m - mx);
+        m = mx;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] *= f;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(s[r] - m);
+        l += p;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vt[(st * 16 + 4 * g + r) * kLd + i * 16 + c], p, o[i], 0, 0, 0);
+      }
+    }
+    if (t + 1 < tl.count) stage((t + 1) & 1);
+    __syncthreads();
+  }
+  if (odd)
+    for (int t = 0; t < tl.count; ++t)
+      for (int j = tl.tile(t) * BN; j < min(tl.tile(t) * BN + BN, n); ++j)
+        if (sees(a, q_row, j)) {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float x = vbase[j * a.v.sn + i * 16 + g * 4 + r];
+              if (!(fabsf(x) < INFINITY)) o[i][r] += x;
+            }
+        }
+  const auto x16 = __builtin_amdgcn_permlane16_swap(__float_as_int(l), __float_as_int(l), false, false);
+  l = sum_of_halves(__int_as_float(x16[0]) + __int_as_float(x16[1]));
+  if (q_row >= n) return;
+  const float inv = 1.f / l;
+  float* out = static_cast<float*>(a.o.ptr) + b * a.o.sb + hq * a.o.sh + int64_t(q_row) * a.o.sn;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(out + i * 16 + g * 4) = o[i] * inv;
 }
 
 int check_window(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
   if (batch < 1 || n < 1 || n_kv_heads < 1) return D2O_ERR_INVALID_ARG;
   if (dtype != D2O_F32 && dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
   if (head_dim != 64 && head_dim != 128) return D2O_ERR_UNSUPPORTED;
+  if (n > 0x7FFF0000 || int64_t(batch) * n_kv_heads > 65535) return D2O_ERR_UNSUPPORTED;
   return D2O_OK;
 }
 
-size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) { return 256; }
+size_t values_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim) {
+  return size_t(batch) * n_kv_heads * ((n + 63) / 64) * head_dim * 64 * sizeof(uint16_t);
+}
+size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
+  if (dtype == D2O_F32) return 16;  // (nothing is kept there)
+  return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * kRec * sizeof(float);
+}
+
+template <int D, int NW>
+hipError_t run_bf16(WindowArgs& a, int batch, hipStream_t s) {
+  a.blocks = (a.n + 32 * NW - 1) / (32 * NW);
+  constexpr int kSmem = 4 * tile_elems<D>() * int(sizeof(uint16_t));
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (e != hipSuccess) return e;
+  window_values<D><<<dim3(a.tiles, batch * (a.Hq / a.G)), 256, 0, s>>>(a);
+  window_bf16<D, NW><<<dim3(unsigned(a.blocks) * batch * a.Hq), 64 * NW, kSmem, s>>>(a);
+  return hipGetLastError();
+}
 
 }  // namespace
 }  // namespace d2o
@@ -82,14 +603,34 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
     if (!dense_view_ok(*v, es, true)) return D2O_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
   if (workspace_bytes < window_bytes(batch, n, n_kv_heads, head_dim, dtype)) return D2O_ERR_CAPACITY;
-  if (int64_t(batch) * n_q_heads > 65535) return D2O_ERR_UNSUPPORTED;
-  WindowArgs a{to_view(Q), to_view(K), to_view(V), to_view(O), lens, n, n_q_heads, n_q_heads / n_kv_heads,
-               window ? window : INT32_MAX, n_sink};
-  const dim3 grid(n, batch * n_q_heads);
+  if (int64_t(batch) * n_q_heads * ((n + 63) / 64) > 0x7FFFFFFF) return D2O_ERR_UNSUPPORTED;
+  WindowArgs a{};
+  a.q = to_view(Q);
+  a.k = to_view(K);
+  a.v = to_view(V);
+  a.o = to_view(O);
+  a.lens = lens;
+  a.n = n;
+  a.Hq = n_q_heads;
+  a.G = n_q_heads / n_kv_heads;
+  a.window = window ? window : INT32_MAX;
+  a.n_sink = n_sink;
+  a.tiles = (n + 63) / 64;
+  a.reverse = a.window > n / 2;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == D2O_BF16)
-    head_dim == 64 ? window_row<uint16_t, 64><<<grid, 64, 0, s>>>(a) : window_row<uint16_t, 128><<<grid, 64, 0, s>>>(a);
-  else
-    head_dim == 64 ? window_row<float, 64><<<grid, 64, 0, s>>>(a) : window_row<float, 128><<<grid, 64, 0, s>>>(a);
+  if (dtype == D2O_BF16) {
+    a.vt = static_cast<uint16_t*>(workspace);
+    a.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + values_bytes(batch, n, n_kv_heads, head_dim));
+    const bool few = int64_t((n + 127) / 128) * n_q_heads * batch <= 512;
+    hipError_t e;
+    if (head_dim == 64)
+      e = few ? run_bf16<64, 4>(a, batch, s) : run_bf16<64, 8>(a, batch, s);
+    else
+      e = few ? run_bf16<128, 4>(a, batch, s) : run_bf16<128, 8>(a, batch, s);
+    return e == hipSuccess ? D2O_OK : D2O_ERR_HIP;
+  }
+  a.blocks = (n + 63) / 64;
+  const dim3 grid(unsigned(a.blocks) * batch * n_q_heads);
+  head_dim == 64 ? window_f32<64><<<grid, 256, 0, s>>>(a) : window_f32<128><<<grid, 256, 0, s>>>(a);
   return hipGetLastError() == hipSuccess ? D2O_OK : D2O_ERR_HIP;
 }
