@@ -2,15 +2,15 @@
 // its budget back to it, in place (d2o_pages_evict).  Both choose by Eq. 7-8: the first tokens, the last ones, and the
 // highest scores among the others.
 #include <algorithm>
+#include <type_traits>
 
 #include "pages.h"
 
 namespace d2o {
 namespace {
 
-constexpr int kSelThreads = 1024;
-
-// Order-preserving integer of a score: larger keys are kept first.  0 is below every score, 0xFFFFFFFF above.
+// Order-preserving integer of a score: larger keys are kept first.  0 is below every score, kProtected above.
+constexpr uint32_t kProtected = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t score_key(float x) {
   if (x != x) return 0xFFFFFFFEu;
   if (x == 0.f) x = 0.f;  // -0 and +0 compare equal
@@ -18,67 +18,113 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// Exclusive prefix sum of v over the workgroup's threads, and the total.
-__device__ __forceinline__ void block_scan(int v, int& before, int& total, int* wa) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  int inc = v;
+// ---- selection of one head by one workgroup.  Radix select from the top: a histogram of 2048 bins of the candidates' next eleven
+// bits, then the bin in which the count from above reaches what is still wanted.  (Eleven bits: sign, exponent and two bits of the
+// fraction spread accumulated attention over a few dozen bins, so that the lanes of a wavefront seldom meet in one; with eight, the
+// exponent alone, they queue.)
+constexpr int kBins = 2048;
+
+struct SelectShared {
+  int hist[kBins];
+  int wave[16];
+  int bin, left, above;
+};
+
+// One digit: of the n candidates counted into sh.hist, the bin that holds the `want`-th largest (1-based), and how many are wanted of
+// that bin.  All threads; sh.hist is free again when it returns.
+template <int NT>
+__device__ __forceinline__ void pick_bin(SelectShared& sh, int want) {
+  constexpr int kPer = kBins / NT;  // bins per thread, from the top: thread 0 has the largest
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  __syncthreads();
+  int h[kPer], tot = 0;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) tot += h[u] = sh.hist[kBins - 1 - tid * kPer - u];
+  int inc = tot;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int t = __shfl_up(inc, o, 64);
     if (lane >= o) inc += t;
   }
+  if (lane == 63) sh.wave[w] = inc;
   __syncthreads();
-  if (lane == 63) wa[w] = inc;
-  __syncthreads();
-  int off = 0, all = 0;
-  for (int i = 0; i < nw; ++i) {
-    if (i < w) off += wa[i];
-    all += wa[i];
+  for (int i = 0; i < w; ++i) inc += sh.wave[i];
+  int left = want - (inc - tot);
+  if (left > 0 && want <= inc) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      if (left > 0 && h[u] >= left) {
+        sh.bin = kBins - 1 - tid * kPer - u;
+        sh.left = left;
+        sh.above = h[u];
+        left = 0;
+      }
+      left -= h[u];
+    }
   }
-  before = off + inc - v;
-  total = all;
+  __syncthreads();
+}
+template <int NT>
+__device__ __forceinline__ void clear_bins(SelectShared& sh) {
+  for (int i = threadIdx.x; i < kBins; i += NT) sh.hist[i] = 0;
+  __syncthreads();
 }
 
-// The `want`-th largest (1-based) of key(0 .. n-1): its value, and how many keys equal to it belong to the `want`
-// largest.  Digits of eight bits from the top: a histogram of the candidates' digits, the bin in which the count from above reaches
-// what is still wanted.
-template <typename Key, typename F>
-__device__ void nth_largest(int n, int want, const F& key, Key& value, int& equal, int* hist, int* sh) {
-  const int tid = threadIdx.x;
-  Key prefix = 0, mask = 0;
-  for (int shift = int(sizeof(Key)) * 8 - 8; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += kSelThreads) {
-      const Key k = key(j);
-      if ((k & mask) == prefix) atomicAdd(&hist[int(k >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (tid < 64) {  // lane i: bins 255 - 4 i down to 252 - 4 i
-      int h[4], tot = 0;
-      for (int u = 0; u < 4; ++u) tot += h[u] = hist[255 - 4 * tid - u];
-      int inc = tot;
+// The `want`-th largest of the 32-bit values that `each_value(f)` hands to f(value) on all threads together; `equal` becomes how many of
+// those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.
+template <int NT, int FIRST = 0, typename F>
+__device__ __forceinline__ uint32_t nth_largest(SelectShared& sh, int want, int& equal, int& same, const F& each_value) {
+  uint32_t prefix = 0;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(inc, o, 64);
-        if (tid >= o) inc += t;
-      }
-      int left = want - (inc - tot);
-      if (left > 0 && want <= inc) {
-        int u = 0;
-        while (h[u] < left) left -= h[u++];
-        sh[0] = 255 - 4 * tid - u;
-        sh[1] = left;
-      }
-    }
-    __syncthreads();
-    prefix |= Key(sh[0]) << shift;
-    mask |= Key(0xFF) << shift;
-    want = sh[1];
-    __syncthreads();
+  for (int pass = FIRST; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t digit = pass == 2 ? 1023u : 2047u;
+    clear_bins<NT>(sh);
+    each_value([&](uint32_t v) {
+      if (pass == 0 || (v >> (pass == 1 ? 21 : 10)) == (prefix >> (pass == 1 ? 21 : 10))) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
+    });
+    pick_bin<NT>(sh, want);
+    prefix |= uint32_t(sh.bin) << shift;
+    want = sh.left;
+    same = sh.above;
   }
-  value = prefix;
+  __syncthreads();
   equal = want;
+  return prefix;
+}
+
+// Ranks in entry order for entries u * NT + thread: counts of two predicates per (u, wavefront) in `cnt` (16 bits each, at most 65535
+// entries), turned into the counts before.
+template <int NT, int PT>
+__device__ __forceinline__ void prefix_counts(uint32_t* cnt) {
+  constexpr int kN = PT * (NT / 64), kPer = (kN + 63) / 64;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    uint32_t v[kPer], tot = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      v[i] = lane * kPer + i < kN ? cnt[lane * kPer + i] : 0;
+      tot += v[i];
+    }
+    uint32_t inc = tot;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t t = __shfl_up(int(inc), o, 64);
+      if (lane >= o) inc += t;
+    }
+    uint32_t run = inc - tot;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (lane * kPer + i < kN) cnt[lane * kPer + i] = run;
+      run += v[i];
+    }
+    if (lane == 63) cnt[kN] = run;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
 
 struct FillArgs {
@@ -86,60 +132,204 @@ struct FillArgs {
   View k, v;
   const int32_t* lens;
   const float* scores;
-  int32_t* src;  // [B][Hkv][budget] kept positions, rising (only where something is evicted)
-  int32_t n, budget, recent, n_sink;
-};
+  int32_t* src;    // [B][Hkv][budget] kept positions, rising (prompts of at most kFillSelect tokens of which some are evicted)
+  uint16_t* hist;  // longer prompts: [B][Hkv][slices][kBins] of a slice's keys
+  int32_t* slice;  // [B][Hkv][slices][2] kept entries before a slice: above the threshold, equal to it
+  uint32_t* mark;  // [B][Hkv][2] threshold, how many equal to it are kept
+  int32_t n, budget, recent, n_sink, slices;
 
-__global__ __launch_bounds__(kSelThreads) void fill_select(FillArgs a) {
-  __shared__ int hist[256], wa[16], sh[2];
-  const int bh = blockIdx.x, b = bh / a.pool.Hkv, tid = threadIdx.x;
-  const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
+  __device__ __forceinline__ int length(int b) const { return lens ? min(max(lens[b], 0), n) : n; }
+  __device__ __forceinline__ uint32_t key(const float* sc, int j, int late) const {
+    return j < n_sink || j >= late ? kProtected : score_key(sc[j]);
+  }
+};
+constexpr int kFillSelect = 16384;  // tokens of a prompt that one workgroup holds in registers
+
+// Prompts of at most NT * PT tokens: keys in registers, the kept positions to a list.
+template <int NT, int PT>
+__global__ __launch_bounds__(NT) void fill_select(FillArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ uint32_t cnt[PT * (NT / 64) + 1];
+  const int bh = blockIdx.x, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = a.length(b);
   if (n <= a.budget) return;
   const float* sc = a.scores + int64_t(bh) * a.n;
-  const int late = n - a.recent;
-  auto key = [&](int j) { return j < a.n_sink || j >= late ? 0xFFFFFFFFu : score_key(sc[j]); };
-  uint32_t value;
-  int equal;
-  nth_largest<uint32_t>(n, a.budget, key, value, equal, hist, sh);
+  uint32_t key[PT];
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const int j = u * NT + tid;
+    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
+  }
+  int equal, same;
+  const uint32_t t = nth_largest<NT>(sh, a.budget, equal, same, [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < PT; ++u)
+      if (u * NT + tid < n) f(key[u]);
+  });
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const uint32_t c = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
+    if (lane == 0) cnt[u * (NT / 64) + w] = c;
+  }
+  prefix_counts<NT, PT>(cnt);
   int32_t* src = a.src + int64_t(bh) * a.budget;
-  int kept = 0, same = 0;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const uint32_t k = j < n ? key(j) : 0u;
-    const bool eq = j < n && k == value;
-    int before, total;
-    block_scan(eq, before, total, wa);
-    const bool keep = j < n && (k > value || (eq && same + before < equal));
-    same += total;
-    block_scan(keep, before, total, wa);
-    if (keep) src[kept + before] = j;
-    kept += total;
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const uint32_t c = cnt[u * (NT / 64) + w];
+    const bool gt = key[u] > t, eq = key[u] == t;
+    const int above = int(c & 0xFFFF) + lanes_before(__ballot(gt)), rank = int(c >> 16) + lanes_before(__ballot(eq));
+    if (gt || (eq && rank < equal)) src[above + min(rank, equal)] = u * NT + tid;
   }
 }
 
-// 16 bytes of a prompt row per lane, consecutive lanes consecutive chunks.
+// Longer prompts, in slices of kSlice tokens.  First a histogram of every slice's top digits ...
+constexpr int kSlice = 4096, kSliceThreads = 256, kSlicePer = kSlice / kSliceThreads;
+__global__ __launch_bounds__(kSliceThreads) void fill_hist(FillArgs a) {
+  __shared__ int hist[kBins];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, tid = threadIdx.x, j0 = blockIdx.x * kSlice;
+  const int n = a.length(b);
+  if (n <= a.budget || j0 >= n) return;
+  const float* sc = a.scores + int64_t(bh) * a.n;
+  uint32_t key[kSlicePer];
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const int j = j0 + u * kSliceThreads + tid;
+    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
+  }
+  for (int i = tid; i < kBins; i += kSliceThreads) hist[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u)
+    if (j0 + u * kSliceThreads + tid < n) atomicAdd(&hist[key[u] >> 21], 1);
+  __syncthreads();
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.hist + (int64_t(bh) * a.slices + blockIdx.x) * kBins);
+  for (int i = tid; i < kBins / 2; i += kSliceThreads) out[i] = uint32_t(hist[2 * i]) | uint32_t(hist[2 * i + 1]) << 16;
+}
+
+// ... then one workgroup per head: the bin that holds the threshold, the tokens in it (their other bits and their slice) into LDS,
+// the threshold among those, and how many entries each slice keeps.  (More candidates than fit: the head's scores are
+// read again for every digit.)
+constexpr int kMark = 1024, kCand = 24576, kMaxSlices = 2048;
+__global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ uint32_t cand[kCand];
+  __shared__ int gt[kMaxSlices], eq[kMaxSlices];
+  __shared__ int ncand;
+  const int bh = blockIdx.x, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63;
+  const int n = a.length(b), late = n - a.recent;
+  if (n <= a.budget) return;
+  const int slices = (n + kSlice - 1) / kSlice;
+  const float* sc = a.scores + int64_t(bh) * a.n;
+  const uint32_t* hist = reinterpret_cast<const uint32_t*>(a.hist + int64_t(bh) * a.slices * kBins);
+  int lo = 0, hi = 0;
+#pragma unroll 8
+  for (int s = 0; s < slices; ++s) {
+    const uint32_t v = hist[int64_t(s) * (kBins / 2) + tid];
+    lo += v & 0xFFFF;
+    hi += v >> 16;
+  }
+  sh.hist[2 * tid] = lo;
+  sh.hist[2 * tid + 1] = hi;
+  for (int i = tid; i < slices; i += kMark) gt[i] = eq[i] = 0;
+  if (tid == 0) ncand = 0;
+  pick_bin<kMark>(sh, a.budget);
+  const uint32_t top = sh.bin;
+  const int want = sh.left, total = sh.above;
+  __syncthreads();
+  const bool fits = total <= kCand;
+  constexpr int kBatch = 16;  // loads in flight per thread; a wavefront's 64 tokens lie in one slice
+  for (int j0 = 0; j0 < n; j0 += kBatch * kMark) {
+    uint32_t k[kBatch];
+    int in_all = 0;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int j = j0 + u * kMark + tid;
+      k[u] = j < n ? a.key(sc, j, late) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int j = j0 + u * kMark + tid;
+      const uint64_t above = __ballot(j < n && k[u] >> 21 > top);
+      if (above && lane == 0) atomicAdd(&gt[j / kSlice], __popcll(above));
+      in_all += __popcll(__ballot(j < n && k[u] >> 21 == top));
+    }
+    if (!in_all || !fits) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&ncand, in_all);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int j = j0 + u * kMark + tid;
+      const bool is = j < n && k[u] >> 21 == top;
+      const uint64_t in = __ballot(is);
+      if (is) cand[at + lanes_before(in)] = (k[u] & 0x1FFFFF) | uint32_t(j / kSlice) << 21;
+      at += __popcll(in);
+    }
+  }
+  __syncthreads();
+  auto each_low = [&](auto f) {  // the lower 21 bits of the bin's keys, and their slice
+    if (fits) {
+      for (int i = tid; i < total; i += kMark) f(cand[i] & 0x1FFFFF, cand[i] >> 21);
+    } else {
+      for (int j = tid; j < n; j += kMark) {
+        const uint32_t k = a.key(sc, j, late);
+        if (k >> 21 == top) f(k & 0x1FFFFF, uint32_t(j) / kSlice);
+      }
+    }
+  };
+  int equal, same;
+  const uint32_t low = nth_largest<kMark, 1>(sh, want, equal, same, [&](auto f) { each_low([&](uint32_t v, uint32_t) { f(v); }); });
+  each_low([&](uint32_t v, uint32_t s) {
+    if (v > low) atomicAdd(&gt[s], 1);
+    if (v == low) atomicAdd(&eq[s], 1);
+  });
+  __syncthreads();
+  if (tid < 64) {  // counts before each slice
+    int g0 = 0, e0 = 0;
+    for (int s0 = 0; s0 < slices; s0 += 64) {
+      const int g = s0 + lane < slices ? gt[s0 + lane] : 0, e = s0 + lane < slices ? eq[s0 + lane] : 0;
+      int gi = g, ei = e;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(gi, o, 64), y = __shfl_up(ei, o, 64);
+        if (lane >= o) gi += x, ei += y;
+      }
+      if (s0 + lane < slices) {
+        int32_t* out = a.slice + (int64_t(bh) * a.slices + s0 + lane) * 2;
+        out[0] = g0 + gi - g;
+        out[1] = e0 + ei - e;
+      }
+      g0 += __shfl(gi, 63, 64);
+      e0 += __shfl(ei, 63, 64);
+    }
+    if (tid == 0) {
+      a.mark[bh * 2] = top << 21 | low;
+      a.mark[bh * 2 + 1] = equal;
+    }
+  }
+}
+
+// Token j of the prompt to entry s: 16 bytes of the row per lane, consecutive lanes consecutive chunks.
 template <typename T, typename CT, int D>
-__global__ __launch_bounds__(256) void fill_rows(FillArgs a) {
-  constexpr int kLanes = D * int(sizeof(T)) / 16, kRows = 256 / kLanes, kE = 16 / int(sizeof(T));
-  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv;
-  const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
-  const int s = blockIdx.x * kRows + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-  if (s >= min(n, a.budget)) return;
+__device__ __forceinline__ void put_row(const FillArgs& a, int bh, int b, int hk, int s, int j, int c) {
+  constexpr int kLanes = D * int(sizeof(T)) / 16, kE = 16 / int(sizeof(T));
   const int page = a.pool.page_of(b, s);
   if (page < 0) return;
-  const int j = n <= a.budget ? s : a.src[int64_t(bh) * a.budget + s];
   const int64_t at = a.pool.at(page, hk, s);
+  u32x4 t[2];
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const View& x = which ? a.v : a.k;
-    const T* row = static_cast<const T*>(x.ptr) + b * x.sb + hk * x.sh + int64_t(j) * x.sn;
-    const u32x4 t = reinterpret_cast<const u32x4*>(row)[c];
+    t[which] = reinterpret_cast<const u32x4*>(static_cast<const T*>(x.ptr) + b * x.sb + hk * x.sh + int64_t(j) * x.sn)[c];
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
     uint8_t* dst = which ? a.pool.v_at(page, hk, s) : a.pool.k_at(page, hk, s);
     if constexpr (sizeof(CT) == 1) {
       float f[kE], m = 0.f;
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
-        f[i] = __uint_as_float(i & 1 ? t[i / 2] & 0xFFFF0000u : t[i / 2] << 16);
+        f[i] = __uint_as_float(i & 1 ? t[which][i / 2] & 0xFFFF0000u : t[which][i / 2] << 16);
         m = fmaxf(m, fabsf(f[i]));
       }
 #pragma unroll
@@ -151,13 +341,67 @@ __global__ __launch_bounds__(256) void fill_rows(FillArgs a) {
       reinterpret_cast<u32x2*>(dst)[c] = u32x2{w[0], w[1]};
       if (c == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at] = int8_t(e);
     } else {
-      reinterpret_cast<u32x4*>(dst)[c] = t;
+      reinterpret_cast<u32x4*>(dst)[c] = t[which];
     }
   }
   if (c == 0) {
     if (a.pool.score) a.pool.score[at] = a.scores ? a.scores[int64_t(bh) * a.n + j] : 0.f;
     if (a.pool.pos) a.pool.pos[at] = j;
   }
+}
+
+template <typename T, typename CT, int D>
+__global__ __launch_bounds__(256) void fill_rows(FillArgs a) {
+  constexpr int kLanes = D * int(sizeof(T)) / 16, kRows = 256 / kLanes;
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv;
+  const int n = a.length(b);
+  const int s = blockIdx.x * kRows + threadIdx.x / kLanes;
+  if (s >= min(n, a.budget)) return;
+  put_row<T, CT, D>(a, bh, b, hk, s, n <= a.budget ? s : a.src[int64_t(bh) * a.budget + s], threadIdx.x % kLanes);
+}
+
+// ... and the slices' kept rows, in order behind those of the slices before.
+template <typename T, typename CT, int D>
+__global__ __launch_bounds__(kSliceThreads) void fill_slice(FillArgs a) {
+  constexpr int kLanes = D * int(sizeof(T)) / 16, kRows = kSliceThreads / kLanes;
+  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
+  __shared__ uint16_t list[kSlice];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = a.length(b), j0 = blockIdx.x * kSlice, c = tid % kLanes;
+  if (j0 >= n) return;
+  if (n <= a.budget) {
+    for (int j = j0 + tid / kLanes; j < min(j0 + kSlice, n); j += kRows) put_row<T, CT, D>(a, bh, b, hk, j, j, c);
+    return;
+  }
+  const float* sc = a.scores + int64_t(bh) * a.n;
+  const uint32_t t = a.mark[bh * 2];
+  const int equal = a.mark[bh * 2 + 1];
+  const int32_t* before = a.slice + (int64_t(bh) * a.slices + blockIdx.x) * 2;
+  const int gt0 = before[0], eq0 = before[1];
+  uint32_t key[kSlicePer];
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const int j = j0 + u * kSliceThreads + tid;
+    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
+  }
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const uint32_t v = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
+    if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = v;
+  }
+  prefix_counts<kSliceThreads, kSlicePer>(cnt);
+  const int quota = max(0, equal - eq0);  // of the equal ones of this slice
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const uint32_t v = cnt[u * (kSliceThreads / 64) + w];
+    const bool gt = key[u] > t, eq = key[u] == t;
+    const int above = int(v & 0xFFFF) + lanes_before(__ballot(gt)), rank = int(v >> 16) + lanes_before(__ballot(eq));
+    if (gt || (eq && rank < quota)) list[above + min(rank, quota)] = uint16_t(u * kSliceThreads + tid);
+  }
+  const uint32_t all = cnt[kSlicePer * (kSliceThreads / 64)];
+  const int kept = int(all & 0xFFFF) + min(int(all >> 16), quota), s0 = gt0 + min(eq0, equal);
+  __syncthreads();
+  for (int i = tid / kLanes; i < kept; i += kRows) put_row<T, CT, D>(a, bh, b, hk, s0 + i, j0 + list[i], c);
 }
 
 struct EvictArgs {
@@ -167,69 +411,10 @@ struct EvictArgs {
   int32_t* count;  // [B][Hkv] pairs
   int32_t max_len, budget, recent, n_sink, most;
 };
+constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself
 
-__global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs a) {
-  __shared__ int hist[256], wa[16], sh[2];
-  const int bh = blockIdx.x, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x;
-  const int n = min(a.lens[b], a.max_len), S = a.budget;
-  if (n <= S) {
-    if (tid == 0) a.count[bh] = 0;
-    return;
-  }
-  int newest = INT32_MIN;
-  for (int j = tid; j < n; j += kSelThreads) {
-    const int page = a.pool.page_of(b, j);
-    if (page >= 0) newest = max(newest, a.pool.pos[a.pool.at(page, hk, j)]);
-  }
-  newest = -wave_min(newest == INT32_MIN ? INT32_MAX : -newest);
-  if ((tid & 63) == 0) wa[tid >> 6] = newest;
-  __syncthreads();
-  for (int i = 0; i < 16; ++i) newest = max(newest, wa[i]);
-  __syncthreads();
-  const int64_t late = int64_t(newest) - a.recent;
-  // protected entries first, then by score, then by position; entries without a page last
-  auto key = [&](int j) -> uint64_t {
-    const int page = a.pool.page_of(b, j);
-    if (page < 0) return 0;
-    const int64_t at = a.pool.at(page, hk, j);
-    const int32_t p = a.pool.pos[at];
-    const uint32_t hi = p < a.n_sink || p > late ? 0xFFFFFFFFu : score_key(a.pool.score[at]);
-    return uint64_t(hi) << 32 | ~(uint32_t(p) ^ 0x80000000u);
-  };
-  uint64_t value;
-  int equal;
-  nth_largest<uint64_t>(n, S, key, value, equal, hist, sh);
-  int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
-  int32_t* from = hole + a.most;
-  int holes = 0, rows = 0, same = 0;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const uint64_t k = j < n ? key(j) : 0u;
-    const bool eq = j < n && k == value;
-    int before, total;
-    block_scan(eq, before, total, wa);
-    const bool keep = j < n && (k > value || (eq && same + before < equal));
-    same += total;
-    const bool is_hole = j < S && !keep && a.pool.page_of(b, j) >= 0, is_row = j >= S && keep && k != 0;
-    block_scan(is_hole, before, total, wa);
-    if (is_hole && holes + before < a.most) hole[holes + before] = j;
-    holes += total;
-    block_scan(is_row, before, total, wa);
-    if (is_row && rows + before < a.most) from[rows + before] = j;
-    rows += total;
-  }
-  if (tid == 0) a.count[bh] = min(min(holes, rows), a.most);
-}
-
-// Kept rows into the holes: sources lie at or behind the budget, targets below it.
-template <int ROW>  // bytes of a row
-__global__ __launch_bounds__(256) void evict_move(EvictArgs a) {
-  constexpr int kLanes = ROW / 16, kRows = 256 / kLanes;
-  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv;
-  const int i = blockIdx.x * kRows + threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-  if (i >= a.count[bh]) return;
-  const int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
-  const int to = hole[i], from = hole[a.most + i];
+// A kept row into a hole: sources lie at or behind the budget, targets below it, so that moves never meet.
+__device__ __forceinline__ void move_row(const EvictArgs& a, int b, int hk, int from, int to, int c) {
   const int pt = a.pool.page_of(b, to), pf = a.pool.page_of(b, from);
   if (pt < 0 || pf < 0) return;
   const u32x4 k = reinterpret_cast<const u32x4*>(a.pool.k_at(pf, hk, from))[c];
@@ -247,11 +432,228 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a) {
   }
 }
 
+// What decides about an entry: protected ones first, then by score, then by position; without a page last.
+struct Rank {
+  uint32_t key, low;
+};
+__device__ __forceinline__ Rank rank_of(const EvictArgs& a, float score, int32_t p, int64_t late) {
+  return {p < a.n_sink || p > late ? kProtected : score_key(score), ~(uint32_t(p) ^ 0x80000000u)};
+}
+template <int NT>
+__device__ __forceinline__ int block_max(int v, int* buf) {
+  v = -wave_min(-max(v, -INT32_MAX));
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+  __syncthreads();
+  for (int i = 0; i < NT / 64; ++i) v = max(v, buf[i]);
+  __syncthreads();
+  return v;
+}
+
+// One workgroup per head, entries u * NT + thread: in registers (PT of them per thread) or, PT = 0, read again for every use.
+template <int NT, int PT>
+__global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
+  __shared__ SelectShared sh;
+  __shared__ uint32_t cnt[(PT ? PT : 16) * (NT / 64) + 1];
+  __shared__ int lists[2 * kInline];
+  const int bh = blockIdx.x, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = min(a.lens[b], a.max_len), S = a.budget;
+  const bool here = a.most <= kInline;
+  if (n <= S) {
+    if (tid == 0 && !here) a.count[bh] = 0;
+    return;
+  }
+  constexpr int kKeep = PT ? PT : 1;
+  float score[kKeep];
+  int32_t pos[kKeep];
+  uint32_t present = 0;  // bit u
+  int newest = -INT32_MAX;
+  auto look = [&](int j, float& sc, int32_t& p) __attribute__((always_inline)) {
+    const int page = j < n ? a.pool.page_of(b, j) : -1;
+    sc = 0.f;
+    p = 0;
+    if (page < 0) return false;
+    const int64_t at = a.pool.at(page, hk, j);
+    sc = a.pool.score[at];
+    p = a.pool.pos[at];
+    return true;
+  };
+  if constexpr (PT > 0) {
+#pragma unroll
+    for (int u = 0; u < PT; ++u)
+      if (look(u * NT + tid, score[u], pos[u])) present |= 1u << u;
+#pragma unroll
+    for (int u = 0; u < PT; ++u)
+      if (present >> u & 1) newest = max(newest, pos[u]);
+  } else {
+    for (int j = tid; j < n; j += NT) {
+      float sc;
+      int32_t p;
+      if (look(j, sc, p)) newest = max(newest, p);
+    }
+  }
+  newest = block_max<NT>(newest, sh.wave);
+  const int64_t late = int64_t(newest) - a.recent;
+  Rank r[kKeep];
+  if constexpr (PT > 0) {
+#pragma unroll
+    for (int u = 0; u < PT; ++u) {
+      r[u] = rank_of(a, score[u], pos[u], late);
+      if (!(present >> u & 1)) r[u] = {0, 0};
+    }
+  }
+  auto rank_at = [&](int j) __attribute__((always_inline)) {
+    float sc;
+    int32_t p;
+    return look(j, sc, p) ? rank_of(a, sc, p, late) : Rank{0, 0};
+  };
+  auto each_rank = [&](auto f) __attribute__((always_inline)) {  // f(entry, rank)
+    if constexpr (PT > 0) {
+#pragma unroll
+      for (int u = 0; u < PT; ++u)
+        if (u * NT + tid < n) f(u * NT + tid, r[u]);
+    } else {
+      for (int j = tid; j < n; j += NT) f(j, rank_at(j));
+    }
+  };
+
+  if (n == S + 1) {  // one entry goes: the lowest, of equals the last
+    uint32_t key = 0xFFFFFFFFu, low = 0xFFFFFFFFu;
+    int at = -1;
+    auto take = [&](uint32_t k, uint32_t l, int j) __attribute__((always_inline)) {
+      if (k < key || (k == key && (l < low || (l == low && j > at)))) key = k, low = l, at = j;
+    };
+    each_rank([&](int j, const Rank& x) { take(x.key, x.low, j); });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+      take(uint32_t(__shfl_xor(int(key), o, 64)), uint32_t(__shfl_xor(int(low), o, 64)), __shfl_xor(at, o, 64));
+    if (lane == 0) {
+      sh.hist[w] = int(key);
+      sh.hist[16 + w] = int(low);
+      sh.hist[32 + w] = at;
+    }
+    __syncthreads();
+    for (int i = 0; i < NT / 64; ++i) take(uint32_t(sh.hist[i]), uint32_t(sh.hist[16 + i]), sh.hist[32 + i]);
+    if (!here) {
+      if (tid == 0) {
+        int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
+        hole[0] = at;
+        hole[a.most] = S;
+        a.count[bh] = at < S ? 1 : 0;
+      }
+    } else if (at < S && tid < lanes) {
+      move_row(a, b, hk, S, at, tid);  // (no move if either has no page)
+    }
+    return;
+  }
+
+  int equal, same;
+  const uint32_t t = nth_largest<NT>(sh, S, equal, same, [&](auto f) __attribute__((always_inline)) {
+    each_rank([&](int, const Rank& x) { f(x.key); });
+  });
+  // of several entries with the threshold's key only some are kept: those with the lowest positions
+  uint32_t tl = 0;
+  bool split = equal < same;
+  if (split)
+    tl = nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
+      each_rank([&](int, const Rank& x) {
+        if (x.key == t) f(x.low);
+      });
+    });
+  auto above = [&](const Rank& x) { return x.key > t || (x.key == t && (!split || x.low > tl)); };
+  auto level = [&](const Rank& x) { return split && x.key == t && x.low == tl; };
+  int32_t *hole = lists, *from = lists + kInline;
+  if (!here) {
+    hole = a.moves + int64_t(bh) * 2 * a.most;
+    from = hole + a.most;
+  }
+  constexpr int kU = PT ? PT : 16;  // rounds of NT entries ranked together
+  int holes = 0, rows = 0, levels = 0;
+  for (int j0 = 0; j0 < n; j0 += kU * NT) {
+    Rank x[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = j0 + u * NT + tid;
+      if constexpr (PT > 0)
+        x[u] = r[u];
+      else
+        x[u] = rank_at(j);
+    }
+    __syncthreads();
+    // the ranks of the entries level with the threshold (entry order)
+    uint32_t keep = 0;
+    if (split) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const uint64_t m = __ballot(j0 + u * NT + tid < n && level(x[u]));
+        if (lane == 0) cnt[u * (NT / 64) + w] = __popcll(m);
+      }
+      prefix_counts<NT, kU>(cnt);
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const bool in = j0 + u * NT + tid < n, lv = in && level(x[u]);
+      const uint64_t m = __ballot(lv);
+      bool k = in && above(x[u]);
+      if (split && lv) k = levels + int(cnt[u * (NT / 64) + w]) + lanes_before(m) < equal;
+      if (k) keep |= 1u << u;
+    }
+    if (split) levels += int(cnt[kU * (NT / 64)]);
+    __syncthreads();
+    // holes below the budget and kept rows behind it
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = j0 + u * NT + tid;
+      const bool there = x[u].key != 0, k = keep >> u & 1;
+      const uint64_t mh = __ballot(j < n && j < S && !k && there), mr = __ballot(j < n && j >= S && k && there);
+      if (lane == 0) cnt[u * (NT / 64) + w] = uint32_t(__popcll(mh)) | uint32_t(__popcll(mr)) << 16;
+    }
+    prefix_counts<NT, kU>(cnt);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int j = j0 + u * NT + tid;
+      const bool there = x[u].key != 0, k = keep >> u & 1;
+      const bool is_hole = j < n && j < S && !k && there, is_row = j < n && j >= S && k && there;
+      const uint32_t c = cnt[u * (NT / 64) + w];
+      const int ih = holes + int(c & 0xFFFF) + lanes_before(__ballot(is_hole)), ir = rows + int(c >> 16) + lanes_before(__ballot(is_row));
+      if (is_hole && ih < a.most) hole[ih] = j;
+      if (is_row && ir < a.most) from[ir] = j;
+    }
+    const uint32_t all = cnt[kU * (NT / 64)];
+    holes += int(all & 0xFFFF);
+    rows += int(all >> 16);
+  }
+  const int pairs = min(min(holes, rows), a.most);
+  if (!here) {
+    if (tid == 0) a.count[bh] = pairs;
+    return;
+  }
+  __syncthreads();
+  for (int i = tid / lanes; i < pairs; i += NT / lanes) move_row(a, b, hk, from[i], hole[i], tid % lanes);
+}
+
+// The moves of heads that have many: `lanes` lanes of 16 bytes per row.
+__global__ __launch_bounds__(256) void evict_move(EvictArgs a, int lanes) {
+  const int bh = blockIdx.y, i = blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
+  if (i >= a.count[bh]) return;
+  const int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
+  move_row(a, bh / a.pool.Hkv, bh % a.pool.Hkv, hole[a.most + i], hole[i], threadIdx.x % lanes);
+}
+
+}  // namespace
+
+namespace {
+// Workspace of a fill: a list of kept positions, or the slices' histograms and counts and the thresholds.
+size_t fill_bytes(size_t bh, size_t n) {
+  if (n <= kFillSelect) return round256(bh * n * sizeof(int32_t));
+  const size_t slices = (n + kSlice - 1) / kSlice;
+  return round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * 2 * sizeof(int32_t)) + round256(bh * 2 * sizeof(uint32_t));
+}
+size_t moves_bytes(size_t bh, size_t n) { return round256(bh * 2 * n * sizeof(int32_t)) + round256(bh * sizeof(int32_t)); }
 }  // namespace
 
 size_t pages_evict_bytes(const d2o_pages* p, int32_t max_len) {
   const size_t bh = size_t(p->batch) * p->n_kv_heads;
-  return round256(bh * 2 * max_len * sizeof(int32_t)) + round256(bh * sizeof(int32_t));
+  return std::max(fill_bytes(bh, max_len), moves_bytes(bh, max_len));
 }
 
 }  // namespace d2o
@@ -271,27 +673,60 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
   const int most = std::min(n, budget);
   if (most > int64_t(pages->max_pages) * pages->page_size) return D2O_ERR_CAPACITY;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
-  if (workspace_bytes < pages_evict_bytes(pages, n)) return D2O_ERR_CAPACITY;
   const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads;
-  if (bh > 65535) return D2O_ERR_UNSUPPORTED;
+  if (workspace_bytes < fill_bytes(bh, n)) return D2O_ERR_CAPACITY;
+  if (bh > 65535 || n > kSlice * kMaxSlices) return D2O_ERR_UNSUPPORTED;
   a.k = to_view(K);
   a.v = to_view(V);
   a.lens = lens;
   a.scores = scores;
-  a.src = static_cast<int32_t*>(workspace);
   a.n = n;
-  a.budget = std::min(budget, n);
+  a.budget = most;
   a.recent = recent;
   a.n_sink = n_sink;
+  a.slices = (n + kSlice - 1) / kSlice;
+  char* ws = static_cast<char*>(workspace);
+  a.src = reinterpret_cast<int32_t*>(ws);
+  a.hist = reinterpret_cast<uint16_t*>(ws);
+  ws += round256(size_t(bh) * a.slices * kBins * sizeof(uint16_t));
+  a.slice = reinterpret_cast<int32_t*>(ws);
+  ws += round256(size_t(bh) * a.slices * 2 * sizeof(int32_t));
+  a.mark = reinterpret_cast<uint32_t*>(ws);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (budget < n) fill_select<<<dim3(unsigned(bh)), kSelThreads, 0, s>>>(a);
-  auto rows = [&](auto kernel, int per) { kernel<<<dim3((most + per - 1) / per, unsigned(bh)), 256, 0, s>>>(a); };
+  const dim3 heads{unsigned(bh)};
+  const bool sliced = most < n && n > kFillSelect;
+  if (sliced) {
+    fill_hist<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
+    fill_mark<<<heads, kMark, 0, s>>>(a);
+  } else if (most < n) {
+    if (n <= 2048)
+      fill_select<256, 8><<<heads, 256, 0, s>>>(a);
+    else if (n <= 8192)
+      fill_select<1024, 8><<<heads, 1024, 0, s>>>(a);
+    else
+      fill_select<1024, 16><<<heads, 1024, 0, s>>>(a);
+  }
+  auto write = [&](auto t, auto ct, auto d) {
+    typedef decltype(t) T;
+    typedef decltype(ct) CT;
+    constexpr int kD = decltype(d)::value, kRows = 256 / (kD * int(sizeof(T)) / 16);
+    if (sliced)
+      fill_slice<T, CT, kD><<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
+    else
+      fill_rows<T, CT, kD><<<dim3((most + kRows - 1) / kRows, unsigned(bh)), 256, 0, s>>>(a);
+  };
+  auto rows = [&](auto t, auto ct) {
+    if (D == 64)
+      write(t, ct, std::integral_constant<int, 64>{});
+    else
+      write(t, ct, std::integral_constant<int, 128>{});
+  };
   if (pages->cache_fp8)
-    D == 64 ? rows(fill_rows<uint16_t, uint8_t, 64>, 32) : rows(fill_rows<uint16_t, uint8_t, 128>, 16);
+    rows(uint16_t{}, uint8_t{});
   else if (pages->dtype == D2O_BF16)
-    D == 64 ? rows(fill_rows<uint16_t, uint16_t, 64>, 32) : rows(fill_rows<uint16_t, uint16_t, 128>, 16);
+    rows(uint16_t{}, uint16_t{});
   else
-    D == 64 ? rows(fill_rows<float, float, 64>, 16) : rows(fill_rows<float, float, 128>, 8);
+    rows(float{}, float{});
   return hipGetLastError() == hipSuccess ? D2O_OK : D2O_ERR_HIP;
 }
 
@@ -304,8 +739,8 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
   if (budget < 1 || recent < 0 || n_sink < 0 || int64_t(recent) + n_sink > budget) return D2O_ERR_INVALID_ARG;
   if (max_len > int64_t(pages->max_pages) * pages->page_size) return D2O_ERR_CAPACITY;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
-  if (workspace_bytes < pages_evict_bytes(pages, max_len)) return D2O_ERR_CAPACITY;
   const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads;
+  if (workspace_bytes < moves_bytes(bh, max_len)) return D2O_ERR_CAPACITY;
   if (bh > 65535) return D2O_ERR_UNSUPPORTED;
   if (max_len <= budget) return D2O_OK;  // no sequence can have more than it keeps
   a.lens = lens;
@@ -317,17 +752,19 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
   a.moves = static_cast<int32_t*>(workspace);
   a.count = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + round256(size_t(bh) * 2 * max_len * sizeof(int32_t)));
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  evict_select<<<dim3(unsigned(bh)), kSelThreads, 0, s>>>(a);
-  const int row = pages->head_dim * (pages->cache_fp8 ? 1 : pages->dtype == D2O_BF16 ? 2 : 4);
-  auto move = [&](auto kernel) {
-    const int per = 256 / (row / 16);
-    kernel<<<dim3((a.most + per - 1) / per, unsigned(bh)), 256, 0, s>>>(a);
-  };
-  switch (row) {
-    case 64: move(evict_move<64>); break;
-    case 128: move(evict_move<128>); break;
-    case 256: move(evict_move<256>); break;
-    default: move(evict_move<512>); break;
+  const int lanes = pages->head_dim * (pages->cache_fp8 ? 1 : pages->dtype == D2O_BF16 ? 2 : 4) / 16;
+  const dim3 heads{unsigned(bh)};
+  if (max_len <= 2048)
+    evict_select<256, 8><<<heads, 256, 0, s>>>(a, lanes);
+  else if (max_len <= 4096)
+    evict_select<1024, 4><<<heads, 1024, 0, s>>>(a, lanes);
+  else if (max_len <= 16384)
+    evict_select<1024, 16><<<heads, 1024, 0, s>>>(a, lanes);
+  else
+    evict_select<1024, 0><<<heads, 1024, 0, s>>>(a, lanes);
+  if (a.most > kInline) {
+    const int per = 256 / lanes;
+    evict_move<<<dim3((a.most + per - 1) / per, unsigned(bh)), 256, 0, s>>>(a, lanes);
   }
   return hipGetLastError() == hipSuccess ? D2O_OK : D2O_ERR_HIP;
 }

@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
   const int r0 = blk * BM;
   if (r0 >= n) return;
-  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, m = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, w = tid >> 6, ws = __builtin_amdgcn_readfirstlane(w), lane = tid & 63, m = lane & 31, h = lane >> 5;
   const float scale2 = kLog2e / sqrtf(float(D));
   const Tiles tl(a, r0, min(r0 + BM, n) - 1, 64);
   const int ntile = tl.count;
@@ -197,24 +197,26 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int64_t vt0 = (int64_t(b) * Hkv + hk) * a.tiles;
   const uint16_t* vtbase = a.vt + vt0 * D * 64;
   const float* rec = a.rec + vt0 * kRec;
-  // a tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB
+  // A tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB.  The tile's start is the same
+  // for all lanes, a lane's displacement in it (32 bits) changes at the prompt's end only.
+  constexpr int kRowsK = 512 / D, kLoadsK = 64 / kRowsK / NW, kLoadsV = D / 8 / NW;  // rows per instruction, instructions per wavefront
+  const uint32_t k_row = uint32_t(a.k.sn);
   auto load_k = [&](int t) __attribute__((always_inline)) {
-    constexpr int kPer = 512 / D;  // rows per instruction
-    const int k0 = tl.tile(t) * 64;
+    const int k0 = tl.tile(t) * 64, last = n - 1 - k0;
+    const uint16_t* src = kbase + int64_t(k0) * a.k.sn;
 #pragma unroll
-    for (int i = 0; i < 64 / kPer / NW; ++i) {
-      const int lr = (w * (64 / kPer / NW) + i) * kPer + lane / (D / 8);
-      const int row = (lr & 32) | perm_key(lr & 31);
+    for (int i = 0; i < kLoadsK; ++i) {
+      const int lr = (ws * kLoadsK + i) * kRowsK + lane / (D / 8), row = (lr & 32) | perm_key(lr & 31);
       const int sw = D == 128 ? swz(lane & 15, lr & 3) : swz(lane & 7, (lr >> 1) & 3);
-      load_lds16(kbase + int64_t(min(k0 + row, n - 1)) * a.k.sn + sw, Ks + (t & 1) * kElems + (w * (64 / kPer / NW) + i) * kGroupLd);
+      load_lds16(src + (uint32_t(min(row, last)) * k_row + sw), Ks + (t & 1) * kElems + (ws * kLoadsK + i) * kGroupLd);
     }
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
-    const uint16_t* src = vtbase + int64_t(tl.tile(t)) * D * 64;
+    const uint16_t* src = vtbase + int64_t(tl.tile(t)) * (D * 64);
 #pragma unroll
-    for (int i = 0; i < D / 8 / NW; ++i) {
-      const int row = (w * (D / 8 / NW) + i) * 8 + (lane >> 3);
-      load_lds16(src + row * 64 + swz(lane & 7, (row >> 1) & 3), Vs + (t & 1) * kElems + (w * (D / 8 / NW) + i) * kGroupLd);
+    for (int i = 0; i < kLoadsV; ++i) {
+      const int row = (ws * kLoadsV + i) * 8 + (lane >> 3);
+      load_lds16(src + uint32_t(row * 64 + swz(lane & 7, (row >> 1) & 3)), Vs + (t & 1) * kElems + (ws * kLoadsV + i) * kGroupLd);
     }
   };
   const int wr0 = r0 + w * 32, q_row = wr0 + m;
@@ -228,7 +230,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   load_v(0);
   if (ntile > 1) load_k(1);
   auto exps_of = [&](int t) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(rec + int64_t(tl.tile(t)) * kRec + h * 4); };
+  auto flag_of = [&](int t) __attribute__((always_inline)) { return rec[int64_t(tl.tile(t)) * kRec + 8]; };
   f32x4 ex = exps_of(0), ex_next = ex;
+  float flag = 0.f, flag_next = flag_of(0);
 
   f32x16 o[kDC];
 #pragma unroll
@@ -257,13 +261,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   auto softmax = [&](int t) __attribute__((always_inline)) {
     const int k0 = tl.tile(t) * 64;
     if (!all_seen(a, wr0, wr0 + 31, k0, k0 + 63)) {
+      // register r of sub-tile st holds key `first` + 32 st + 16 (r / 8) + r % 8
+      const int first = k0 + h * 8, last = q_row - first, gone = q_row - a.window - first, sinks = a.n_sink - first;
+      const bool ahead = k0 + 63 > wr0, behind = k0 <= wr0 + 31 - a.window;  // keys that follow a row, that its window has left
+      if (ahead) {
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = k0 + st * 32 + (r >> 3) * 16 + h * 8 + (r & 7);
-          if (!sees(a, q_row, key)) s[st][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r)
+            if (st * 32 + (r >> 3) * 16 + (r & 7) > last) s[st][r] = -INFINITY;
+      }
+      if (behind) {
+        if (k0 >= a.n_sink) {
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (st * 32 + (r >> 3) * 16 + (r & 7) <= gone) s[st][r] = -INFINITY;
+        } else {
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int key = st * 32 + (r >> 3) * 16 + (r & 7);
+              if (key <= gone && key >= sinks) s[st][r] = -INFINITY;
+            }
         }
+      }
     }
     float mx[4];
 #pragma unroll
@@ -361,39 +385,32 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   for (int ks = 0; ks < kKS; ++ks) asm volatile("" ::"v"(bq[ks]));  // the queries have arrived
   wait_vm<0>();
   __syncthreads();
-  bool now = active(0);
-  if (now) {
-    products(-1, P1{}, P2{});  // S of tile 0
-    if (!late) softmax(0);
-  }
-  __syncthreads();
-  for (int t = 0; t < ntile; ++t) {
+  bool now = false;
+  for (int t = -1; t < ntile; ++t) {
     const bool more = t + 1 < ntile, next = more && active(t + 1);
-    if (t + 2 < ntile) load_k(t + 2);
-    if (more) {
-      load_v(t + 1);
-      ex_next = exps_of(t + 1);
+    if (t >= 0) {  // K(t) and V(t - 1) were last read before this iteration: their buffers take K(t + 2) and V(t + 1)
+      if (t + 2 < ntile) load_k(t + 2);
+      if (more) {
+        load_v(t + 1);
+        ex_next = exps_of(t + 1);
+        flag_next = flag_of(t + 1);
+      }
     }
-    if (late) {
-      if (now) softmax(t);
-      matrix(t, now, next);
-    } else {
-      matrix(t, now, next);
-    }
+    if (late && now) softmax(t);
+    matrix(t, now, next);
     ex = ex_next;
     if (!late && next) softmax(t + 1);
     now = next;
     wait_vm<0>();  // this wavefront's part of the next tiles is in LDS
+    flag = fmaxf(flag, flag_next);
     __syncthreads();
   }
-  // infinities and NaN of V, which counted as zero above: a row that sees one takes it as it is, whatever its weight
-  for (int t0 = 0; t0 < ntile; t0 += 64) {
-    const int t = t0 + lane;
-    uint64_t flagged = __ballot(t < ntile && rec[int64_t(tl.tile(min(t, ntile - 1))) * kRec + 8] != 0.f);
-    while (flagged) {
-      const int k0 = tl.tile(t0 + __builtin_ctzll(flagged)) * 64;
-      flagged &= flagged - 1;
-      const uint16_t* vsrc = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
+  if (flag != 0.f) {
+    // infinities and NaN of V, which counted as zero above: a row that sees one takes it as it is, whatever its weight
+    const uint16_t* vsrc = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
+    for (int t = 0; t < ntile; ++t) {
+      if (flag_of(t) == 0.f) continue;
+      const int k0 = tl.tile(t) * 64;
       for (int j = k0; j < min(k0 + 64, n); ++j) {
         if (!sees(a, q_row, j)) continue;
         const uint16_t* row = vsrc + int64_t(j) * a.v.sn;
@@ -604,6 +621,7 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
   if (workspace_bytes < window_bytes(batch, n, n_kv_heads, head_dim, dtype)) return D2O_ERR_CAPACITY;
   if (int64_t(batch) * n_q_heads * ((n + 63) / 64) > 0x7FFFFFFF) return D2O_ERR_UNSUPPORTED;
+  if (K.stride_n >= 1 << 24) return D2O_ERR_UNSUPPORTED;  // (displacements inside a tile of 64 keys have 32 bits)
   WindowArgs a{};
   a.q = to_view(Q);
   a.k = to_view(K);
