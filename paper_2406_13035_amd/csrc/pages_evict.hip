@@ -132,15 +132,24 @@ struct FillArgs {
   View k, v;
   const int32_t* lens;
   const float* scores;
-  int32_t* src;    // [B][Hkv][budget] kept positions, rising (prompts of at most kFillSelect tokens of which some are evicted)
+  int32_t* src;    // [B][Hkv][budget] kept positions, rising (where some are evicted)
   uint16_t* hist;  // longer prompts: [B][Hkv][slices][kBins] of a slice's keys
   int32_t* slice;  // [B][Hkv][slices][2] kept entries before a slice: above the threshold, equal to it
   uint32_t* mark;  // [B][Hkv][2] threshold, how many equal to it are kept
   int32_t n, budget, recent, n_sink, slices;
 
   __device__ __forceinline__ int length(int b) const { return lens ? min(max(lens[b], 0), n) : n; }
-  __device__ __forceinline__ uint32_t key(const float* sc, int j, int late) const {
-    return j < n_sink || j >= late ? kProtected : score_key(sc[j]);
+  // keys of tokens j0, j0 + step, ..: all loads on their way before the first is used (tokens behind the last: key 0)
+  template <int N>
+  __device__ __forceinline__ void keys(const float* sc, int len, int j0, int step, uint32_t* key) const {
+    float x[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) x[u] = sc[min(j0 + u * step, len - 1)];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int j = j0 + u * step;
+      key[u] = j >= len ? 0 : j < n_sink || j >= len - recent ? kProtected : score_key(x[u]);
+    }
   }
 };
 constexpr int kFillSelect = 16384;  // tokens of a prompt that one workgroup holds in registers
@@ -155,11 +164,7 @@ __global__ __launch_bounds__(NT) void fill_select(FillArgs a) {
   if (n <= a.budget) return;
   const float* sc = a.scores + int64_t(bh) * a.n;
   uint32_t key[PT];
-#pragma unroll
-  for (int u = 0; u < PT; ++u) {
-    const int j = u * NT + tid;
-    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
-  }
+  a.keys<PT>(sc, n, tid, NT, key);
   int equal, same;
   const uint32_t t = nth_largest<NT>(sh, a.budget, equal, same, [&](auto f) {
 #pragma unroll
@@ -191,11 +196,7 @@ __global__ __launch_bounds__(kSliceThreads) void fill_hist(FillArgs a) {
   if (n <= a.budget || j0 >= n) return;
   const float* sc = a.scores + int64_t(bh) * a.n;
   uint32_t key[kSlicePer];
-#pragma unroll
-  for (int u = 0; u < kSlicePer; ++u) {
-    const int j = j0 + u * kSliceThreads + tid;
-    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
-  }
+  a.keys<kSlicePer>(sc, n, j0 + tid, kSliceThreads, key);
   for (int i = tid; i < kBins; i += kSliceThreads) hist[i] = 0;
   __syncthreads();
 #pragma unroll
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
   __shared__ int gt[kMaxSlices], eq[kMaxSlices];
   __shared__ int ncand;
   const int bh = blockIdx.x, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63;
-  const int n = a.length(b), late = n - a.recent;
+  const int n = a.length(b);
   if (n <= a.budget) return;
   const int slices = (n + kSlice - 1) / kSlice;
   const float* sc = a.scores + int64_t(bh) * a.n;
@@ -241,11 +242,7 @@ __global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
   for (int j0 = 0; j0 < n; j0 += kBatch * kMark) {
     uint32_t k[kBatch];
     int in_all = 0;
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int j = j0 + u * kMark + tid;
-      k[u] = j < n ? a.key(sc, j, late) : 0;
-    }
+    a.keys<kBatch>(sc, n, j0 + tid, kMark, k);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int j = j0 + u * kMark + tid;
@@ -272,7 +269,8 @@ __global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
       for (int i = tid; i < total; i += kMark) f(cand[i] & 0x1FFFFF, cand[i] >> 21);
     } else {
       for (int j = tid; j < n; j += kMark) {
-        const uint32_t k = a.key(sc, j, late);
+        uint32_t k;
+        a.keys<1>(sc, n, j, 0, &k);
         if (k >> 21 == top) f(k & 0x1FFFFF, uint32_t(j) / kSlice);
       }
     }
@@ -306,6 +304,37 @@ __global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
       a.mark[bh * 2] = top << 21 | low;
       a.mark[bh * 2 + 1] = equal;
     }
+  }
+}
+
+// ... and the slices' kept positions, in order behind those of the slices before.  (Their rows are copied by a launch of their own: the
+// slice with the recent tokens has more than all others.)
+__global__ __launch_bounds__(kSliceThreads) void fill_list(FillArgs a) {
+  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = a.length(b), j0 = blockIdx.x * kSlice;
+  if (n <= a.budget || j0 >= n) return;
+  const float* sc = a.scores + int64_t(bh) * a.n;
+  const uint32_t t = a.mark[bh * 2];
+  const int equal = a.mark[bh * 2 + 1];
+  const int32_t* before = a.slice + (int64_t(bh) * a.slices + blockIdx.x) * 2;
+  const int gt0 = before[0], eq0 = before[1];
+  uint32_t key[kSlicePer];
+  a.keys<kSlicePer>(sc, n, j0 + tid, kSliceThreads, key);
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const uint32_t v = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
+    if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = v;
+  }
+  prefix_counts<kSliceThreads, kSlicePer>(cnt);
+  const int quota = max(0, equal - eq0);  // of the equal ones of this slice
+  int32_t* src = a.src + int64_t(bh) * a.budget + gt0 + min(eq0, equal);
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const uint32_t v = cnt[u * (kSliceThreads / 64) + w];
+    const bool gt = key[u] > t, eq = key[u] == t;
+    const int above = int(v & 0xFFFF) + lanes_before(__ballot(gt)), rank = int(v >> 16) + lanes_before(__ballot(eq));
+    if (gt || (eq && rank < quota)) src[above + min(rank, quota)] = j0 + u * kSliceThreads + tid;
   }
 }
 
@@ -360,50 +389,6 @@ __global__ __launch_bounds__(256) void fill_rows(FillArgs a) {
   put_row<T, CT, D>(a, bh, b, hk, s, n <= a.budget ? s : a.src[int64_t(bh) * a.budget + s], threadIdx.x % kLanes);
 }
 
-// ... and the slices' kept rows, in order behind those of the slices before.
-template <typename T, typename CT, int D>
-__global__ __launch_bounds__(kSliceThreads) void fill_slice(FillArgs a) {
-  constexpr int kLanes = D * int(sizeof(T)) / 16, kRows = kSliceThreads / kLanes;
-  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
-  __shared__ uint16_t list[kSlice];
-  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int n = a.length(b), j0 = blockIdx.x * kSlice, c = tid % kLanes;
-  if (j0 >= n) return;
-  if (n <= a.budget) {
-    for (int j = j0 + tid / kLanes; j < min(j0 + kSlice, n); j += kRows) put_row<T, CT, D>(a, bh, b, hk, j, j, c);
-    return;
-  }
-  const float* sc = a.scores + int64_t(bh) * a.n;
-  const uint32_t t = a.mark[bh * 2];
-  const int equal = a.mark[bh * 2 + 1];
-  const int32_t* before = a.slice + (int64_t(bh) * a.slices + blockIdx.x) * 2;
-  const int gt0 = before[0], eq0 = before[1];
-  uint32_t key[kSlicePer];
-#pragma unroll
-  for (int u = 0; u < kSlicePer; ++u) {
-    const int j = j0 + u * kSliceThreads + tid;
-    key[u] = j < n ? a.key(sc, j, n - a.recent) : 0;
-  }
-#pragma unroll
-  for (int u = 0; u < kSlicePer; ++u) {
-    const uint32_t v = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
-    if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = v;
-  }
-  prefix_counts<kSliceThreads, kSlicePer>(cnt);
-  const int quota = max(0, equal - eq0);  // of the equal ones of this slice
-#pragma unroll
-  for (int u = 0; u < kSlicePer; ++u) {
-    const uint32_t v = cnt[u * (kSliceThreads / 64) + w];
-    const bool gt = key[u] > t, eq = key[u] == t;
-    const int above = int(v & 0xFFFF) + lanes_before(__ballot(gt)), rank = int(v >> 16) + lanes_before(__ballot(eq));
-    if (gt || (eq && rank < quota)) list[above + min(rank, quota)] = uint16_t(u * kSliceThreads + tid);
-  }
-  const uint32_t all = cnt[kSlicePer * (kSliceThreads / 64)];
-  const int kept = int(all & 0xFFFF) + min(int(all >> 16), quota), s0 = gt0 + min(eq0, equal);
-  __syncthreads();
-  for (int i = tid / kLanes; i < kept; i += kRows) put_row<T, CT, D>(a, bh, b, hk, s0 + i, j0 + list[i], c);
-}
-
 struct EvictArgs {
   PagePool pool;
   const int32_t* lens;
@@ -413,21 +398,47 @@ struct EvictArgs {
 };
 constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself
 
-// A kept row into a hole: sources lie at or behind the budget, targets below it, so that moves never meet.
-__device__ __forceinline__ void move_row(const EvictArgs& a, int b, int hk, int from, int to, int c) {
-  const int pt = a.pool.page_of(b, to), pf = a.pool.page_of(b, from);
-  if (pt < 0 || pf < 0) return;
-  const u32x4 k = reinterpret_cast<const u32x4*>(a.pool.k_at(pf, hk, from))[c];
-  const u32x4 v = reinterpret_cast<const u32x4*>(a.pool.v_at(pf, hk, from))[c];
-  reinterpret_cast<u32x4*>(a.pool.k_at(pt, hk, to))[c] = k;
-  reinterpret_cast<u32x4*>(a.pool.v_at(pt, hk, to))[c] = v;
-  if (c == 0) {
-    const int64_t t = a.pool.at(pt, hk, to), f = a.pool.at(pf, hk, from);
-    a.pool.score[t] = a.pool.score[f];
-    a.pool.pos[t] = a.pool.pos[f];
-    if (a.pool.k_exp) {
-      a.pool.k_exp[t] = a.pool.k_exp[f];
-      a.pool.v_exp[t] = a.pool.v_exp[f];
+// Kept rows into holes, `lanes` lanes of 16 bytes per row: pairs i0, i0 + step, .. below `pairs`, a few at a time on their way.  Sources lie
+// at or behind the budget, targets below it: moves never meet.
+template <int N>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int hk, const int32_t* from, const int32_t* hole, int i0, int step,
+                                          int pairs, int c) {
+  for (int i = i0; i < pairs; i += N * step) {
+    u32x4 k[N], v[N];
+    float score[N];
+    int32_t pos[N], to[N], pt[N];
+    int8_t ke[N], ve[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const bool is = i + u * step < pairs;
+      const int src = is ? from[i + u * step] : 0;
+      to[u] = is ? hole[i + u * step] : 0;
+      pt[u] = is ? a.pool.page_of(b, to[u]) : -1;
+      const int pf = is ? a.pool.page_of(b, src) : -1;
+      if (pf < 0) pt[u] = -1;
+      const int page = max(pf, 0);
+      const int64_t at = a.pool.at(page, hk, src);
+      k[u] = reinterpret_cast<const u32x4*>(a.pool.k_at(page, hk, src))[c];
+      v[u] = reinterpret_cast<const u32x4*>(a.pool.v_at(page, hk, src))[c];
+      score[u] = a.pool.score[at];
+      pos[u] = a.pool.pos[at];
+      ke[u] = a.pool.k_exp ? a.pool.k_exp[at] : 0;
+      ve[u] = a.pool.k_exp ? a.pool.v_exp[at] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      if (pt[u] < 0) continue;
+      reinterpret_cast<u32x4*>(a.pool.k_at(pt[u], hk, to[u]))[c] = k[u];
+      reinterpret_cast<u32x4*>(a.pool.v_at(pt[u], hk, to[u]))[c] = v[u];
+      if (c == 0) {
+        const int64_t at = a.pool.at(pt[u], hk, to[u]);
+        a.pool.score[at] = score[u];
+        a.pool.pos[at] = pos[u];
+        if (a.pool.k_exp) {
+          a.pool.k_exp[at] = ke[u];
+          a.pool.v_exp[at] = ve[u];
+        }
+      }
     }
   }
 }
@@ -467,24 +478,32 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   int32_t pos[kKeep];
   uint32_t present = 0;  // bit u
   int newest = -INT32_MAX;
+  // score and position of entry j, false where it has no page or is none (then of the pool's first row)
   auto look = [&](int j, float& sc, int32_t& p) __attribute__((always_inline)) {
-    const int page = j < n ? a.pool.page_of(b, j) : -1;
-    sc = 0.f;
-    p = 0;
-    if (page < 0) return false;
-    const int64_t at = a.pool.at(page, hk, j);
+    const int page = a.pool.page_of(b, min(j, n - 1));
+    const bool there = j < n && page >= 0;
+    const int64_t at = there ? a.pool.at(page, hk, j) : 0;
     sc = a.pool.score[at];
     p = a.pool.pos[at];
-    return true;
+    return there;
   };
   if constexpr (PT > 0) {
+    int page[kKeep];
 #pragma unroll
-    for (int u = 0; u < PT; ++u)
-      if (look(u * NT + tid, score[u], pos[u])) present |= 1u << u;
+    for (int u = 0; u < PT; ++u) page[u] = a.pool.page_of(b, min(u * NT + tid, n - 1));
+#pragma unroll
+    for (int u = 0; u < PT; ++u) {
+      const bool there = u * NT + tid < n && page[u] >= 0;
+      const int64_t at = there ? a.pool.at(page[u], hk, u * NT + tid) : 0;
+      score[u] = a.pool.score[at];
+      pos[u] = a.pool.pos[at];
+      present |= uint32_t(there) << u;
+    }
 #pragma unroll
     for (int u = 0; u < PT; ++u)
       if (present >> u & 1) newest = max(newest, pos[u]);
   } else {
+#pragma unroll 4
     for (int j = tid; j < n; j += NT) {
       float sc;
       int32_t p;
@@ -512,6 +531,7 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
       for (int u = 0; u < PT; ++u)
         if (u * NT + tid < n) f(u * NT + tid, r[u]);
     } else {
+#pragma unroll 4
       for (int j = tid; j < n; j += NT) f(j, rank_at(j));
     }
   };
@@ -541,7 +561,7 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
         a.count[bh] = at < S ? 1 : 0;
       }
     } else if (at < S && tid < lanes) {
-      move_row(a, b, hk, S, at, tid);  // (no move if either has no page)
+      move_rows<1>(a, b, hk, &S, &at, 0, 1, 1, tid);  // (no move if either has no page)
     }
     return;
   }
@@ -628,25 +648,22 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
     return;
   }
   __syncthreads();
-  for (int i = tid / lanes; i < pairs; i += NT / lanes) move_row(a, b, hk, from[i], hole[i], tid % lanes);
+  move_rows<4>(a, b, hk, from, hole, tid / lanes, NT / lanes, pairs, tid % lanes);
 }
 
 // The moves of heads that have many: `lanes` lanes of 16 bytes per row.
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int lanes) {
-  const int bh = blockIdx.y, i = blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
-  if (i >= a.count[bh]) return;
+  const int bh = blockIdx.y, per = 256 / lanes;
   const int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
-  move_row(a, bh / a.pool.Hkv, bh % a.pool.Hkv, hole[a.most + i], hole[i], threadIdx.x % lanes);
+  move_rows<1>(a, bh / a.pool.Hkv, bh % a.pool.Hkv, hole + a.most, hole, blockIdx.x * per + threadIdx.x / lanes, gridDim.x * per,
+               a.count[bh], threadIdx.x % lanes);
 }
 
-}  // namespace
-
-namespace {
-// Workspace of a fill: a list of kept positions, or the slices' histograms and counts and the thresholds.
+// Workspace of a fill: a list of kept positions; of a long prompt also the slices' histograms and counts and the thresholds.
 size_t fill_bytes(size_t bh, size_t n) {
-  if (n <= kFillSelect) return round256(bh * n * sizeof(int32_t));
-  const size_t slices = (n + kSlice - 1) / kSlice;
-  return round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * 2 * sizeof(int32_t)) + round256(bh * 2 * sizeof(uint32_t));
+  const size_t list = round256(bh * n * sizeof(int32_t)), slices = (n + kSlice - 1) / kSlice;
+  if (n <= kFillSelect) return list;
+  return list + round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * 2 * sizeof(int32_t)) + round256(bh * 2 * sizeof(uint32_t));
 }
 size_t moves_bytes(size_t bh, size_t n) { return round256(bh * 2 * n * sizeof(int32_t)) + round256(bh * sizeof(int32_t)); }
 }  // namespace
@@ -687,6 +704,7 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
   a.slices = (n + kSlice - 1) / kSlice;
   char* ws = static_cast<char*>(workspace);
   a.src = reinterpret_cast<int32_t*>(ws);
+  ws += round256(size_t(bh) * n * sizeof(int32_t));
   a.hist = reinterpret_cast<uint16_t*>(ws);
   ws += round256(size_t(bh) * a.slices * kBins * sizeof(uint16_t));
   a.slice = reinterpret_cast<int32_t*>(ws);
@@ -694,10 +712,10 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
   a.mark = reinterpret_cast<uint32_t*>(ws);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 heads{unsigned(bh)};
-  const bool sliced = most < n && n > kFillSelect;
-  if (sliced) {
+  if (most < n && n > kFillSelect) {
     fill_hist<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
     fill_mark<<<heads, kMark, 0, s>>>(a);
+    fill_list<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
   } else if (most < n) {
     if (n <= 2048)
       fill_select<256, 8><<<heads, 256, 0, s>>>(a);
@@ -710,10 +728,7 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
     typedef decltype(t) T;
     typedef decltype(ct) CT;
     constexpr int kD = decltype(d)::value, kRows = 256 / (kD * int(sizeof(T)) / 16);
-    if (sliced)
-      fill_slice<T, CT, kD><<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
-    else
-      fill_rows<T, CT, kD><<<dim3((most + kRows - 1) / kRows, unsigned(bh)), 256, 0, s>>>(a);
+    fill_rows<T, CT, kD><<<dim3((most + kRows - 1) / kRows, unsigned(bh)), 256, 0, s>>>(a);
   };
   auto rows = [&](auto t, auto ct) {
     if (D == 64)
