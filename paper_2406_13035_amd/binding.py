@@ -421,39 +421,30 @@ def _ok(rc, what):
         raise D2OError(f"{what} failed with {rc} ({_STATUS.get(rc, 'unknown')})")
 
 
-def _view_of(t: torch.Tensor, batch_dim=0, head_dim_=1, row_dim=2) -> d2o_view:
+def _view_of(t: torch.Tensor, rows=True) -> d2o_view:
     # (a dimension of size one may have any stride: it takes no part)
     s, n = t.stride(), t.shape
-    return d2o_view(t.data_ptr(), s[batch_dim] if n[batch_dim] > 1 else 0, s[head_dim_] if n[head_dim_] > 1 else 0,
-                    s[row_dim] if row_dim is not None and n[row_dim] > 1 else 0)
+    return d2o_view(t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if rows and n[2] > 1 else 0)
 
 
-def _tensor_ok(t, shape, dtype, device, what):
-    _need(isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape)
-          and (t.numel() == 0 or t.stride(-1) == 1 or t.shape[-1] == 1),
-          f"{what}: a tensor of shape {tuple(shape)} and type {dtype} on {device}, with its last dimension contiguous, "
-          "is needed")
+def _tensor_ok(t, shape, dtype, device, what, whole=False):
+    """`t` has this shape, type and device, and its last dimension (`whole`: all of it) is contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device
+            and (t.is_contiguous() if whole else t.stride(-1) == 1)):
+        raise D2OError(f"{what}: a tensor of shape {tuple(shape)} and type {dtype} on {device}, "
+                       f"{'contiguous' if whole else 'with its last dimension contiguous'}, is needed")
 
 
 def _vector_ok(t, shape, dtype, device, what):
-    _tensor_ok(t, shape, dtype, device, what)
-    _need(t.is_contiguous(), f"{what} must be contiguous")
+    _tensor_ok(t, shape, dtype, device, what, whole=True)
 
 
-class _on:
-    """Makes `device` the current one for a call (nothing to do in the usual case that it is)."""
-
-    def __init__(self, device):
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return int(torch.cuda.current_stream().cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _enqueue(device, call):
+    """call(stream) with `device` current, which it nearly always is already."""
+    if torch.cuda.current_device() == device.index:
+        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return call(torch.cuda.current_stream().cuda_stream)
 
 
 def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=None):
@@ -470,17 +461,19 @@ def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=No
     _tensor_ok(V, (B, Hkv, n, d), dt, dev, "V")
     if lens is not None:
         _vector_ok(lens, (B,), torch.int32, dev, "lens")
-    need = C.c_size_t()
-    _ok(lib.d2o_window_workspace_bytes(B, n, Hkv, d, _DTYPE_CODES[dt], C.byref(need)), "d2o_window_workspace_bytes")
-    with _on(dev) as stream:
-        if O is None:
-            O = torch.empty(Q.shape, dtype=dt, device=dev) if lens is None else torch.zeros(Q.shape, dtype=dt, device=dev)
-        else:
-            _tensor_ok(O, Q.shape, dt, dev, "O")
+    if O is None:
+        O = torch.empty(Q.shape, dtype=dt, device=dev) if lens is None else torch.zeros(Q.shape, dtype=dt, device=dev)
+    else:
+        _tensor_ok(O, Q.shape, dt, dev, "O")
+    code, need = _DTYPE_CODES[dt], C.c_size_t()
+    _ok(lib.d2o_window_workspace_bytes(B, n, Hkv, d, code, C.byref(need)), "d2o_window_workspace_bytes")
+
+    def call(stream):
         ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        _ok(lib.d2o_window_attend(B, n, Hq, Hkv, d, _DTYPE_CODES[dt], _view_of(Q), _view_of(K), _view_of(V),
-                                  lens.data_ptr() if lens is not None else None, window, n_sink, _view_of(O),
-                                  ws.data_ptr(), need.value, stream), "d2o_window_attend")
+        return lib.d2o_window_attend(B, n, Hq, Hkv, d, code, _view_of(Q), _view_of(K), _view_of(V),
+                                     lens.data_ptr() if lens is not None else None, window, n_sink, _view_of(O),
+                                     ws.data_ptr(), need.value, stream)
+    _ok(_enqueue(dev, call), "d2o_window_attend")
     return O
 
 
@@ -519,9 +512,10 @@ class Pages:
         self.desc = d2o_pages(B, n_q_heads, Hkv, d, _DTYPE_CODES[self.dtype], 1 if fp8 else 0, page_size, n_pages,
                               max_pages, _view_of(K), _view_of(V), ptr(K_exp), ptr(V_exp), ptr(score), ptr(pos),
                               page_table.data_ptr())
-        self.capacity = max_pages * page_size
+        self._ref = C.byref(self.desc)
+        self._bound = min(self.max_len, max_pages * page_size)  # of every sequence's entries
         need = C.c_size_t()
-        _ok(self.lib.d2o_pages_workspace_bytes(C.byref(self.desc), self.max_len, C.byref(need)),
+        _ok(self.lib.d2o_pages_workspace_bytes(self._ref, self.max_len, C.byref(need)),
             "d2o_pages_workspace_bytes")
         self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
         self._ws = (self.workspace.data_ptr(), need.value)
@@ -539,11 +533,9 @@ class Pages:
         _tensor_ok(V, shape, self.dtype, self.device, "V")
         if score is not None:
             _vector_ok(score, shape[:3], torch.float32, self.device, "score")
-        with _on(self.device) as stream:
-            _ok(self.lib.d2o_pages_fill(C.byref(self.desc), _view_of(K), _view_of(V), n,
-                                        None if lens is None else self._lens(lens),
-                                        None if score is None else score.data_ptr(), budget, recent, n_sink, *self._ws,
-                                        stream), "d2o_pages_fill")
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_fill(
+            self._ref, _view_of(K), _view_of(V), n, None if lens is None else self._lens(lens),
+            None if score is None else score.data_ptr(), budget, recent, n_sink, *self._ws, stream)), "d2o_pages_fill")
 
     def d2o_pages_step(self, q, k_new, v_new, lens, out, positions=None, window=0, n_sink=0):
         """One new token per sequence: q, out [B, Hq, d]; k_new, v_new [B, Hkv, d], or None: attention only; lens int32
@@ -556,18 +548,16 @@ class Pages:
         if k_new is not None:
             _tensor_ok(k_new, new, self.dtype, self.device, "k_new")
             _tensor_ok(v_new, new, self.dtype, self.device, "v_new")
-        with _on(self.device) as stream:
-            _ok(self.lib.d2o_pages_step(C.byref(self.desc), _view_of(q, row_dim=None),
-                                        _NULL_VIEW if k_new is None else _view_of(k_new, row_dim=None),
-                                        _NULL_VIEW if v_new is None else _view_of(v_new, row_dim=None), self._lens(lens),
-                                        None if positions is None else self._lens(positions, "positions"),
-                                        min(self.max_len, self.capacity), window, n_sink, _view_of(out, row_dim=None), *self._ws, stream), "d2o_pages_step")
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_step(
+            self._ref, _view_of(q, False), _NULL_VIEW if k_new is None else _view_of(k_new, False),
+            _NULL_VIEW if v_new is None else _view_of(v_new, False), self._lens(lens),
+            None if positions is None else self._lens(positions, "positions"), self._bound, window, n_sink,
+            _view_of(out, False), *self._ws, stream)), "d2o_pages_step")
 
     def d2o_pages_evict(self, lens, budget, recent=0, n_sink=0):
         """Every head of a sequence with more than `budget` entries goes back to that many, in place."""
-        with _on(self.device) as stream:
-            _ok(self.lib.d2o_pages_evict(C.byref(self.desc), self._lens(lens), min(self.max_len, self.capacity), budget,
-                                         recent, n_sink, *self._ws, stream), "d2o_pages_evict")
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_evict(
+            self._ref, self._lens(lens), self._bound, budget, recent, n_sink, *self._ws, stream)), "d2o_pages_evict")
 
 
 KERNEL_IDS = {"attn_fwd": 0, "colsum": 1, "select": 2, "match_filter": 3, "match_refine": 4,

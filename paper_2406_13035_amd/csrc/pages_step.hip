@@ -67,7 +67,7 @@ struct StepArgs {
   float* logits;   // [B][Hq][pad] base-2 logits of the entries that are seen (scores kept)
   float* part_o;   // [B * Hkv][splits][G][D] outputs of a share, not normalised
   float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum
-  int32_t Hq, G, max_len, window, n_sink, pad, splits;
+  int32_t Hq, G, max_len, window, n_sink, pad, splits, joins;  // joins: workgroups of step_finish that join outputs
 };
 
 // The tiles of a sequence that hold what a step sees: those of the first tokens, then those from the window's start.  (Where the
@@ -96,7 +96,7 @@ struct TileList {
       rest0 = all - 1;
       tiles = 1;
     }
-    share = max((tiles + a.splits - 1) / a.splits, least);
+    share = ((tiles + a.splits - 1) / a.splits + least - 1) / least * least;  // whole rounds of the wavefronts
   }
   __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
   __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }
@@ -256,6 +256,38 @@ __device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int 
   }
 }
 
+// Adds the softmax rows of a (sequence, KV head) to the scores of entries i0, i0 + step, .. (in the order of the tiles) below `end`, N of them,
+// all loads on their way at once (Eq. 6); the group's query heads in rising order.  M and inv: maximum and reciprocal sum of each.
+template <int N>
+__device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& list, int b, int hk, int i0, int step, int end,
+                                           const float* M, const float* inv) {
+  const float* lg = a.logits + (int64_t(b) * a.Hq + hk * a.G) * a.pad;
+  int s[N], page[N];
+  float add[N], old[N];
+  int64_t at[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int i = i0 + u * step;
+    s[u] = i < end ? list.slot(i / kTile) + i % kTile : list.n;
+    page[u] = s[u] < list.n ? a.pool.page_of(b, s[u]) : -1;
+    add[u] = 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    at[u] = page[u] >= 0 ? a.pool.at(page[u], hk, s[u]) : 0;
+    old[u] = a.pool.score[at[u]];
+  }
+  for (int h = 0; h < a.G; ++h) {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      add[u] += __builtin_amdgcn_exp2f(lg[int64_t(h) * a.pad + min(s[u], list.n - 1)] - M[h]) * inv[h];
+  }
+  // (an entry that is not seen has logits of -infinity and gets nothing; NaN is added)
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (page[u] >= 0 && add[u] != 0.f) a.pool.score[at[u]] = old[u] + add[u];
+}
+
 // One workgroup per (sequence, KV head, share of its tiles).  U tiles of 16 entries per wavefront and round: the logits of all
 // query heads of the group come from the matrix core (heads are its columns, padded to 16), straight from rows in registers: lane l
 // holds 16 bytes of row l % 16 at a time, and the order of the products' terms is free.  A lane of the result has head
@@ -263,14 +295,18 @@ __device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int 
 // softmax of its own over the entries it meets, with nothing exchanged in the loop; a probability reaches the lanes of
 // its row by a register broadcast.  P V runs on the vector ALU in fp32 (a rounding of P would cost more bits than the products
 // save: the loads bound the kernel up to 16 heads per group).
-template <typename T, typename CT, int D, int GM, int U>
+// WIDE: a tile lies in one page, whose number and address are the same for all lanes and live in scalar registers; a lane adds a
+// displacement of 32 bits that never changes.  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
+// addresses as with sums: 8-bit rows 71 us where they take 30.)
+template <typename T, typename CT, int D, int GM, int U, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
   typedef Rows<CT, D> R;
   constexpr int E = R::kE;
   __shared__ float so[kWaves][GM][D];
   __shared__ float sml[kWaves][GM][2];
+  __shared__ float sM[GM], sinv[GM];
   const int Hkv = a.pool.Hkv, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv;
-  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   const TileList list(a, b, kWaves * U);
   const int t0 = blockIdx.x * list.share, t1 = min(t0 + list.share, list.tiles);
   if (list.n == 0) {
@@ -292,59 +328,97 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
   const float scale2 = kLog2e / sqrtf(float(D));
   const bool ordered = a.window != 0 && !a.pool.pos, by_pos = a.window != 0 && a.pool.pos;
   const int64_t lo64 = a.window == 0 ? INT64_MIN : list.last - a.window + 1;  // first position of the window
+  const int lo = int(min(max(lo64, int64_t(0)), int64_t(n)));                 // (entries in order of position)
   float m = -3.402823466e38f, l = 0.f, acc[GM][E] = {};
   float* lg = a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
-  const bool big_pages = a.pool.shift >= 4;
+  // (the page table: what an earlier launch or copy wrote, read through the scalar cache)
+  const auto table = (const __attribute__((address_space(4))) int32_t*)(a.pool.table + int64_t(b) * a.pool.max_pages);
+  const int rmask = (1 << a.pool.shift) - 1;
+  const uint32_t koff = uint32_t(c) * uint32_t(a.pool.k_row) + g * 16, voff = uint32_t(4 * g) * uint32_t(a.pool.v_row);
   for (int t = t0 + w * U; t < t1; t += kWaves * U) {
     u32x4 k[U][R::kK];
     typename R::VReg v[U][4];
     float ke[U], ve[U][4];
     uint32_t seen[U];  // bit i: entry i of the tile is seen
+    if constexpr (WIDE) {
+      int page[U], s0[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s0 = t + u < t1 ? list.slot(t + u) : n;  // (a tile behind the share: no entry)
-      const int s = s0 + c;
-      int pk = -1, pv[4];
-      if (big_pages) {  // a tile lies in one page
-        if (s0 < n) pk = a.pool.page_of(b, s0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) pv[r] = pk;
-      } else {
-        if (s < n) pk = a.pool.page_of(b, s);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) pv[r] = __shfl(pk, 4 * g + r, 64);
+      for (int u = 0; u < U; ++u) {
+        s0[u] = list.slot(min(t + u, t1 - 1));
+        page[u] = table[s0[u] >> a.pool.shift];
       }
-      bool ok = s < n && pk >= 0;
-      if (ordered) ok = ok && (s >= lo64 || s < a.n_sink);
-      if (by_pos && ok) {
-        const int p = a.pool.pos[a.pool.at(pk, hk, s)];
-        ok = p >= lo64 || p < a.n_sink;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool there = uint32_t(page[u]) < uint32_t(a.pool.n_pages);
+        const int p = there ? page[u] : 0;  // (no page: the pool's first, whose values are not used; rows behind the end lie in the page)
+        const int64_t at = ((int64_t(p) * Hkv + hk) << a.pool.shift) + (s0[u] & rmask);
+        const uint8_t* kp = a.pool.K + p * a.pool.k_page + hk * a.pool.k_head + (s0[u] & rmask) * a.pool.k_row;
+        const uint8_t* vp = a.pool.V + p * a.pool.v_page + hk * a.pool.v_head + (s0[u] & rmask) * a.pool.v_row;
+#pragma unroll
+        for (int i = 0; i < R::kK; ++i) k[u][i] = *reinterpret_cast<const u32x4*>(kp + (koff + i * 64));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[u][r] = R::load_v(vp + r * a.pool.v_row + voff, c);
+        if constexpr (sizeof(CT) == 1) {
+          ke[u] = pow2_f32((a.pool.k_exp + at)[uint32_t(c)]);
+          const uint32_t four = *reinterpret_cast<const uint32_t*>(a.pool.v_exp + at + uint32_t(4 * g));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) ve[u][r] = pow2_f32(int8_t(four >> (8 * r)));
+        }
+        seen[u] = 0;
+        if (there && t + u < t1) {
+          if (s0[u] + kTile <= n && !by_pos && (!ordered || s0[u] >= lo || s0[u] + kTile <= a.n_sink)) {
+            seen[u] = 0xFFFFu;
+          } else {
+            const int s = s0[u] + c;
+            bool ok = s < n;
+            if (ordered) ok = ok && (s >= lo || s < a.n_sink);
+            if (by_pos) {
+              const int ps = (a.pool.pos + at)[uint32_t(c)];
+              ok = ok && (ps >= lo64 || ps < a.n_sink);
+            }
+            seen[u] = uint32_t(__ballot(ok)) & 0xFFFFu;
+          }
+        }
       }
-      seen[u] = uint32_t(__ballot(ok)) & 0xFFFFu;
-      // (rows that are not seen: the first row of the pool instead, whose values are not used)
-      const uint8_t* kr = ok ? a.pool.k_at(pk, hk, s) : a.pool.K;
+    } else {
 #pragma unroll
-      for (int i = 0; i < R::kK; ++i) k[u][i] = reinterpret_cast<const u32x4*>(kr)[i * 4 + g];
-      if constexpr (sizeof(CT) == 1) ke[u] = ok ? pow2_f32(a.pool.k_exp[a.pool.at(pk, hk, s)]) : 1.f;
+      for (int u = 0; u < U; ++u) {
+        const int s0 = t + u < t1 ? list.slot(t + u) : n;  // (a tile behind the share: no entry)
+        const int s = s0 + c;
+        const int pk = s < n ? a.pool.page_of(b, s) : -1;
+        bool ok = s < n && pk >= 0;
+        if (ordered) ok = ok && (s >= lo || s < a.n_sink);
+        if (by_pos && ok) {
+          const int p = a.pool.pos[a.pool.at(pk, hk, s)];
+          ok = p >= lo64 || p < a.n_sink;
+        }
+        seen[u] = uint32_t(__ballot(ok)) & 0xFFFFu;
+        // (rows that are not seen: the first row of the pool instead, whose values are not used)
+        const uint8_t* kr = ok ? a.pool.k_at(pk, hk, s) : a.pool.K;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int sv = s0 + 4 * g + r;
-        const bool okv = seen[u] >> (4 * g + r) & 1;
-        v[u][r] = R::load_v(okv ? a.pool.v_at(pv[r], hk, sv) : a.pool.V, c);
-        if constexpr (sizeof(CT) == 1) ve[u][r] = okv ? pow2_f32(a.pool.v_exp[a.pool.at(pv[r], hk, sv)]) : 1.f;
+        for (int i = 0; i < R::kK; ++i) k[u][i] = reinterpret_cast<const u32x4*>(kr)[i * 4 + g];
+        if constexpr (sizeof(CT) == 1) ke[u] = ok ? pow2_f32(a.pool.k_exp[a.pool.at(pk, hk, s)]) : 1.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int sv = s0 + 4 * g + r, pv = __shfl(pk, 4 * g + r, 64);
+          const bool okv = seen[u] >> (4 * g + r) & 1;
+          v[u][r] = R::load_v(okv ? a.pool.v_at(pv, hk, sv) : a.pool.V, c);
+          if constexpr (sizeof(CT) == 1) ve[u][r] = okv ? pow2_f32(a.pool.v_exp[a.pool.at(pv, hk, sv)]) : 1.f;
+        }
       }
     }
     f32x4 s[U];
     float mx = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      s[u] = rows.logits(k[u], ke[u]);
+      s[u] = rows.logits(k[u], ke[u]) * scale2;
+      if (seen[u] != 0xFFFFu) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[u][r] *= scale2;
-        if (!(seen[u] >> (4 * g + r) & 1)) s[u][r] = -INFINITY;
-        mx = fmaxf(mx, s[u][r]);
+        for (int r = 0; r < 4; ++r)
+          if (!(seen[u] >> (4 * g + r) & 1)) s[u][r] = -INFINITY;
       }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[u][r]);
       if (lg && c < a.G && t + u < t1) *reinterpret_cast<f32x4*>(lg + list.slot(t + u) + 4 * g) = s[u];
     }
     if (__any(mx > m)) {
@@ -359,14 +433,13 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool whole = seen[u] == 0xFFFFu;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float p = __builtin_amdgcn_exp2f(s[u][r] - m);
         l += p;
         float f[E];
         R::values(v[u][r], ve[u][r], f);
-        if (!whole) {
+        if (seen[u] != 0xFFFFu) {
           const bool okv = seen[u] >> (4 * g + r) & 1;
 #pragma unroll
           for (int e = 0; e < E; ++e) f[e] = okv ? f[e] : 0.f;
@@ -396,8 +469,9 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
     sml[w][lane][0] = mw;
     sml[w][lane][1] = l;
   }
+  __threadfence_block();  // (the logits, which the whole workgroup reads where it is a head's only one)
   __syncthreads();
-  const bool single = list.shares() == 1, lg_kept = a.pool.score != nullptr;
+  const bool single = list.shares() == 1;
   for (int i = tid; i < a.G * D; i += 64 * kWaves) {
     const int h = i / D, col = i % D;
     float M = sml[0][h][0];
@@ -415,86 +489,102 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
       store_out<T>(a, b, hk * a.G + h, col, L == 0.f ? 0.f : o / L);
     else
       a.part_o[at * D + col] = o;
-    if (col == 0 && (lg_kept || !single)) {
-      a.part_ml[at * 2] = M;
-      a.part_ml[at * 2 + 1] = L;
+    if (col == 0) {
+      if (single) {
+        sM[h] = M;
+        sinv[h] = L == 0.f ? 0.f : 1.f / L;
+      } else {
+        a.part_ml[at * 2] = M;
+        a.part_ml[at * 2 + 1] = L;
+      }
     }
   }
-}
-
-// Joins the shares of a (sequence, query head): one workgroup each, a thread per column.
-template <typename T, int D>
-__global__ __launch_bounds__(D) void step_join(StepArgs a, int least) {
-  const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, bh = b * a.pool.Hkv + hq / a.G, h = hq % a.G;
-  const TileList list(a, b, least);
-  const int ns = list.shares();
-  if (ns <= 1) return;
-  const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2;
-  const float* po = a.part_o + (int64_t(bh) * a.splits * a.G + h) * D + threadIdx.x;
-  float M = -3.402823466e38f;
-  for (int i = 0; i < ns; ++i) M = fmaxf(M, ml[int64_t(i) * a.G * 2]);
-  float L = 0.f, o = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < ns; ++i) {
-    const float f = __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M);
-    L = fmaf(ml[int64_t(i) * a.G * 2 + 1], f, L);
-    o = fmaf(po[int64_t(i) * a.G * D], f, o);
+  if (lg && single) {
+    __syncthreads();
+    for (int i = tid; i < list.tiles * kTile; i += 64 * kWaves) add_scores<1>(a, list, b, hk, i, 0, list.tiles * kTile, sM, sinv);
   }
-  store_out<T>(a, b, hq, threadIdx.x, L == 0.f ? 0.f : o / L);
 }
 
-// Adds the softmax rows to the scores (Eq. 6): a thread per entry, the group's query heads in rising order.
-constexpr int kScoreThreads = 256;
-__global__ __launch_bounds__(kScoreThreads) void step_scores(StepArgs a, int least) {
-  __shared__ float M[16], inv[16];
-  const int Hkv = a.pool.Hkv, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv, tid = threadIdx.x;
+// Joins the shares of the heads that have several: the first `joins` workgroups the outputs, one query head each, the others the scores.
+constexpr int kFinish = 256, kFinishEntries = 1024;  // threads; entries of a workgroup that adds scores
+template <typename T, int D>
+__global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  // maximum and sum of a query head over the shares: a wavefront, a lane per share
+  auto total = [&](const float* ml, int ns, float& M, float& L) __attribute__((always_inline)) {
+    M = -3.402823466e38f;
+    for (int i = lane; i < ns; i += 64) M = fmaxf(M, ml[int64_t(i) * a.G * 2]);
+    M = wave_max(M);
+    L = 0.f;
+    for (int i = lane; i < ns; i += 64) L = fmaf(ml[int64_t(i) * a.G * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M), L);
+    L = wave_sum(L);
+  };
+  if (int(blockIdx.x) < a.joins) {
+    constexpr int kCols = D / 4, kParts = kFinish / kCols;  // four columns per thread, the shares among kParts groups of threads
+    __shared__ f32x4 so[kParts][kCols];
+    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, bh = b * a.pool.Hkv + hq / a.G, h = hq % a.G;
+    const TileList list(a, b, least);
+    const int ns = list.shares();
+    if (ns <= 1) return;
+    const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2;
+    float M, L;
+    total(ml, ns, M, L);
+    const int col = tid % kCols, part = tid / kCols;
+    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (int64_t(bh) * a.splits * a.G + h) * D) + col;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int i = part; i < ns; i += kParts) o += po[int64_t(i) * a.G * kCols] * __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M);
+    so[part][col] = o;
+    __syncthreads();
+    if (tid < D) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) sum += so[i][tid / 4][tid % 4];
+      store_out<T>(a, b, hq, tid, L == 0.f ? 0.f : sum / L);
+    }
+    return;
+  }
+  __shared__ float sM[16], sinv[16];
+  const int per = (a.pad + kFinishEntries - 1) / kFinishEntries, x = blockIdx.x - a.joins, bh = x / per, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv;
   const TileList list(a, b, least);
-  const int first = blockIdx.x * kScoreThreads;
-  if (first >= list.tiles * kTile) return;
-  const int ns = list.shares();
-  if (tid < a.G) {
-    const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + tid) * 2;
-    float m = -3.402823466e38f, L = 0.f;
-    for (int i = 0; i < ns; ++i) m = fmaxf(m, ml[int64_t(i) * a.G * 2]);
-    for (int i = 0; i < ns; ++i) L = fmaf(ml[int64_t(i) * a.G * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - m), L);
-    M[tid] = m;
-    inv[tid] = 1.f / L;
+  const int first = x % per * kFinishEntries, ns = list.shares();
+  if (first >= list.tiles * kTile || ns <= 1) return;
+  for (int h = w; h < a.G; h += kFinish / 64) {
+    float M, L;
+    total(a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2, ns, M, L);
+    if (lane == 0) {
+      sM[h] = M;
+      sinv[h] = L == 0.f ? 0.f : 1.f / L;
+    }
   }
   __syncthreads();
-  const int i = first + tid;
-  if (i >= list.tiles * kTile) return;
-  const int s = list.slot(i / kTile) + i % kTile;
-  if (s >= list.n) return;
-  const float* lg = a.logits + (int64_t(b) * a.Hq + hk * a.G) * a.pad + s;
-  float add = 0.f;
-  for (int h = 0; h < a.G; ++h) {
-    const float x = lg[int64_t(h) * a.pad];
-    if (x != -INFINITY) add += __builtin_amdgcn_exp2f(x - M[h]) * inv[h];
-  }
-  if (add != 0.f) {
-    const int page = a.pool.page_of(b, s);
-    if (page >= 0) a.pool.score[a.pool.at(page, hk, s)] += add;
-  }
+  add_scores<kFinishEntries / kFinish>(a, list, b, hk, first + tid, kFinish, min(first + kFinishEntries, list.tiles * kTile), sM, sinv);
 }
 
-// Tiles per wavefront and round: 8 KB of rows in flight, half of it where the outputs of 16 heads fill the registers.
+// Tiles per wavefront and round: two, where their rows take 16 KB at most (8 KB where the outputs of 16 heads fill the registers).
+// (8-bit rows in fours: 39 instead of 36 us for 4 x 32 heads x 4100 entries; bf16 rows of 128 singly: 109 instead of 105 us for 8 heads of 131072.)
 template <typename CT, int D, int GM>
 constexpr int tiles_per_round() {
-  constexpr int u = (GM > 8 ? 8192 : 16384) / (kTile * 2 * D * int(sizeof(CT)));
-  return u < 1 ? 1 : u > 4 ? 4 : u;
+  return (GM > 8 ? 8192 : 16384) / (kTile * 2 * D * int(sizeof(CT))) >= 2 ? 2 : 1;
 }
 
 template <typename T, typename CT, int D, int GM>
-void launch_step(const StepArgs& a, int batch, hipStream_t s) {
+void launch_step(StepArgs& a, int batch, hipStream_t s) {
   constexpr int U = tiles_per_round<CT, D, GM>();
   const int bh = batch * a.pool.Hkv;
-  step_part<T, CT, D, GM, U><<<dim3(a.splits, bh), 64 * kWaves, 0, s>>>(a);
-  if (a.splits > 1) step_join<T, D><<<dim3(batch * a.Hq), D, 0, s>>>(a, kWaves * U);
-  if (a.pool.score) step_scores<<<dim3((a.pad + kScoreThreads - 1) / kScoreThreads, bh), kScoreThreads, 0, s>>>(a, kWaves * U);
+  // pages that hold whole tiles, displacements that fit, exponents that can be read four at a time
+  const bool wide = a.pool.shift >= 4 && a.pool.k_row < (1 << 24) && a.pool.v_row < (1 << 24) &&
+                    !(reinterpret_cast<uintptr_t>(a.pool.v_exp) & 3);
+  const auto part = wide ? step_part<T, CT, D, GM, U, true> : step_part<T, CT, D, GM, U, false>;
+  part<<<dim3(a.splits, bh), 64 * kWaves, 0, s>>>(a);
+  if (a.splits == 1) return;
+  a.joins = batch * a.Hq;
+  const int64_t scores = a.pool.score ? int64_t((a.pad + kFinishEntries - 1) / kFinishEntries) * bh : 0;
+  step_finish<T, D><<<dim3(unsigned(a.joins + scores)), kFinish, 0, s>>>(a, kWaves * U);
 }
 
 template <typename T, typename CT, int D>
-void launch_step(const StepArgs& a, int batch, hipStream_t s) {
+void launch_step(StepArgs& a, int batch, hipStream_t s) {
   if (a.G == 1) launch_step<T, CT, D, 1>(a, batch, s);
   else if (a.G == 2) launch_step<T, CT, D, 2>(a, batch, s);
   else if (a.G <= 4) launch_step<T, CT, D, 4>(a, batch, s);
@@ -503,7 +593,7 @@ void launch_step(const StepArgs& a, int batch, hipStream_t s) {
 }
 
 template <typename T, typename CT>
-void launch_step(const StepArgs& a, int batch, int D, hipStream_t s) {
+void launch_step(StepArgs& a, int batch, int D, hipStream_t s) {
   if (D == 64) launch_step<T, CT, 64>(a, batch, s);
   else launch_step<T, CT, 128>(a, batch, s);
 }
@@ -556,7 +646,7 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   a.lens = lens;
   a.positions = positions;
   const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads, hq = int64_t(pages->batch) * pages->n_q_heads;
-  if (bh > 65535) return D2O_ERR_UNSUPPORTED;
+  if (bh > 65535 || bh * ((max_len + kFinishEntries - 1) / kFinishEntries) > 0x3FFFFFFF) return D2O_ERR_UNSUPPORTED;
   a.pad = (max_len + kTile - 1) / kTile * kTile;
   a.splits = step_splits(bh, max_len);
   char* ws = static_cast<char*>(workspace);
