@@ -333,7 +333,8 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * Q, O: [B][Hq][n][d]; K, V: [B][Hkv][n][d]; O in `dtype`.  lens: device [B], the tokens of each sequence
  * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
  * its keys behind the end are never looked at.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
- * INVALID_ARG, UNSUPPORTED, CAPACITY (workspace smaller than d2o_window_workspace_bytes says), HIP. */
+ * INVALID_ARG, UNSUPPORTED (also a row stride of K of 2^24 elements or more), CAPACITY (workspace smaller than
+ * d2o_window_workspace_bytes says; where it says 0, NULL will do), HIP. */
 int d2o_window_workspace_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                size_t* bytes);
 int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,

@@ -439,12 +439,20 @@ def _vector_ok(t, shape, dtype, device, what):
     _tensor_ok(t, shape, dtype, device, what, whole=True)
 
 
+def _public_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# (the public call makes a Stream object first: 4 us of a step's 13)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_stream)
+
+
 def _enqueue(device, call):
     """call(stream) with `device` current, which it nearly always is already."""
     if torch.cuda.current_device() == device.index:
-        return call(torch.cuda.current_stream().cuda_stream)
+        return call(_current_stream(device.index))
     with torch.cuda.device(device):
-        return call(torch.cuda.current_stream().cuda_stream)
+        return call(_current_stream(device.index))
 
 
 def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=None):
@@ -469,10 +477,10 @@ def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=No
     _ok(lib.d2o_window_workspace_bytes(B, n, Hkv, d, code, C.byref(need)), "d2o_window_workspace_bytes")
 
     def call(stream):
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
         return lib.d2o_window_attend(B, n, Hq, Hkv, d, code, _view_of(Q), _view_of(K), _view_of(V),
                                      lens.data_ptr() if lens is not None else None, window, n_sink, _view_of(O),
-                                     ws.data_ptr(), need.value, stream)
+                                     None if ws is None else ws.data_ptr(), need.value, stream)
     _ok(_enqueue(dev, call), "d2o_window_attend")
     return O
 

@@ -71,18 +71,24 @@ __device__ __forceinline__ void clear_bins(SelectShared& sh) {
 }
 
 // The `want`-th largest of the 32-bit values that `each_value(f)` hands to f(value) on all threads together; `equal` becomes how many of
-// those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.
+// those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.  (Protected entries share one value: a thread
+// counts its own, for thousands of them would queue at one bin.)
 template <int NT, int FIRST = 0, typename F>
 __device__ __forceinline__ uint32_t nth_largest(SelectShared& sh, int want, int& equal, int& same, const F& each_value) {
   uint32_t prefix = 0;
+  int mine = 0;
 #pragma unroll
   for (int pass = FIRST; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digit = pass == 2 ? 1023u : 2047u;
     clear_bins<NT>(sh);
     each_value([&](uint32_t v) {
-      if (pass == 0 || (v >> (pass == 1 ? 21 : 10)) == (prefix >> (pass == 1 ? 21 : 10))) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
+      const bool in = pass == 0 || (v >> (pass == 1 ? 21 : 10)) == (prefix >> (pass == 1 ? 21 : 10));
+      if (in && v == kProtected) ++mine;
+      else if (in) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
     });
+    if (mine) atomicAdd(&sh.hist[digit], mine);
+    mine = 0;
     pick_bin<NT>(sh, want);
     prefix |= uint32_t(sh.bin) << shift;
     want = sh.left;
@@ -133,9 +139,11 @@ struct FillArgs {
   const int32_t* lens;
   const float* scores;
   int32_t* src;    // [B][Hkv][budget] kept positions, rising (where some are evicted)
-  uint16_t* hist;  // longer prompts: [B][Hkv][slices][kBins] of a slice's keys
-  int32_t* slice;  // [B][Hkv][slices][2] kept entries before a slice: above the threshold, equal to it
-  uint32_t* mark;  // [B][Hkv][2] threshold, how many equal to it are kept
+  // longer prompts, by slices:
+  uint16_t* hist;  // [B][Hkv][slices][kBins] of a slice's keys
+  uint32_t* cand;  // [B][Hkv][n] the tokens in the threshold's bin: slice and lower 21 bits of the key, slice by slice in any order
+  int32_t* above;  // [B][Hkv][slices] keys above that bin
+  int32_t* head;   // [B][Hkv][4] candidates, the bin, how many of it are kept
   int32_t n, budget, recent, n_sink, slices;
 
   __device__ __forceinline__ int length(int b) const { return lens ? min(max(lens[b], 0), n) : n; }
@@ -205,128 +213,116 @@ __global__ __launch_bounds__(kSliceThreads) void fill_hist(FillArgs a) {
   __syncthreads();
   uint32_t* out = reinterpret_cast<uint32_t*>(a.hist + (int64_t(bh) * a.slices + blockIdx.x) * kBins);
   for (int i = tid; i < kBins / 2; i += kSliceThreads) out[i] = uint32_t(hist[2 * i]) | uint32_t(hist[2 * i + 1]) << 16;
+  if (blockIdx.x == 0 && tid == 0) a.head[bh * 4] = 0;
 }
 
-// ... then one workgroup per head: the bin that holds the threshold, the tokens in it (their other bits and their slice) into LDS,
-// the threshold among those, and how many entries each slice keeps.  (More candidates than fit: the head's scores are
-// read again for every digit.)
-constexpr int kMark = 1024, kCand = 24576, kMaxSlices = 2048;
-__global__ __launch_bounds__(kMark) void fill_mark(FillArgs a) {
+// ... then the bin that holds the threshold (found by every slice for itself from all histograms: a workgroup that did it for
+// the head, and then read all its scores, took 48 us at 131072 tokens), and the tokens in it to the head's list ...
+constexpr int kMaxSlices = 2048;
+__global__ __launch_bounds__(kSliceThreads) void fill_candidates(FillArgs a) {
   __shared__ SelectShared sh;
-  __shared__ uint32_t cand[kCand];
-  __shared__ int gt[kMaxSlices], eq[kMaxSlices];
-  __shared__ int ncand;
-  const int bh = blockIdx.x, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63;
+  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
+  __shared__ int at;
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j0 = blockIdx.x * kSlice;
   const int n = a.length(b);
-  if (n <= a.budget) return;
+  if (n <= a.budget || j0 >= n) return;
+  uint32_t key[kSlicePer];
+  a.keys<kSlicePer>(a.scores + int64_t(bh) * a.n, n, j0 + tid, kSliceThreads, key);
   const int slices = (n + kSlice - 1) / kSlice;
-  const float* sc = a.scores + int64_t(bh) * a.n;
-  const uint32_t* hist = reinterpret_cast<const uint32_t*>(a.hist + int64_t(bh) * a.slices * kBins);
-  int lo = 0, hi = 0;
+  constexpr int kWords = kBins / 2 / kSliceThreads;  // pairs of bins per thread
+  static_assert(kWords == 4, "a load of 16 bytes");
+  const u32x4* hist = reinterpret_cast<const u32x4*>(a.hist + int64_t(bh) * a.slices * kBins) + tid;
+  int sum[2 * kWords] = {};
 #pragma unroll 8
   for (int s = 0; s < slices; ++s) {
-    const uint32_t v = hist[int64_t(s) * (kBins / 2) + tid];
-    lo += v & 0xFFFF;
-    hi += v >> 16;
+    const u32x4 v = hist[int64_t(s) * (kBins / 8)];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      sum[2 * i] += v[i] & 0xFFFF;
+      sum[2 * i + 1] += v[i] >> 16;
+    }
   }
-  sh.hist[2 * tid] = lo;
-  sh.hist[2 * tid + 1] = hi;
-  for (int i = tid; i < slices; i += kMark) gt[i] = eq[i] = 0;
-  if (tid == 0) ncand = 0;
-  pick_bin<kMark>(sh, a.budget);
+#pragma unroll
+  for (int i = 0; i < 2 * kWords; ++i) sh.hist[tid * 2 * kWords + i] = sum[i];
+  pick_bin<kSliceThreads>(sh, a.budget);
   const uint32_t top = sh.bin;
-  const int want = sh.left, total = sh.above;
-  __syncthreads();
-  const bool fits = total <= kCand;
-  constexpr int kBatch = 16;  // loads in flight per thread; a wavefront's 64 tokens lie in one slice
-  for (int j0 = 0; j0 < n; j0 += kBatch * kMark) {
-    uint32_t k[kBatch];
-    int in_all = 0;
-    a.keys<kBatch>(sc, n, j0 + tid, kMark, k);
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int j = j0 + u * kMark + tid;
-      const uint64_t above = __ballot(j < n && k[u] >> 21 > top);
-      if (above && lane == 0) atomicAdd(&gt[j / kSlice], __popcll(above));
-      in_all += __popcll(__ballot(j < n && k[u] >> 21 == top));
-    }
-    if (!in_all || !fits) continue;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&ncand, in_all);
-    at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int j = j0 + u * kMark + tid;
-      const bool is = j < n && k[u] >> 21 == top;
-      const uint64_t in = __ballot(is);
-      if (is) cand[at + lanes_before(in)] = (k[u] & 0x1FFFFF) | uint32_t(j / kSlice) << 21;
-      at += __popcll(in);
+  for (int u = 0; u < kSlicePer; ++u) {
+    const bool in = j0 + u * kSliceThreads + tid < n;
+    const uint32_t v = uint32_t(__popcll(__ballot(in && key[u] >> 21 > top))) | uint32_t(__popcll(__ballot(in && key[u] >> 21 == top))) << 16;
+    if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = v;
+  }
+  prefix_counts<kSliceThreads, kSlicePer>(cnt);
+  const uint32_t all = cnt[kSlicePer * (kSliceThreads / 64)];
+  if (tid == 0) {
+    a.above[int64_t(bh) * a.slices + blockIdx.x] = int(all & 0xFFFF);
+    at = atomicAdd(&a.head[bh * 4], int(all >> 16));
+    if (blockIdx.x == 0) {
+      a.head[bh * 4 + 1] = int(top);
+      a.head[bh * 4 + 2] = sh.left;
     }
   }
   __syncthreads();
-  auto each_low = [&](auto f) {  // the lower 21 bits of the bin's keys, and their slice
+  uint32_t* cand = a.cand + int64_t(bh) * a.n + at;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const bool is = j0 + u * kSliceThreads + tid < n && key[u] >> 21 == top;
+    const uint64_t m = __ballot(is);
+    if (is) cand[int(cnt[u * (kSliceThreads / 64) + w] >> 16) + lanes_before(m)] = (key[u] & 0x1FFFFF) | uint32_t(blockIdx.x) << 21;
+  }
+}
+
+// ... and every slice finds the threshold among the candidates, counts what the slices before it keep, and lists its kept positions
+// behind those.  (Their rows are copied by a launch of their own: the slice with the recent tokens has more than all others.)
+constexpr int kCand = 8192;  // candidates held in LDS
+__global__ __launch_bounds__(kSliceThreads) void fill_list(FillArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ uint32_t held[kCand];
+  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
+  __shared__ int before[2];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = a.length(b), j0 = blockIdx.x * kSlice, me = blockIdx.x;
+  if (n <= a.budget || j0 >= n) return;
+  uint32_t key[kSlicePer];
+  a.keys<kSlicePer>(a.scores + int64_t(bh) * a.n, n, j0 + tid, kSliceThreads, key);
+  const int total = a.head[bh * 4];
+  const uint32_t top = a.head[bh * 4 + 1];
+  const uint32_t* list = a.cand + int64_t(bh) * a.n;
+  const bool fits = total <= kCand;
+  if (fits)
+    for (int i = tid; i < total; i += kSliceThreads) held[i] = list[i];
+  if (tid < 2) before[tid] = 0;
+  __syncthreads();
+  auto each_candidate = [&](auto f) {
     if (fits) {
-      for (int i = tid; i < total; i += kMark) f(cand[i] & 0x1FFFFF, cand[i] >> 21);
+      for (int i = tid; i < total; i += kSliceThreads) f(held[i]);
     } else {
-      for (int j = tid; j < n; j += kMark) {
-        uint32_t k;
-        a.keys<1>(sc, n, j, 0, &k);
-        if (k >> 21 == top) f(k & 0x1FFFFF, uint32_t(j) / kSlice);
-      }
+#pragma unroll 8
+      for (int i = tid; i < total; i += kSliceThreads) f(list[i]);
     }
   };
   int equal, same;
-  const uint32_t low = nth_largest<kMark, 1>(sh, want, equal, same, [&](auto f) { each_low([&](uint32_t v, uint32_t) { f(v); }); });
-  each_low([&](uint32_t v, uint32_t s) {
-    if (v > low) atomicAdd(&gt[s], 1);
-    if (v == low) atomicAdd(&eq[s], 1);
+  const uint32_t low = nth_largest<kSliceThreads, 1>(sh, a.head[bh * 4 + 2], equal, same,
+                                                     [&](auto f) { each_candidate([&](uint32_t v) { f(v & 0x1FFFFF); }); });
+  int gt0 = 0, eq0 = 0;  // kept by the slices before: above the threshold, level with it
+  for (int s = tid; s < me; s += kSliceThreads) gt0 += a.above[int64_t(bh) * a.slices + s];
+  each_candidate([&](uint32_t v) {
+    if (int(v >> 21) < me) {
+      gt0 += (v & 0x1FFFFF) > low;
+      eq0 += (v & 0x1FFFFF) == low;
+    }
   });
-  __syncthreads();
-  if (tid < 64) {  // counts before each slice
-    int g0 = 0, e0 = 0;
-    for (int s0 = 0; s0 < slices; s0 += 64) {
-      const int g = s0 + lane < slices ? gt[s0 + lane] : 0, e = s0 + lane < slices ? eq[s0 + lane] : 0;
-      int gi = g, ei = e;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(gi, o, 64), y = __shfl_up(ei, o, 64);
-        if (lane >= o) gi += x, ei += y;
-      }
-      if (s0 + lane < slices) {
-        int32_t* out = a.slice + (int64_t(bh) * a.slices + s0 + lane) * 2;
-        out[0] = g0 + gi - g;
-        out[1] = e0 + ei - e;
-      }
-      g0 += __shfl(gi, 63, 64);
-      e0 += __shfl(ei, 63, 64);
-    }
-    if (tid == 0) {
-      a.mark[bh * 2] = top << 21 | low;
-      a.mark[bh * 2 + 1] = equal;
-    }
-  }
-}
-
-// ... and the slices' kept positions, in order behind those of the slices before.  (Their rows are copied by a launch of their own: the
-// slice with the recent tokens has more than all others.)
-__global__ __launch_bounds__(kSliceThreads) void fill_list(FillArgs a) {
-  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
-  const int bh = blockIdx.y, b = bh / a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int n = a.length(b), j0 = blockIdx.x * kSlice;
-  if (n <= a.budget || j0 >= n) return;
-  const float* sc = a.scores + int64_t(bh) * a.n;
-  const uint32_t t = a.mark[bh * 2];
-  const int equal = a.mark[bh * 2 + 1];
-  const int32_t* before = a.slice + (int64_t(bh) * a.slices + blockIdx.x) * 2;
-  const int gt0 = before[0], eq0 = before[1];
-  uint32_t key[kSlicePer];
-  a.keys<kSlicePer>(sc, n, j0 + tid, kSliceThreads, key);
+  if (gt0) atomicAdd(&before[0], gt0);
+  if (eq0) atomicAdd(&before[1], eq0);
+  const uint32_t t = top << 21 | low;
 #pragma unroll
   for (int u = 0; u < kSlicePer; ++u) {
     const uint32_t v = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
     if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = v;
   }
   prefix_counts<kSliceThreads, kSlicePer>(cnt);
+  gt0 = before[0];
+  eq0 = before[1];
   const int quota = max(0, equal - eq0);  // of the equal ones of this slice
   int32_t* src = a.src + int64_t(bh) * a.budget + gt0 + min(eq0, equal);
 #pragma unroll
@@ -659,11 +655,11 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int lanes) {
                a.count[bh], threadIdx.x % lanes);
 }
 
-// Workspace of a fill: a list of kept positions; of a long prompt also the slices' histograms and counts and the thresholds.
+// Workspace of a fill: a list of kept positions; of a long prompt also the slices' histograms and counts, and the candidates.
 size_t fill_bytes(size_t bh, size_t n) {
   const size_t list = round256(bh * n * sizeof(int32_t)), slices = (n + kSlice - 1) / kSlice;
   if (n <= kFillSelect) return list;
-  return list + round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * 2 * sizeof(int32_t)) + round256(bh * 2 * sizeof(uint32_t));
+  return 2 * list + round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * sizeof(int32_t)) + round256(bh * 4 * sizeof(int32_t));
 }
 size_t moves_bytes(size_t bh, size_t n) { return round256(bh * 2 * n * sizeof(int32_t)) + round256(bh * sizeof(int32_t)); }
 }  // namespace
@@ -705,16 +701,18 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
   char* ws = static_cast<char*>(workspace);
   a.src = reinterpret_cast<int32_t*>(ws);
   ws += round256(size_t(bh) * n * sizeof(int32_t));
+  a.cand = reinterpret_cast<uint32_t*>(ws);
+  ws += round256(size_t(bh) * n * sizeof(int32_t));
   a.hist = reinterpret_cast<uint16_t*>(ws);
   ws += round256(size_t(bh) * a.slices * kBins * sizeof(uint16_t));
-  a.slice = reinterpret_cast<int32_t*>(ws);
-  ws += round256(size_t(bh) * a.slices * 2 * sizeof(int32_t));
-  a.mark = reinterpret_cast<uint32_t*>(ws);
+  a.above = reinterpret_cast<int32_t*>(ws);
+  ws += round256(size_t(bh) * a.slices * sizeof(int32_t));
+  a.head = reinterpret_cast<int32_t*>(ws);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 heads{unsigned(bh)};
   if (most < n && n > kFillSelect) {
     fill_hist<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
-    fill_mark<<<heads, kMark, 0, s>>>(a);
+    fill_candidates<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
     fill_list<<<dim3(a.slices, unsigned(bh)), kSliceThreads, 0, s>>>(a);
   } else if (most < n) {
     if (n <= 2048)

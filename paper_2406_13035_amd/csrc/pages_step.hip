@@ -316,12 +316,18 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
   }
   if (t0 >= t1) return;
   const int n = list.n;
-  // the workgroup of the last tile stores the new token before it reads the tile
+  // the workgroup of the last tile stores the new token; it reads it where it came from, not to wait for the store
+  int fresh = -1;
   if (a.kn.ptr && t1 == list.tiles && a.lens[b] <= a.max_len) {
     const int page = a.pool.page_of(b, n - 1);
-    if (page >= 0) store_new<T, CT, D>(a, b, hk, page, n - 1, list.last);
-    __threadfence_block();
-    __syncthreads();
+    if (page >= 0) {
+      store_new<T, CT, D>(a, b, hk, page, n - 1, list.last);
+      fresh = n - 1;
+    }
+    if constexpr (sizeof(CT) == 1) {  // read back, as it was encoded
+      __threadfence_block();
+      __syncthreads();
+    }
   }
   R rows;
   rows.load_q(c < a.G ? static_cast<const T*>(a.q.ptr) + b * a.q.sb + (hk * a.G + c) * a.q.sh : nullptr, g);
@@ -404,6 +410,25 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
           const bool okv = seen[u] >> (4 * g + r) & 1;
           v[u][r] = R::load_v(okv ? a.pool.v_at(pv, hk, sv) : a.pool.V, c);
           if constexpr (sizeof(CT) == 1) ve[u][r] = okv ? pow2_f32(a.pool.v_exp[a.pool.at(pv, hk, sv)]) : 1.f;
+        }
+      }
+    }
+    if constexpr (sizeof(CT) > 1) {
+      if (fresh >= 0) {
+        const uint8_t* kn = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.kn.ptr) + b * a.kn.sb + hk * a.kn.sh);
+        const uint8_t* vn = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.vn.ptr) + b * a.vn.sb + hk * a.vn.sh);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int at = fresh - (t + u < t1 ? list.slot(t + u) : n);
+          if (at < 0 || at >= kTile) continue;
+          if (c == at) {
+#pragma unroll
+            for (int i = 0; i < R::kK; ++i) k[u][i] = *reinterpret_cast<const u32x4*>(kn + (i * 4 + g) * 16);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * g + r == at) v[u][r] = R::load_v(vn, c);
+          if (by_pos) seen[u] |= 1u << at;  // (its position is being written)
         }
       }
     }

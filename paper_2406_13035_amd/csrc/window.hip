@@ -579,7 +579,7 @@ size_t values_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_d
   return size_t(batch) * n_kv_heads * ((n + 63) / 64) * head_dim * 64 * sizeof(uint16_t);
 }
 size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
-  if (dtype == D2O_F32) return 16;  // (nothing is kept there)
+  if (dtype == D2O_F32) return 0;
   return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * kRec * sizeof(float);
 }
 
@@ -618,8 +618,9 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   if (n_q_heads < 1 || n_q_heads % n_kv_heads || window < 0 || n_sink < 0) return D2O_ERR_INVALID_ARG;
   for (const d2o_view* v : {&Q, &K, &V, &O})
     if (!dense_view_ok(*v, es, true)) return D2O_ERR_INVALID_ARG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
-  if (workspace_bytes < window_bytes(batch, n, n_kv_heads, head_dim, dtype)) return D2O_ERR_CAPACITY;
+  const size_t need = window_bytes(batch, n, n_kv_heads, head_dim, dtype);
+  if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return D2O_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return D2O_ERR_CAPACITY;
   if (int64_t(batch) * n_q_heads * ((n + 63) / 64) > 0x7FFFFFFF) return D2O_ERR_UNSUPPORTED;
   if (K.stride_n >= 1 << 24) return D2O_ERR_UNSUPPORTED;  // (displacements inside a tile of 64 keys have 32 bits)
   WindowArgs a{};
