@@ -71,12 +71,10 @@ __device__ __forceinline__ void clear_bins(SelectShared& sh) {
 }
 
 // The `want`-th largest of the 32-bit values that `each_value(f)` hands to f(value) on all threads together; `equal` becomes how many of
-// those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.  (Protected entries share one value: a thread
-// counts its own, for thousands of them would queue at one bin.)
+// those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.
 template <int NT, int FIRST = 0, typename F>
 __device__ __forceinline__ uint32_t nth_largest(SelectShared& sh, int want, int& equal, int& same, const F& each_value) {
   uint32_t prefix = 0;
-  int mine = 0;
 #pragma unroll
   for (int pass = FIRST; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
@@ -84,11 +82,8 @@ __device__ __forceinline__ uint32_t nth_largest(SelectShared& sh, int want, int&
     clear_bins<NT>(sh);
     each_value([&](uint32_t v) {
       const bool in = pass == 0 || (v >> (pass == 1 ? 21 : 10)) == (prefix >> (pass == 1 ? 21 : 10));
-      if (in && v == kProtected) ++mine;
-      else if (in) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
+      if (in) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
     });
-    if (mine) atomicAdd(&sh.hist[digit], mine);
-    mine = 0;
     pick_bin<NT>(sh, want);
     prefix |= uint32_t(sh.bin) << shift;
     want = sh.left;
@@ -173,12 +168,15 @@ __global__ __launch_bounds__(NT) void fill_select(FillArgs a) {
   const float* sc = a.scores + int64_t(bh) * a.n;
   uint32_t key[PT];
   a.keys<PT>(sc, n, tid, NT, key);
-  int equal, same;
-  const uint32_t t = nth_largest<NT>(sh, a.budget, equal, same, [&](auto f) {
+  // among those that are not protected (these share one key, at whose bin thousands would queue): n_sink + recent are
+  int equal = a.n_sink + a.recent, same;
+  uint32_t t = kProtected;
+  if (a.budget > equal)
+    t = nth_largest<NT>(sh, a.budget - equal, equal, same, [&](auto f) {
 #pragma unroll
-    for (int u = 0; u < PT; ++u)
-      if (u * NT + tid < n) f(key[u]);
-  });
+      for (int u = 0; u < PT; ++u)
+        if (u * NT + tid < n && key[u] != kProtected) f(key[u]);
+    });
 #pragma unroll
   for (int u = 0; u < PT; ++u) {
     const uint32_t c = uint32_t(__popcll(__ballot(key[u] > t))) | uint32_t(__popcll(__ballot(key[u] == t))) << 16;
@@ -392,7 +390,8 @@ struct EvictArgs {
   int32_t* count;  // [B][Hkv] pairs
   int32_t max_len, budget, recent, n_sink, most;
 };
-constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself
+constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself (256 rows of 32 heads: 15.7 us,
+                              // in a launch of their own 18)
 
 // Kept rows into holes, `lanes` lanes of 16 bytes per row: pairs i0, i0 + step, .. below `pairs`, a few at a time on their way.  Sources lie
 // at or behind the budget, targets below it: moves never meet.
@@ -445,6 +444,11 @@ struct Rank {
 };
 __device__ __forceinline__ Rank rank_of(const EvictArgs& a, float score, int32_t p, int64_t late) {
   return {p < a.n_sink || p > late ? kProtected : score_key(score), ~(uint32_t(p) ^ 0x80000000u)};
+}
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
 }
 template <int NT>
 __device__ __forceinline__ int block_max(int v, int* buf) {
@@ -562,10 +566,23 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
     return;
   }
 
-  int equal, same;
-  const uint32_t t = nth_largest<NT>(sh, S, equal, same, [&](auto f) __attribute__((always_inline)) {
-    each_rank([&](int, const Rank& x) { f(x.key); });
-  });
+  // the threshold, among the entries that are not protected (which share one key, at whose bin thousands would queue)
+  int guarded = 0;
+  each_rank([&](int, const Rank& x) { guarded += x.key == kProtected; });
+  guarded = wave_total(guarded);
+  if (lane == 0) sh.wave[w] = guarded;
+  __syncthreads();
+  guarded = 0;
+  for (int i = 0; i < NT / 64; ++i) guarded += sh.wave[i];
+  __syncthreads();
+  int equal = S, same = guarded;
+  uint32_t t = kProtected;
+  if (guarded < S)
+    t = nth_largest<NT>(sh, S - guarded, equal, same, [&](auto f) __attribute__((always_inline)) {
+      each_rank([&](int, const Rank& x) {
+        if (x.key != kProtected) f(x.key);
+      });
+    });
   // of several entries with the threshold's key only some are kept: those with the lowest positions
   uint32_t tl = 0;
   bool split = equal < same;
