@@ -390,9 +390,9 @@ int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view 
                    const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
                    void* workspace, size_t workspace_bytes, void* stream);
 
-/* Evicts in place.  Every KV head of a sequence with lens[b] > budget entries (device [B], read only) keeps `budget` of
- * them: the positions below n_sink and above the newest position - recent, then the highest scores (equal scores: the lower
- * position, then the lower entry; NaN ranks highest).  Kept entries below `budget` stay where they are; the i-th given-up entry below
+/* Evicts in place.  Every KV head of a sequence with lens[b] > budget entries (device [B], read only) keeps the `budget` highest of
+ * them: an entry with a position below n_sink or above the newest position - recent is above one without, otherwise the higher score is
+ * above (NaN the highest), then the lower position, then the lower entry.  Kept entries below `budget` stay where they are; the i-th given-up entry below
  * it takes row, score and position of the i-th kept one behind it.  Afterwards the sequence has min(lens[b], budget)
  * entries; the rows behind are left as they were.  pages->score must not be NULL, and pages->pos not either (an entry moves, its position with it).
  * max_len as for d2o_pages_step.  Errors: INVALID_ARG (budget < max(1, n_sink + recent)), UNSUPPORTED, CAPACITY, HIP. */

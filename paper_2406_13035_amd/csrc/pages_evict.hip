@@ -438,16 +438,26 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int hk, con
   }
 }
 
-// What decides about an entry: protected ones first, then by score, then by position; without a page last.
+// What decides about an entry: protected ones first, then by score, then by position; without a page last.  `crowded`: more are protected than
+// stay (positions that occur more than once): these go by score too, and the others are below all of them.
 struct Rank {
   uint32_t key, low;
 };
-__device__ __forceinline__ Rank rank_of(const EvictArgs& a, float score, int32_t p, int64_t late) {
-  return {p < a.n_sink || p > late ? kProtected : score_key(score), ~(uint32_t(p) ^ 0x80000000u)};
+__device__ __forceinline__ bool is_guarded(const EvictArgs& a, int32_t p, int64_t late) { return p < a.n_sink || p > late; }
+__device__ __forceinline__ Rank rank_of(const EvictArgs& a, float score, int32_t p, int64_t late, bool crowded) {
+  const bool guarded = is_guarded(a, p, late);
+  const uint32_t k = score_key(score);
+  return {crowded ? (guarded ? k : 1u) : (guarded ? kProtected : k), ~(uint32_t(p) ^ 0x80000000u)};
 }
-__device__ __forceinline__ int wave_total(int v) {
+template <int NT>
+__device__ __forceinline__ int block_total(int v, int* buf) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+  for (int i = 0; i < NT / 64; ++i) v += buf[i];
+  __syncthreads();
   return v;
 }
 template <int NT>
@@ -512,18 +522,33 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   }
   newest = block_max<NT>(newest, sh.wave);
   const int64_t late = int64_t(newest) - a.recent;
+  // the protected entries: more than stay?
+  int guarded = 0;
+  if constexpr (PT > 0) {
+#pragma unroll
+    for (int u = 0; u < PT; ++u) guarded += (present >> u & 1) && is_guarded(a, pos[u], late);
+  } else {
+#pragma unroll 4
+    for (int j = tid; j < n; j += NT) {
+      float sc;
+      int32_t p;
+      guarded += look(j, sc, p) && is_guarded(a, p, late);
+    }
+  }
+  guarded = block_total<NT>(guarded, sh.wave);
+  const bool crowded = guarded > S;
   Rank r[kKeep];
   if constexpr (PT > 0) {
 #pragma unroll
     for (int u = 0; u < PT; ++u) {
-      r[u] = rank_of(a, score[u], pos[u], late);
+      r[u] = rank_of(a, score[u], pos[u], late, crowded);
       if (!(present >> u & 1)) r[u] = {0, 0};
     }
   }
   auto rank_at = [&](int j) __attribute__((always_inline)) {
     float sc;
     int32_t p;
-    return look(j, sc, p) ? rank_of(a, sc, p, late) : Rank{0, 0};
+    return look(j, sc, p) ? rank_of(a, sc, p, late, crowded) : Rank{0, 0};
   };
   auto each_rank = [&](auto f) __attribute__((always_inline)) {  // f(entry, rank)
     if constexpr (PT > 0) {
@@ -567,42 +592,67 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   }
 
   // the threshold, among the entries that are not protected (which share one key, at whose bin thousands would queue)
-  int guarded = 0;
-  each_rank([&](int, const Rank& x) { guarded += x.key == kProtected; });
-  guarded = wave_total(guarded);
-  if (lane == 0) sh.wave[w] = guarded;
-  __syncthreads();
-  guarded = 0;
-  for (int i = 0; i < NT / 64; ++i) guarded += sh.wave[i];
-  __syncthreads();
   int equal = S, same = guarded;
   uint32_t t = kProtected;
-  if (guarded < S)
-    t = nth_largest<NT>(sh, S - guarded, equal, same, [&](auto f) __attribute__((always_inline)) {
+  if (guarded != S)
+    t = nth_largest<NT>(sh, crowded ? S : S - guarded, equal, same, [&](auto f) __attribute__((always_inline)) {
       each_rank([&](int, const Rank& x) {
         if (x.key != kProtected) f(x.key);
       });
     });
-  // of several entries with the threshold's key only some are kept: those with the lowest positions
+  // Of several entries with the threshold's key only some stay: those with the lowest positions, of equal positions the first entries; (tl, ts)
+  // are the last one's.  A few are ranked against each other, many selected digit by digit.
   uint32_t tl = 0;
-  bool split = equal < same;
-  if (split)
+  int ts = INT32_MAX;
+  constexpr int kFew = 256;
+  static_assert(kFew <= NT && 2 * kFew <= 2 * kInline, "a thread and two words each");
+  if (equal < same && same <= kFew) {
+    if (tid == 0) sh.bin = 0;
+    __syncthreads();
+    each_rank([&](int j, const Rank& x) {
+      if (x.key != t) return;
+      const int i = atomicAdd(&sh.bin, 1);
+      lists[i] = int(x.low);
+      lists[kFew + i] = j;
+    });
+    __syncthreads();
+    if (tid < same) {
+      const uint32_t low = lists[tid];
+      const int j = lists[kFew + tid];
+      int before = 0;
+      for (int i = 0; i < same; ++i) before += uint32_t(lists[i]) > low || (uint32_t(lists[i]) == low && lists[kFew + i] < j);
+      if (before == equal - 1) {
+        sh.left = int(low);
+        sh.above = j;
+      }
+    }
+    __syncthreads();
+    tl = sh.left;
+    ts = sh.above;
+  } else if (equal < same) {
     tl = nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
       each_rank([&](int, const Rank& x) {
         if (x.key == t) f(x.low);
       });
     });
-  auto above = [&](const Rank& x) { return x.key > t || (x.key == t && (!split || x.low > tl)); };
-  auto level = [&](const Rank& x) { return split && x.key == t && x.low == tl; };
+    if (equal < same)
+      ts = ~int(nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
+        each_rank([&](int j, const Rank& x) {
+          if (x.key == t && x.low == tl) f(~uint32_t(j));
+        });
+      }));
+  }
+  auto stays = [&](const Rank& x, int j) { return x.key > t || (x.key == t && (x.low > tl || (x.low == tl && j <= ts))); };
   int32_t *hole = lists, *from = lists + kInline;
   if (!here) {
     hole = a.moves + int64_t(bh) * 2 * a.most;
     from = hole + a.most;
   }
   constexpr int kU = PT ? PT : 16;  // rounds of NT entries ranked together
-  int holes = 0, rows = 0, levels = 0;
+  int holes = 0, rows = 0;
   for (int j0 = 0; j0 < n; j0 += kU * NT) {
     Rank x[kU];
+    uint32_t keep = 0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       const int j = j0 + u * NT + tid;
@@ -610,27 +660,8 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
         x[u] = r[u];
       else
         x[u] = rank_at(j);
+      keep |= uint32_t(j < n && stays(x[u], j)) << u;
     }
-    __syncthreads();
-    // the ranks of the entries level with the threshold (entry order)
-    uint32_t keep = 0;
-    if (split) {
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const uint64_t m = __ballot(j0 + u * NT + tid < n && level(x[u]));
-        if (lane == 0) cnt[u * (NT / 64) + w] = __popcll(m);
-      }
-      prefix_counts<NT, kU>(cnt);
-    }
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const bool in = j0 + u * NT + tid < n, lv = in && level(x[u]);
-      const uint64_t m = __ballot(lv);
-      bool k = in && above(x[u]);
-      if (split && lv) k = levels + int(cnt[u * (NT / 64) + w]) + lanes_before(m) < equal;
-      if (k) keep |= 1u << u;
-    }
-    if (split) levels += int(cnt[kU * (NT / 64)]);
     __syncthreads();
     // holes below the budget and kept rows behind it
 #pragma unroll

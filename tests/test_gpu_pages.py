@@ -414,6 +414,34 @@ def test_evict_the_same_position_twice(over):
     evict_case(BF16, 64, 1, 2, 16, [200 + over], 200, 10, 30, spoil=twins)
 
 
+@pytest.mark.parametrize("n_sink,recent", [(300, 0), (0, 200), (3, 10)])
+@pytest.mark.parametrize("lens,budget", [([201], 200), ([240], 200), ([5000], 4999), ([5000], 4000), ([17001], 17000), ([17001], 300)],
+                         ids=str)
+def test_evict_more_protected_entries_than_stay(lens, budget, n_sink, recent):
+    """Positions that occur many times, all protected: then the scores decide among them too."""
+    def spoil(t, lens):
+        p, r = ref.entries(t, 0, lens[0])
+        t["pos"][p, :, r] = torch.where(torch.arange(lens[0])[:, None] % 50 == 7, 1000, 5 if n_sink > 5 else 2000).to(torch.int32).expand(-1, 2)
+        t["score"][p[::3], :, r[::3]] = 0.5
+    evict_case(BF16, 64, 1, 2, 16, lens, budget, min(recent, budget - min(n_sink, budget)), min(n_sink, budget), spoil=spoil)
+
+
+def test_evict_again_what_was_not_shortened():
+    """A second call on the same lengths meets entries that were moved and still lie behind the budget: each position twice."""
+    t = ref.make_pages(1, 2, 64, 16, 30, BF16, 12)
+    g = torch.Generator().manual_seed(12)
+    p, r = ref.entries(t, 0, 400)
+    for h in range(2):
+        t["pos"][p, h, r] = torch.cat([torch.randperm(300, generator=g), torch.arange(300, 400)]).to(torch.int32)
+    gt = on_gpu(t)
+    pages = pages_of(gt, 2)
+    lens = torch.tensor([400], dtype=torch.int32, device="cuda:0")
+    for _ in range(3):
+        t = ref.evict_ref(t, [400], 300, 250, 4)
+        pages.d2o_pages_evict(lens, 300, 250, 4)
+        same(gt, t)
+
+
 @pytest.mark.parametrize("over", [1, 50])
 def test_evict_scores_that_are_not_finite_and_any_positions(over):
     def spoil(t, lens):
