@@ -70,6 +70,16 @@ __device__ __forceinline__ void clear_bins(SelectShared& sh) {
   __syncthreads();
 }
 
+// One of a bin for every active lane; lanes that all have the same bin (scores that are all zero, or equal) add once.
+__device__ __forceinline__ void count_bin(int* hist, int bin) {
+  const int first = __builtin_amdgcn_readfirstlane(bin);
+  const uint64_t all = __ballot(true);
+  if (__ballot(bin == first) != all)
+    atomicAdd(&hist[bin], 1);
+  else if (__builtin_amdgcn_mbcnt_hi(uint32_t(all >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(all), 0)) == 0)
+    atomicAdd(&hist[bin], __popcll(all));
+}
+
 // The `want`-th largest of the 32-bit values that `each_value(f)` hands to f(value) on all threads together; `equal` becomes how many of
 // those equal to it are wanted, `same` how many there are.  FIRST = 1: values of 21 bits.
 template <int NT, int FIRST = 0, typename F>
@@ -82,7 +92,7 @@ __device__ __forceinline__ uint32_t nth_largest(SelectShared& sh, int want, int&
     clear_bins<NT>(sh);
     each_value([&](uint32_t v) {
       const bool in = pass == 0 || (v >> (pass == 1 ? 21 : 10)) == (prefix >> (pass == 1 ? 21 : 10));
-      if (in) atomicAdd(&sh.hist[(v >> shift) & digit], 1);
+      if (in) count_bin(sh.hist, int((v >> shift) & digit));
     });
     pick_bin<NT>(sh, want);
     prefix |= uint32_t(sh.bin) << shift;
@@ -207,7 +217,7 @@ __global__ __launch_bounds__(kSliceThreads) void fill_hist(FillArgs a) {
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < kSlicePer; ++u)
-    if (j0 + u * kSliceThreads + tid < n) atomicAdd(&hist[key[u] >> 21], 1);
+    if (j0 + u * kSliceThreads + tid < n) count_bin(hist, int(key[u] >> 21));
   __syncthreads();
   uint32_t* out = reinterpret_cast<uint32_t*>(a.hist + (int64_t(bh) * a.slices + blockIdx.x) * kBins);
   for (int i = tid; i < kBins / 2; i += kSliceThreads) out[i] = uint32_t(hist[2 * i]) | uint32_t(hist[2 * i + 1]) << 16;
