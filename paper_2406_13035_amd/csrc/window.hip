@@ -197,27 +197,31 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int64_t vt0 = (int64_t(b) * Hkv + hk) * a.tiles;
   const uint16_t* vtbase = a.vt + vt0 * D * 64;
   const float* rec = a.rec + vt0 * kRec;
-  // A tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB.  The tile's start is the same
-  // for all lanes, a lane's displacement in it (32 bits) changes at the prompt's end only.
+  // A tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB.  Through buffer descriptors: rows
+  // behind the prompt's end read as zero, a lane's displacement never changes, and the compiler lets the LDS reads of the products
+  // return one by one while such loads are on their way (behind global_load_lds, which counts as a flat access, it waits for all).
   constexpr int kRowsK = 512 / D, kLoadsK = 64 / kRowsK / NW, kLoadsV = D / 8 / NW;  // rows per instruction, instructions per wavefront
-  const uint32_t k_row = uint32_t(a.k.sn);
-  auto load_k = [&](int t) __attribute__((always_inline)) {
-    const int k0 = tl.tile(t) * 64, last = n - 1 - k0;
-    const uint16_t* src = kbase + int64_t(k0) * a.k.sn;
+  uint32_t k_off[kLoadsK], v_off[kLoadsV];
 #pragma unroll
-    for (int i = 0; i < kLoadsK; ++i) {
-      const int lr = (ws * kLoadsK + i) * kRowsK + lane / (D / 8), row = (lr & 32) | perm_key(lr & 31);
-      const int sw = D == 128 ? swz(lane & 15, lr & 3) : swz(lane & 7, (lr >> 1) & 3);
-      load_lds16(src + (uint32_t(min(row, last)) * k_row + sw), Ks + (t & 1) * kElems + (ws * kLoadsK + i) * kGroupLd);
-    }
+  for (int i = 0; i < kLoadsK; ++i) {
+    const int lr = (ws * kLoadsK + i) * kRowsK + lane / (D / 8), row = (lr & 32) | perm_key(lr & 31);
+    k_off[i] = 2 * (uint32_t(row) * uint32_t(a.k.sn) + (D == 128 ? swz(lane & 15, lr & 3) : swz(lane & 7, (lr >> 1) & 3)));
+  }
+#pragma unroll
+  for (int i = 0; i < kLoadsV; ++i) {
+    const int row = (ws * kLoadsV + i) * 8 + (lane >> 3);
+    v_off[i] = 2 * uint32_t(row * 64 + swz(lane & 7, (row >> 1) & 3));
+  }
+  auto load_k = [&](int t) __attribute__((always_inline)) {
+    const int k0 = tl.tile(t) * 64, last = min(63, n - 1 - k0);
+    const auto src = buffer_of(kbase + int64_t(k0) * a.k.sn, 2 * (uint32_t(last) * uint32_t(a.k.sn) + D));
+#pragma unroll
+    for (int i = 0; i < kLoadsK; ++i) load_lds16(src, k_off[i], Ks + (t & 1) * kElems + (ws * kLoadsK + i) * kGroupLd);
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
-    const uint16_t* src = vtbase + int64_t(tl.tile(t)) * (D * 64);
+    const auto src = buffer_of(vtbase + int64_t(tl.tile(t)) * (D * 64), D * 128);
 #pragma unroll
-    for (int i = 0; i < kLoadsV; ++i) {
-      const int row = (ws * kLoadsV + i) * 8 + (lane >> 3);
-      load_lds16(src + uint32_t(row * 64 + swz(lane & 7, (row >> 1) & 3)), Vs + (t & 1) * kElems + (ws * kLoadsV + i) * kGroupLd);
-    }
+    for (int i = 0; i < kLoadsV; ++i) load_lds16(src, v_off[i], Vs + (t & 1) * kElems + (ws * kLoadsV + i) * kGroupLd);
   };
   const int wr0 = r0 + w * 32, q_row = wr0 + m;
   bf16x8 bq[kKS];
