@@ -623,17 +623,24 @@ void launch_step(StepArgs& a, int batch, int D, hipStream_t s) {
   else launch_step<T, CT, 128>(a, batch, s);
 }
 
-int step_splits(int64_t bh, int max_len) {
-  const int64_t tiles = (int64_t(max_len) + kTile - 1) / kTile;
-  const int64_t want = std::max<int64_t>(1, 1024 / bh);
-  return int(std::max<int64_t>(1, std::min<int64_t>(want, tiles / (2 * kWaves))));
+// Shares per head, for at most `tiles` tiles each: workgroups of 64 tiles, about four per CU (a workgroup's ends cost as much as a dozen
+// tiles: 128 heads of 258 tiles of 8-bit rows 36 us in eight shares, 30 in four), but for two per CU shares as small as two rounds of a workgroup.
+int step_splits(int64_t bh, int64_t tiles) {
+  const int64_t large = std::min<int64_t>(1024 / bh, tiles / 64), small = std::min<int64_t>(512 / bh, tiles / (2 * kWaves));
+  return int(std::max<int64_t>(1, std::max(large, small)));
+}
+// Tiles that a sequence of max_len entries shows at most.
+int64_t most_tiles(const d2o_pages* p, int32_t max_len, int32_t window, int32_t n_sink) {
+  const int64_t all = (int64_t(max_len) + kTile - 1) / kTile;
+  if (window == 0 || p->pos) return all;
+  return std::min(all, (int64_t(window) + n_sink) / kTile + 3);
 }
 
 }  // namespace
 
 size_t pages_step_bytes(const d2o_pages* p, int32_t max_len) {
   const size_t bh = size_t(p->batch) * p->n_kv_heads, hq = size_t(p->batch) * p->n_q_heads, pad = (size_t(max_len) + kTile - 1) / kTile * kTile;
-  const size_t splits = step_splits(bh, max_len);
+  const size_t splits = step_splits(bh, most_tiles(p, max_len, 0, 0));  // (a window has no more tiles, so no more shares)
   return round256(p->score ? hq * pad * sizeof(float) : 0) + round256(hq * splits * p->head_dim * sizeof(float)) +
          round256(hq * splits * 2 * sizeof(float));
 }
@@ -673,7 +680,7 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads, hq = int64_t(pages->batch) * pages->n_q_heads;
   if (bh > 65535 || bh * ((max_len + kFinishEntries - 1) / kFinishEntries) > 0x3FFFFFFF) return D2O_ERR_UNSUPPORTED;
   a.pad = (max_len + kTile - 1) / kTile * kTile;
-  a.splits = step_splits(bh, max_len);
+  a.splits = step_splits(bh, most_tiles(pages, max_len, window, n_sink));
   char* ws = static_cast<char*>(workspace);
   a.logits = reinterpret_cast<float*>(ws);
   ws += round256(pages->score ? size_t(hq) * a.pad * sizeof(float) : 0);
