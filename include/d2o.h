@@ -332,7 +332,7 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * O = softmax(Q K^T / sqrt(d)) V over those.  window = 0: no window (every j <= i).
  * Q, O: [B][Hq][n][d]; K, V: [B][Hkv][n][d]; O in `dtype`.  lens: device [B], the tokens of each sequence
  * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
- * its keys behind the end are never looked at.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
+ * its keys behind the end take no part.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
  * INVALID_ARG, UNSUPPORTED (also a row stride of K of 2^24 elements or more), CAPACITY (workspace smaller than
  * d2o_window_workspace_bytes says; where it says 0, NULL will do), HIP. */
 int d2o_window_workspace_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
@@ -343,8 +343,8 @@ int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_
 
 /* A cache in pages.  Entry s of sequence b is row s % page_size of page page_table[b][s / page_size], for every
  * KV head.  A page id outside [0, n_pages) stands for no page: entries there are as if absent (never attended to, written
- * or moved; evictions rank them below all others).  A page that a call writes must belong to one sequence; pages that are
- * only attended to, with no scores, may be shared. */
+ * or moved; evictions rank them below all others).  A page that a call writes (rows, scores, positions) must stand once in one
+ * sequence's row of the table; pages that are only attended to, with no scores kept, may be shared. */
 typedef struct {
   int32_t batch;       /* B: sequences, rows of page_table                                  */
   int32_t n_q_heads;   /* Hq, a multiple of n_kv_heads with Hq / Hkv <= 16                  */

@@ -439,6 +439,12 @@ def _vector_ok(t, shape, dtype, device, what):
     _tensor_ok(t, shape, dtype, device, what, whole=True)
 
 
+def _int32_ok(*values):
+    for v in values:
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise D2OError(f"{v} does not fit 32 bits")
+
+
 def _public_stream(index):
     return torch.cuda.current_stream(index).cuda_stream
 
@@ -473,6 +479,7 @@ def d2o_window_attend(Q, K, V, window: int = 0, n_sink: int = 0, lens=None, O=No
         O = torch.empty(Q.shape, dtype=dt, device=dev) if lens is None else torch.zeros(Q.shape, dtype=dt, device=dev)
     else:
         _tensor_ok(O, Q.shape, dt, dev, "O")
+    _int32_ok(window, n_sink)
     code, need = _DTYPE_CODES[dt], C.c_size_t()
     _ok(lib.d2o_window_workspace_bytes(B, n, Hkv, d, code, C.byref(need)), "d2o_window_workspace_bytes")
 
@@ -517,6 +524,7 @@ class Pages:
         self.tensors = (K, V, page_table, K_exp, V_exp, score, pos)
         self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = B, n_q_heads, Hkv, d
         self.max_len = max_pages * page_size if max_len is None else int(max_len)
+        _int32_ok(n_q_heads, self.max_len, n_pages)
         self.desc = d2o_pages(B, n_q_heads, Hkv, d, _DTYPE_CODES[self.dtype], 1 if fp8 else 0, page_size, n_pages,
                               max_pages, _view_of(K), _view_of(V), ptr(K_exp), ptr(V_exp), ptr(score), ptr(pos),
                               page_table.data_ptr())
@@ -541,6 +549,7 @@ class Pages:
         _tensor_ok(V, shape, self.dtype, self.device, "V")
         if score is not None:
             _vector_ok(score, shape[:3], torch.float32, self.device, "score")
+        _int32_ok(budget, recent, n_sink)
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_fill(
             self._ref, _view_of(K), _view_of(V), n, None if lens is None else self._lens(lens),
             None if score is None else score.data_ptr(), budget, recent, n_sink, *self._ws, stream)), "d2o_pages_fill")
@@ -556,6 +565,7 @@ class Pages:
         if k_new is not None:
             _tensor_ok(k_new, new, self.dtype, self.device, "k_new")
             _tensor_ok(v_new, new, self.dtype, self.device, "v_new")
+        _int32_ok(window, n_sink)
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_step(
             self._ref, _view_of(q, False), _NULL_VIEW if k_new is None else _view_of(k_new, False),
             _NULL_VIEW if v_new is None else _view_of(v_new, False), self._lens(lens),
@@ -564,6 +574,7 @@ class Pages:
 
     def d2o_pages_evict(self, lens, budget, recent=0, n_sink=0):
         """Every head of a sequence with more than `budget` entries goes back to that many, in place."""
+        _int32_ok(budget, recent, n_sink)
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_evict(
             self._ref, self._lens(lens), self._bound, budget, recent, n_sink, *self._ws, stream)), "d2o_pages_evict")
 

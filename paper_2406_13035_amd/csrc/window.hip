@@ -19,7 +19,7 @@ constexpr float kFloor = -1e30f;  // exponent reference before a row has seen a 
 struct WindowArgs {
   View q, k, v, o;
   const int32_t* lens;
-  int32_t n, Hq, G, window, n_sink;  // window: at least 1, INT32_MAX without one
+  int32_t n, Hq, G, window, n_sink;  // window and n_sink: at most n; window: at least 1
   // bf16: transposed values and a record per tile of 64 keys
   uint16_t* vt;  // [B][Hkv][tiles][D][64] fp16, every group of eight keys scaled by a power of two of its own
   float* rec;    // [B][Hkv][tiles][kRec]: exponents of the groups (of the even ones, then of the odd ones), a flag
@@ -176,12 +176,11 @@ constexpr int tile_elems() { return D / 8 * kGroupLd; }  // a tile of K, and of 
 // NW wavefronts of 32 query rows.  K and V^T tiles are double-buffered in LDS, filled straight from memory; the two halves of the
 // wavefronts run half a tile apart, one forming its probabilities on the vector ALU while the other runs P V of its tile and
 // Q K^T of the next on the matrix core.
-template <int D, int NW>
+// SPLIT: the two halves own the same rows and take the tiles in turn, each with buffers of its own, and join their softmaxes at the end.
+template <int D, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_bf16(WindowArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
-  constexpr int kElems = tile_elems<D>(), kDC = D / 32, kKS = D / 16, BM = 32 * NW;
-  uint16_t* Ks = smem;               // [2][kElems]
-  uint16_t* Vs = smem + 2 * kElems;  // [2][kElems]
+  constexpr int kElems = tile_elems<D>(), kDC = D / 32, kKS = D / 16, kRW = SPLIT ? NW / 2 : NW, BM = 32 * kRW;  // kRW: wavefronts that share a tile's loads
   const int Hkv = a.Hq / a.G;
   int blk, hz;
   place(a, gridDim.x / a.blocks, blk, hz);
@@ -189,10 +188,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
   const int r0 = blk * BM;
   if (r0 >= n) return;
-  const int tid = threadIdx.x, w = tid >> 6, ws = __builtin_amdgcn_readfirstlane(w), lane = tid & 63, m = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, w = tid >> 6, half = SPLIT ? w / kRW : 0, ws = __builtin_amdgcn_readfirstlane(w % kRW), lane = tid & 63, m = lane & 31, h = lane >> 5;
   const float scale2 = kLog2e / sqrtf(float(D));
   const Tiles tl(a, r0, min(r0 + BM, n) - 1, 64);
-  const int ntile = tl.count;
+  const int ntile = SPLIT ? (tl.count - half + 1) / 2 : tl.count, rounds = SPLIT ? (tl.count + 1) / 2 : tl.count;  // of this half, of both
+  auto tile_of = [&](int t) __attribute__((always_inline)) { return tl.tile(SPLIT ? 2 * t + half : t); };
+  uint16_t* Ks = smem + __builtin_amdgcn_readfirstlane(half) * 4 * kElems;  // [2][kElems]
+  uint16_t* Vs = Ks + 2 * kElems;                                           // [2][kElems]
   const uint16_t* kbase = static_cast<const uint16_t*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
   const int64_t vt0 = (int64_t(b) * Hkv + hk) * a.tiles;
   const uint16_t* vtbase = a.vt + vt0 * D * 64;
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // A tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB.  Through buffer descriptors: rows
   // behind the prompt's end read as zero, a lane's displacement never changes, and the compiler lets the LDS reads of the products
   // return one by one while such loads are on their way (behind global_load_lds, which counts as a flat access, it waits for all).
-  constexpr int kRowsK = 512 / D, kLoadsK = 64 / kRowsK / NW, kLoadsV = D / 8 / NW;  // rows per instruction, instructions per wavefront
+  constexpr int kRowsK = 512 / D, kLoadsK = 64 / kRowsK / kRW, kLoadsV = D / 8 / kRW;  // rows per instruction, instructions per wavefront
   uint32_t k_off[kLoadsK], v_off[kLoadsV];
 #pragma unroll
   for (int i = 0; i < kLoadsK; ++i) {
@@ -213,30 +215,35 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     v_off[i] = 2 * uint32_t(row * 64 + swz(lane & 7, (row >> 1) & 3));
   }
   auto load_k = [&](int t) __attribute__((always_inline)) {
-    const int k0 = tl.tile(t) * 64, last = min(63, n - 1 - k0);
+    const int k0 = __builtin_amdgcn_readfirstlane(tile_of(t)) * 64, last = min(63, n - 1 - k0);
     const auto src = buffer_of(kbase + int64_t(k0) * a.k.sn, 2 * (uint32_t(last) * uint32_t(a.k.sn) + D));
 #pragma unroll
     for (int i = 0; i < kLoadsK; ++i) load_lds16(src, k_off[i], Ks + (t & 1) * kElems + (ws * kLoadsK + i) * kGroupLd);
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
-    const auto src = buffer_of(vtbase + int64_t(tl.tile(t)) * (D * 64), D * 128);
+    const auto src = buffer_of(vtbase + int64_t(tile_of(t)) * (D * 64), D * 128);
 #pragma unroll
     for (int i = 0; i < kLoadsV; ++i) load_lds16(src, v_off[i], Vs + (t & 1) * kElems + (ws * kLoadsV + i) * kGroupLd);
   };
-  const int wr0 = r0 + w * 32, q_row = wr0 + m;
+  const int wr0 = r0 + w % kRW * 32, q_row = wr0 + m;
   bf16x8 bq[kKS];
-  load_k(0);
+  if (!SPLIT || ntile > 0) load_k(0);
   {
     const uint16_t* qp = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh + int64_t(min(q_row, n - 1)) * a.q.sn;
 #pragma unroll
     for (int ks = 0; ks < kKS; ++ks) bq[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16 + h * 8);
   }
-  load_v(0);
+  if (!SPLIT || ntile > 0) load_v(0);
   if (ntile > 1) load_k(1);
-  auto exps_of = [&](int t) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(rec + int64_t(tl.tile(t)) * kRec + h * 4); };
-  auto flag_of = [&](int t) __attribute__((always_inline)) { return rec[int64_t(tl.tile(t)) * kRec + 8]; };
-  f32x4 ex = exps_of(0), ex_next = ex;
-  float flag = 0.f, flag_next = flag_of(0);
+  auto exps_of = [&](int t) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(rec + int64_t(tile_of(t)) * kRec + h * 4); };
+  auto flag_of = [&](int t) __attribute__((always_inline)) { return rec[int64_t(tile_of(t)) * kRec + 8]; };
+  f32x4 ex = {0.f, 0.f, 0.f, 0.f}, ex_next;
+  float flag = 0.f, flag_next = 0.f;
+  if (!SPLIT || ntile > 0) {
+    ex = exps_of(0);
+    flag_next = flag_of(0);
+  }
+  ex_next = ex;
 
   f32x16 o[kDC];
 #pragma unroll
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   f32x16 s[2];
   f16x8 pb[2][2];
   auto active = [&](int t) __attribute__((always_inline)) {
-    const int k0 = tl.tile(t) * 64;
+    const int k0 = tile_of(t) * 64;
     return any_seen(a, wr0, wr0 + 31, k0, k0 + 63);
   };
   // probabilities of one group of eight registers (sub-tile st, half kb) with exponent reference c
@@ -263,7 +270,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     return sum;
   };
   auto softmax = [&](int t) __attribute__((always_inline)) {
-    const int k0 = tl.tile(t) * 64;
+    const int k0 = tile_of(t) * 64;
     if (!all_seen(a, wr0, wr0 + 31, k0, k0 + 63)) {
       // register r of sub-tile st holds key `first` + 32 st + 16 (r / 8) + r % 8
       const int first = k0 + h * 8, last = q_row - first, gone = q_row - a.window - first, sinks = a.n_sink - first;
@@ -384,13 +391,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     __builtin_amdgcn_s_setprio(0);
   };
 
-  const bool late = w >= NW / 2;
+  const bool late = w >= NW / 2;  // (SPLIT: the second half)
 #pragma unroll
   for (int ks = 0; ks < kKS; ++ks) asm volatile("" ::"v"(bq[ks]));  // the queries have arrived
   wait_vm<0>();
   __syncthreads();
   bool now = false;
-  for (int t = -1; t < ntile; ++t) {
+  for (int t = -1; t < rounds; ++t) {
     const bool more = t + 1 < ntile, next = more && active(t + 1);
     if (t >= 0) {  // K(t) and V(t - 1) were last read before this iteration: their buffers take K(t + 2) and V(t + 1)
       if (t + 2 < ntile) load_k(t + 2);
@@ -409,11 +416,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     flag = fmaxf(flag, flag_next);
     __syncthreads();
   }
+  if constexpr (SPLIT) {
+    // the second half's rows to LDS (the tiles are done with), the first half adds them to its own
+    float* os = reinterpret_cast<float*>(smem) + ws * (kDC * 16 + 4) * 64 + lane;
+    if (half) {
+      each<kDC>([&](auto dc) { each<16>([&](auto r) { os[(dc * 16 + r) * 64] = o[dc][decltype(r)::value]; }); });
+      os[kDC * 16 * 64] = mrun;
+      os[(kDC * 16 + 1) * 64] = el;
+      os[(kDC * 16 + 2) * 64] = lsum;
+      os[(kDC * 16 + 3) * 64] = flag;
+    }
+    __syncthreads();
+    if (half) return;
+    const float m1 = os[kDC * 16 * 64], el1 = os[(kDC * 16 + 1) * 64], l1 = os[(kDC * 16 + 2) * 64];
+    flag = fmaxf(flag, os[(kDC * 16 + 3) * 64]);
+    const float M = fmaxf(mrun, m1), E = mrun >= m1 ? el : el1;
+    const float f0 = __builtin_amdgcn_exp2f(mrun - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
+    lsum = lsum * __builtin_amdgcn_exp2f((mrun - M) - (el - E)) + l1 * __builtin_amdgcn_exp2f((m1 - M) - (el1 - E));
+    el = E;
+    each<kDC>([&](auto dc) {
+      each<16>([&](auto r) { o[dc][decltype(r)::value] = o[dc][decltype(r)::value] * f0 + os[(dc * 16 + r) * 64] * f1; });
+    });
+  }
   if (flag != 0.f) {
     // infinities and NaN of V, which counted as zero above: a row that sees one takes it as it is, whatever its weight
     const uint16_t* vsrc = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
-    for (int t = 0; t < ntile; ++t) {
-      if (flag_of(t) == 0.f) continue;
+    for (int t = 0; t < tl.count; ++t) {
+      if (rec[int64_t(tl.tile(t)) * kRec + 8] == 0.f) continue;
       const int k0 = tl.tile(t) * 64;
       for (int j = k0; j < min(k0 + 64, n); ++j) {
         if (!sees(a, q_row, j)) continue;
@@ -703,15 +732,16 @@ size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_d
   return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * kRec * sizeof(float);
 }
 
-template <int D, int NW>
+template <int D, int NW, bool SPLIT>
 hipError_t run_bf16(WindowArgs& a, int batch, hipStream_t s) {
-  a.blocks = (a.n + 32 * NW - 1) / (32 * NW);
-  constexpr int kSmem = 4 * tile_elems<D>() * int(sizeof(uint16_t));
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW>),
+  constexpr int BM = 32 * (SPLIT ? NW / 2 : NW), kSmem = (SPLIT ? 8 : 4) * tile_elems<D>() * int(sizeof(uint16_t));
+  static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 4) * 64 * int(sizeof(float)), "the second half's rows");
+  a.blocks = (a.n + BM - 1) / BM;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW, SPLIT>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != hipSuccess) return e;
   window_values<D><<<dim3(a.tiles, batch * (a.Hq / a.G)), 256, 0, s>>>(a);
-  window_bf16<D, NW><<<dim3(unsigned(a.blocks) * batch * a.Hq), 64 * NW, kSmem, s>>>(a);
+  window_bf16<D, NW, SPLIT><<<dim3(unsigned(a.blocks) * batch * a.Hq), 64 * NW, kSmem, s>>>(a);
   return hipGetLastError();
 }
 
@@ -752,20 +782,22 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   a.n = n;
   a.Hq = n_q_heads;
   a.G = n_q_heads / n_kv_heads;
-  a.window = window ? window : INT32_MAX;
-  a.n_sink = n_sink;
+  a.window = window == 0 || window > n ? n : window;
+  a.n_sink = std::min(n_sink, n);
   a.tiles = (n + 63) / 64;
   a.reverse = a.window > n / 2;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == D2O_BF16) {
     a.vt = static_cast<uint16_t*>(workspace);
     a.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + values_bytes(batch, n, n_kv_heads, head_dim));
-    const bool few = int64_t((n + 127) / 128) * n_q_heads * batch <= 512;
+    // Blocks of 256 rows, one workgroup per CU; of 128 where two per CU hold all of them; where one per CU does, with the
+    // tiles split over two halves of a workgroup.
+    const int64_t blocks = int64_t((n + 127) / 128) * n_q_heads * batch;
     hipError_t e;
     if (head_dim == 64)
-      e = few ? run_bf16<64, 4>(a, batch, s) : run_bf16<64, 8>(a, batch, s);
+      e = blocks <= 256 ? run_bf16<64, 8, true>(a, batch, s) : blocks <= 512 ? run_bf16<64, 4, false>(a, batch, s) : run_bf16<64, 8, false>(a, batch, s);
     else
-      e = few ? run_bf16<128, 4>(a, batch, s) : run_bf16<128, 8>(a, batch, s);
+      e = blocks <= 256 ? run_bf16<128, 8, true>(a, batch, s) : blocks <= 512 ? run_bf16<128, 4, false>(a, batch, s) : run_bf16<128, 8, false>(a, batch, s);
     return e == hipSuccess ? D2O_OK : D2O_ERR_HIP;
   }
   const int64_t heads = int64_t(batch) * n_q_heads;

@@ -479,6 +479,36 @@ def test_evict_rows_by_token_and_lengths_beyond_max_len():
     same(gt, want)
 
 
+@pytest.mark.parametrize("page", [16, 4])
+def test_pools_beyond_32_bits(page):
+    """A pool of 9 GiB of which a few pages at its end are in use: prompts, a step and an eviction."""
+    Hkv, d, per = 2, 128, -(-80 // page)
+    n_pages = (9 << 30) // (2 * page * Hkv * d)
+    t = ref.make_pages(1, Hkv, d, page, per, BF16, 21, spare=0)
+    g = torch.Generator().manual_seed(21)
+    K, V = (torch.randn((1, Hkv, 100, d), generator=g).to(BF16) for _ in range(2))
+    sc = torch.rand((1, Hkv, 100), generator=g)
+    q, kn, vn = (torch.randn((1, h, d), generator=g).to(BF16) for h in (4, 2, 2))
+    lens = torch.tensor([71], dtype=torch.int32)
+    at = torch.tensor([100], dtype=torch.int32)
+    big = {}
+    for x in ("k", "v", "score", "pos"):
+        big[x] = torch.empty((n_pages,) + t[x].shape[1:], dtype=t[x].dtype, device="cuda:0")
+        big[x][n_pages - per:] = t[x].cuda()
+    table = (t["table"] + (n_pages - per)).cuda()
+    p = binding.Pages(big["k"], big["v"], table, 4, score=big["score"], pos=big["pos"], max_len=100)
+    p.d2o_pages_fill(*cuda(K, V), 70, 20, 2, score=sc.cuda())
+    t = ref.fill_ref(t, K, V, [100], sc, 70, 20, 2)
+    want, tol, t, add, add_tol = ref.step_ref(t, q, kn, vn, lens, at, 0, 0, 80, BF16)
+    out = torch.zeros((1, 4, d), dtype=BF16, device="cuda:0")
+    p.d2o_pages_step(*cuda(q, kn, vn, lens), out, positions=at.cuda())
+    assert bool(((out.cpu().double() - want).abs() <= tol).all())
+    t["score"] = big["score"][n_pages - per:].cpu()
+    p.d2o_pages_evict(lens.cuda(), 60, 20, 2)
+    t = ref.evict_ref(t, [71], 60, 20, 2)
+    same({x: (None if t[x] is None else big[x][n_pages - per:]) for x in TENSORS}, t)
+
+
 # ---- as they are used together --------------------------------------------------------------
 
 def test_wrong_arguments_are_refused():
@@ -513,6 +543,8 @@ def test_wrong_arguments_are_refused():
         lambda: p.d2o_pages_fill(torch.zeros((2, 2, 100, 64), dtype=BF16, device="cuda:0"),
                                  torch.zeros((2, 2, 100, 64), dtype=BF16, device="cuda:0"), 100),
         lambda: p.d2o_pages_evict(lens, 0),
+        lambda: p.d2o_pages_evict(lens, (1 << 32) + 2),
+        lambda: p.d2o_pages_step(q, kn, kn, lens, q, window=1 << 32),
         lambda: p.d2o_pages_evict(lens, 10, 9, 2),
         lambda: bare.d2o_pages_evict(lens, 10),
     ]

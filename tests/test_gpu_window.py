@@ -199,6 +199,39 @@ def test_captured_and_replayed(dtype):
         assert torch.equal(O, want) and bool((O[:, :, :m] != 0).any())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_the_largest_window_and_number_of_first_tokens(dtype):
+    Q, K, V = inputs(dtype, 1, 2, 1, 200, 64)
+    want = run(Q, K, V, 0, 0)
+    check(Q, K, V, want, 0, 0)
+    for window, n_sink in ((0x7FFFFFFF, 0), (200, 5), (0x7FFFFFFF, 0x7FFFFFFF)):
+        assert torch.equal(run(Q, K, V, window, n_sink), want)
+    # every token a first one: the window adds nothing (the order of the sums may differ)
+    check(Q, K, V, run(Q, K, V, 1, 0x7FFFFFFF), 1, 0x7FFFFFFF)
+
+
+@pytest.mark.parametrize("n,heads", [(150, 4), (150, 300)], ids=["few", "many"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_offsets_beyond_32_bits(dtype, n, heads):
+    """Rows millions of elements apart: the last ones lie more than 4 GiB behind the first."""
+    d, step = 64, (1 << 24) - 64
+    Q, K, V = inputs(dtype, 1, heads, heads, n, d)
+    big = torch.empty(step * n + 2 * heads * d, dtype=dtype, device="cuda:0")
+    k, v = (big.as_strided((1, heads, n, d), (0, d, step, 1), at) for at in (0, heads * d))
+    k.copy_(K), v.copy_(V)
+    O = binding.d2o_window_attend(Q.cuda(), k, v, 60, 3)
+    assert torch.equal(O.cpu(), run(Q, K, V, 60, 3))
+    with pytest.raises(binding.D2OError):
+        binding.d2o_window_attend(Q[:, :, 1:].cuda(), big.as_strided((1, heads, n - 1, d), (0, d, 1 << 24, 1)), v[:, :, 1:], 60, 3)
+
+
+def test_output_in_the_place_of_the_queries():
+    for dtype in (F32, BF16):
+        Q, K, V = (x.cuda() for x in inputs(dtype, 1, 4, 2, 700, 64))
+        want = binding.d2o_window_attend(Q, K, V, 90, 2)
+        assert binding.d2o_window_attend(Q, K, V, 90, 2, O=Q) is Q and torch.equal(Q, want)
+
+
 def test_wrong_arguments_are_refused():
     Q, K, V = (x.cuda() for x in inputs(BF16, 2, 4, 2, 10, 64))
     bad = [
@@ -208,6 +241,7 @@ def test_wrong_arguments_are_refused():
         lambda: binding.d2o_window_attend(Q, K[:, :1].expand(2, 3, 10, 64), V[:, :1].expand(2, 3, 10, 64), 4),
         lambda: binding.d2o_window_attend(Q, K, V, -1),
         lambda: binding.d2o_window_attend(Q, K, V, 4, -1),
+        lambda: binding.d2o_window_attend(Q, K, V, 1 << 32),
         lambda: binding.d2o_window_attend(Q, K, V, 4, lens=torch.tensor([1, 2], device="cuda:0")),
         lambda: binding.d2o_window_attend(Q, K, V, 4, O=torch.empty(2, 4, 10, 64, device="cuda:0")),
         lambda: binding.d2o_window_attend(Q[..., :32], K[..., :32], V[..., :32], 4),
