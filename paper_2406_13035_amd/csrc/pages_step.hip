@@ -134,7 +134,7 @@ struct Rows<uint16_t, D> {
     for (int i = 0; i < kK; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i]), q[i], s, 0, 0, 0);
     return s;
   }
-  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return reinterpret_cast<const VReg*>(row)[c]; }
+  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return __builtin_nontemporal_load(reinterpret_cast<const VReg*>(row) + c); }
   static __device__ __forceinline__ int column(int c, int e) { return c * kE + e; }
   static __device__ __forceinline__ void values(const VReg& v, float, float* f) {
 #pragma unroll
@@ -168,7 +168,7 @@ struct Rows<float, D> {
   static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) {
     VReg v;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) v.x[i] = reinterpret_cast<const f32x4*>(row)[i * 16 + c];
+    for (int i = 0; i < D / 64; ++i) v.x[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row) + i * 16 + c);
     return v;
   }
   static __device__ __forceinline__ int column(int c, int e) { return (e / 4) * 64 + c * 4 + e % 4; }
@@ -204,7 +204,7 @@ struct Rows<uint8_t, D> {
     }
     return s;
   }
-  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return reinterpret_cast<const VReg*>(row)[c]; }
+  static __device__ __forceinline__ VReg load_v(const uint8_t* row, int c) { return __builtin_nontemporal_load(reinterpret_cast<const VReg*>(row) + c); }
   static __device__ __forceinline__ int column(int c, int e) { return c * kE + e; }
   static __device__ __forceinline__ void values(const VReg& v, float scale, float* f) {
 #pragma unroll
@@ -296,7 +296,8 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
 // its row by a register broadcast.  P V runs on the vector ALU in fp32 (a rounding of P would cost more bits than the products
 // save: the loads bound the kernel up to 16 heads per group).
 // WIDE: a tile lies in one page, whose number and address are the same for all lanes and live in scalar registers; a lane adds a
-// displacement of 32 bits that never changes.  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
+// displacement of 32 bits that never changes.  Rows of V are read once and past the caches (16 lanes take whole lines; 131072 entries
+// 104 -> 98 us), K's are not: an instruction takes half lines, and with the hint the other half came from memory again.  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
 // addresses as with sums: 8-bit rows 71 us where they take 30.)
 template <typename T, typename CT, int D, int GM, int U, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
