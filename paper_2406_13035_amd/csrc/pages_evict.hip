@@ -489,7 +489,7 @@ template <int NT, int PT>
 __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   __shared__ SelectShared sh;
   __shared__ uint32_t cnt[(PT ? PT : 16) * (NT / 64) + 1];
-  __shared__ int lists[2 * kInline];
+  __shared__ __attribute__((aligned(8))) int lists[2 * kInline];
   const int bh = blockIdx.x, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int n = min(a.lens[b], a.max_len), S = a.budget;
   const bool here = a.most <= kInline;
@@ -621,23 +621,21 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   constexpr int kFew = 256;
   static_assert(kFew <= NT && 2 * kFew <= 2 * kInline, "a thread and two words each");
   if (equal < same && same <= kFew) {
+    uint64_t* few = reinterpret_cast<uint64_t*>(lists);  // larger: kept before
     if (tid == 0) sh.bin = 0;
     __syncthreads();
     each_rank([&](int j, const Rank& x) {
-      if (x.key != t) return;
-      const int i = atomicAdd(&sh.bin, 1);
-      lists[i] = int(x.low);
-      lists[kFew + i] = j;
+      if (x.key == t) few[atomicAdd(&sh.bin, 1)] = uint64_t(x.low) << 32 | ~uint32_t(j);
     });
     __syncthreads();
     if (tid < same) {
-      const uint32_t low = lists[tid];
-      const int j = lists[kFew + tid];
+      const uint64_t mine = few[tid];
       int before = 0;
-      for (int i = 0; i < same; ++i) before += uint32_t(lists[i]) > low || (uint32_t(lists[i]) == low && lists[kFew + i] < j);
+#pragma unroll 8
+      for (int i = 0; i < same; ++i) before += few[i] > mine;
       if (before == equal - 1) {
-        sh.left = int(low);
-        sh.above = j;
+        sh.left = int(mine >> 32);
+        sh.above = int(~uint32_t(mine));
       }
     }
     __syncthreads();
