@@ -256,32 +256,41 @@ __device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int 
   }
 }
 
-// Adds the softmax rows of a (sequence, KV head) to the scores of entries i0, i0 + step, .. (in the order of the tiles) below `end`, N of them,
-// all loads on their way at once (Eq. 6); the group's query heads in rising order.  M and inv: maximum and reciprocal sum of each.
-template <int N>
+// Adds the softmax rows of a (sequence, KV head) to the scores of entries i0, i0 + step, .. (in the order of the tiles) below `end`, N of them
+// (Eq. 6); the group's query heads in rising order.  What is read - logits, pages, old scores - is on its way before `totals` forms M and
+// inv, maximum and reciprocal sum of each head.
+template <int N, int GM, typename F>
 __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& list, int b, int hk, int i0, int step, int end,
-                                           const float* M, const float* inv) {
+                                           const float* M, const float* inv, const F& totals) {
   const float* lg = a.logits + (int64_t(b) * a.Hq + hk * a.G) * a.pad;
   int s[N], page[N];
-  float add[N], old[N];
+  float x[GM][N], old[N];
   int64_t at[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int i = i0 + u * step;
     s[u] = i < end ? list.slot(i / kTile) + i % kTile : list.n;
     page[u] = s[u] < list.n ? a.pool.page_of(b, s[u]) : -1;
-    add[u] = 0.f;
   }
+#pragma unroll
+  for (int h = 0; h < GM; ++h)
+    if (h < a.G) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) x[h][u] = lg[int64_t(h) * a.pad + min(s[u], list.n - 1)];
+    }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     at[u] = page[u] >= 0 ? a.pool.at(page[u], hk, s[u]) : 0;
     old[u] = a.pool.score[at[u]];
   }
-  for (int h = 0; h < a.G; ++h) {
+  totals();
+  float add[N] = {};
 #pragma unroll
-    for (int u = 0; u < N; ++u)
-      add[u] += __builtin_amdgcn_exp2f(lg[int64_t(h) * a.pad + min(s[u], list.n - 1)] - M[h]) * inv[h];
-  }
+  for (int h = 0; h < GM; ++h)
+    if (h < a.G) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) add[u] += __builtin_amdgcn_exp2f(x[h][u] - M[h]) * inv[h];
+    }
   // (an entry that is not seen has logits of -infinity and gets nothing; NaN is added)
 #pragma unroll
   for (int u = 0; u < N; ++u)
@@ -297,10 +306,11 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
 // save: the loads bound the kernel up to 16 heads per group).
 // WIDE: a tile lies in one page, whose number and address are the same for all lanes and live in scalar registers; a lane adds a
 // displacement of 32 bits that never changes.  Rows of V are read once and past the caches (16 lanes take whole lines; 131072 entries
-// 104 -> 98 us), K's are not: an instruction takes half lines, and with the hint the other half came from memory again.  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
+// 104 -> 98 us), K's are not: an instruction takes half lines, and with the hint the other half came from memory again.  Two wavefronts per
+// SIMD at least (16 heads per group of bf16 rows: 84 -> 72 us, of fp32 rows, which would spill, 104 -> 140; three: 65 -> 71 us for four).  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
 // addresses as with sums: 8-bit rows 71 us where they take 30.)
 template <typename T, typename CT, int D, int GM, int U, bool WIDE>
-__global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM > 8 && sizeof(CT) == 4 ? 1 : 2))) void step_part(StepArgs a) {
   typedef Rows<CT, D> R;
   constexpr int E = R::kE;
   __shared__ float so[kWaves][GM][D];
@@ -527,13 +537,14 @@ __global__ __launch_bounds__(64 * kWaves) void step_part(StepArgs a) {
   }
   if (lg && single) {
     __syncthreads();
-    for (int i = tid; i < list.tiles * kTile; i += 64 * kWaves) add_scores<1>(a, list, b, hk, i, 0, list.tiles * kTile, sM, sinv);
+    for (int i = tid; i < list.tiles * kTile; i += 64 * kWaves)
+      add_scores<1, GM>(a, list, b, hk, i, 0, list.tiles * kTile, sM, sinv, [] {});
   }
 }
 
 // Joins the shares of the heads that have several: the first `joins` workgroups the outputs, one query head each, the others the scores.
 constexpr int kFinish = 256, kFinishEntries = 1024;  // threads; entries of a workgroup that adds scores
-template <typename T, int D>
+template <typename T, int D, int GM>
 __global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   // maximum and sum of a query head over the shares: a wavefront, a lane per share
@@ -575,23 +586,25 @@ __global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
   const TileList list(a, b, least);
   const int first = x % per * kFinishEntries, ns = list.shares();
   if (first >= list.tiles * kTile || ns <= 1) return;
-  for (int h = w; h < a.G; h += kFinish / 64) {
-    float M, L;
-    total(a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2, ns, M, L);
-    if (lane == 0) {
-      sM[h] = M;
-      sinv[h] = L == 0.f ? 0.f : 1.f / L;
+  const int end = min(first + kFinishEntries, list.tiles * kTile);
+  add_scores<kFinishEntries / kFinish, GM>(a, list, b, hk, first + tid, kFinish, end, sM, sinv, [&]() __attribute__((always_inline)) {
+    for (int h = w; h < a.G; h += kFinish / 64) {
+      float M, L;
+      total(a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2, ns, M, L);
+      if (lane == 0) {
+        sM[h] = M;
+        sinv[h] = L == 0.f ? 0.f : 1.f / L;
+      }
     }
-  }
-  __syncthreads();
-  add_scores<kFinishEntries / kFinish>(a, list, b, hk, first + tid, kFinish, min(first + kFinishEntries, list.tiles * kTile), sM, sinv);
+    __syncthreads();
+  });
 }
 
-// Tiles per wavefront and round: two, where their rows take 16 KB at most (8 KB where the outputs of 16 heads fill the registers).
+// Tiles per wavefront and round: two, where their rows take 16 KB at most and the outputs of 16 heads do not fill the registers.
 // (8-bit rows in fours: 39 instead of 36 us for 4 x 32 heads x 4100 entries; bf16 rows of 128 singly: 109 instead of 105 us for 8 heads of 131072.)
 template <typename CT, int D, int GM>
 constexpr int tiles_per_round() {
-  return (GM > 8 ? 8192 : 16384) / (kTile * 2 * D * int(sizeof(CT))) >= 2 ? 2 : 1;
+  return GM <= 8 && 2 * kTile * 2 * D * int(sizeof(CT)) <= 16384 ? 2 : 1;
 }
 
 template <typename T, typename CT, int D, int GM>
@@ -606,7 +619,7 @@ void launch_step(StepArgs& a, int batch, hipStream_t s) {
   if (a.splits == 1) return;
   a.joins = batch * a.Hq;
   const int64_t scores = a.pool.score ? int64_t((a.pad + kFinishEntries - 1) / kFinishEntries) * bh : 0;
-  step_finish<T, D><<<dim3(unsigned(a.joins + scores)), kFinish, 0, s>>>(a, kWaves * U);
+  step_finish<T, D, GM><<<dim3(unsigned(a.joins + scores)), kFinish, 0, s>>>(a, kWaves * U);
 }
 
 template <typename T, typename CT, int D>
