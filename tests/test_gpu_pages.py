@@ -323,6 +323,23 @@ def test_fill_long_prompt():
     fill_case(BF16, 64, 1, 2, 70001, None, 3501, 800, 4, 64)
 
 
+def test_fill_long_prompts_of_different_lengths():
+    """One batch in which a prompt is long, one short of the budget, one shorter than what a workgroup holds, and one empty."""
+    fill_case(BF16, 64, 5, 2, 20001, [20001, 300, 16000, 0, 4097], 500, 100, 3, 16, seed=1)
+    fill_case(F32, 64, 2, 1, 20001, [17000, 18000], 500, 497, 3, 16, seed=2)  # nothing but what is protected
+    fill_case(BF16, 128, 1, 1, 40000, [36865], 36864, 5, 0, 128, fp8=True, seed=3)
+
+
+def test_fill_long_prompts_with_scores_that_are_not_finite():
+    def spoil(t, K, V, s):
+        s[..., 10::50] = math.nan
+        s[..., 20::50] = math.inf
+        s[..., 30::50] = -math.inf
+        s[..., 31::3] = 0.25
+    for budget in (300, 1000, 12000):
+        fill_case(BF16, 64, 1, 2, 20000, None, budget, 20, 2, 16, spoil=spoil)
+
+
 def test_fill_scores_that_are_not_finite():
     def spoil(t, K, V, s):
         s[..., 10::50] = math.nan
