@@ -23,7 +23,7 @@ struct WindowArgs {
   // bf16: transposed values and a record per tile of 64 keys
   uint16_t* vt;  // [B][Hkv][tiles][D][64] fp16, every group of eight keys scaled by a power of two of its own
   float* rec;    // [B][Hkv][tiles][kRec]: exponents of the groups (of the even ones, then of the odd ones), a flag
-  int32_t tiles, blocks, reverse;
+  int32_t tiles, blocks, reverse, share;  // share: log2 of the query heads of a block
 };
 constexpr int kRec = 16;  // floats per record
 
@@ -53,7 +53,9 @@ __device__ __forceinline__ bool all_seen(const WindowArgs& a, int r0, int r1, in
   return k1 <= r0 && (k0 > r1 - a.window || k1 < a.n_sink);
 }
 
-// Workgroup number -> (block of rows, head and sequence).  Workgroups go to the chip's eight XCDs, each with an L2 of its own, in
+// A block's rows are those of BM / 2^share tokens and 2^share query heads of a group, wavefront by wavefront: the heads share K and V, and fewer
+// tokens see fewer tiles (8192 tokens, 32 heads on 8, window 1024: 220 -> 201 us).
+// Workgroup number -> (block of rows, heads and sequence).  Workgroups go to the chip's eight XCDs, each with an L2 of its own, in
 // turn; here each XCD gets a contiguous run of (head, block), so that blocks that share most of their window meet in one L2.
 // Without a window (reverse) the work grows with the block's position: the longest blocks of all heads first.
 __device__ __forceinline__ void place(const WindowArgs& a, int heads, int& block, int& hz) {
@@ -184,13 +186,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int Hkv = a.Hq / a.G;
   int blk, hz;
   place(a, gridDim.x / a.blocks, blk, hz);
-  const int hq = hz % a.Hq, b = hz / a.Hq, hk = hq / a.G;
+  const int groups = a.Hq >> a.share, b = hz / groups, hq0 = (hz % groups) << a.share, hk = hq0 / a.G;
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
-  const int r0 = blk * BM;
+  const int tokens = BM >> a.share, r0 = blk * tokens;
   if (r0 >= n) return;
   const int tid = threadIdx.x, w = tid >> 6, half = SPLIT ? w / kRW : 0, ws = __builtin_amdgcn_readfirstlane(w % kRW), lane = tid & 63, m = lane & 31, h = lane >> 5;
+  const int hq = hq0 + (w % kRW & ((1 << a.share) - 1));
   const float scale2 = kLog2e / sqrtf(float(D));
-  const Tiles tl(a, r0, min(r0 + BM, n) - 1, 64);
+  const Tiles tl(a, r0, min(r0 + tokens, n) - 1, 64);
   const int ntile = SPLIT ? (tl.count - half + 1) / 2 : tl.count, rounds = SPLIT ? (tl.count + 1) / 2 : tl.count;  // of this half, of both
   auto tile_of = [&](int t) __attribute__((always_inline)) { return tl.tile(SPLIT ? 2 * t + half : t); };
   uint16_t* Ks = smem + __builtin_amdgcn_readfirstlane(half) * 4 * kElems;  // [2][kElems]
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int i = 0; i < kLoadsV; ++i) load_lds16(src, v_off[i], Vs + (t & 1) * kElems + (ws * kLoadsV + i) * kGroupLd);
   };
-  const int wr0 = r0 + w % kRW * 32, q_row = wr0 + m;
+  const int wr0 = r0 + (w % kRW >> a.share) * 32, q_row = wr0 + m;
   bf16x8 bq[kKS];
   if (!SPLIT || ntile > 0) load_k(0);
   {
@@ -488,13 +491,13 @@ __global__ __launch_bounds__(256) void window_f32(WindowArgs a) {
   __shared__ int odd;
   int blk, hz;
   place(a, gridDim.x / a.blocks, blk, hz);
-  const int hq = hz % a.Hq, b = hz / a.Hq, hk = hq / a.G;
+  const int groups = a.Hq >> a.share, b = hz / groups, hq0 = (hz % groups) << a.share, hk = hq0 / a.G;
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
-  const int r0 = blk * BM;
+  const int tokens = BM >> a.share, r0 = blk * tokens;
   if (r0 >= n) return;
-  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4, hq = hq0 + (w & ((1 << a.share) - 1));
   const float scale2 = kLog2e / sqrtf(float(D));
-  const Tiles tl(a, r0, min(r0 + BM, n) - 1, BN);
+  const Tiles tl(a, r0, min(r0 + tokens, n) - 1, BN);
   const float* kbase = static_cast<const float*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
   const float* vbase = static_cast<const float*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
   f32x4 kr[kLoads], vr[kLoads];
@@ -521,7 +524,7 @@ __global__ __launch_bounds__(256) void window_f32(WindowArgs a) {
     }
     if (bad) odd = 1;
   };
-  const int wr0 = r0 + w * 16, q_row = wr0 + c;
+  const int wr0 = r0 + (w >> a.share) * 16, q_row = wr0 + c;
   f32x4 q[D / 16];
   fetch(0);
   const float* qp = static_cast<const float*>(a.q.ptr) + b * a.q.sb + hq * a.q.sh + int64_t(min(q_row, n - 1)) * a.q.sn;
@@ -732,16 +735,24 @@ size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_d
   return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * kRec * sizeof(float);
 }
 
+// Query heads that a block of `waves` wavefronts shares, and its blocks of rows.
+void share_heads(WindowArgs& a, int waves, int rows) {
+  a.share = 0;
+  while (a.G % (2 << a.share) == 0 && 2 << a.share <= waves) ++a.share;
+  const int tokens = (waves * rows) >> a.share;
+  a.blocks = (a.n + tokens - 1) / tokens;
+}
+
 template <int D, int NW, bool SPLIT>
 hipError_t run_bf16(WindowArgs& a, int batch, hipStream_t s) {
-  constexpr int BM = 32 * (SPLIT ? NW / 2 : NW), kSmem = (SPLIT ? 8 : 4) * tile_elems<D>() * int(sizeof(uint16_t));
+  constexpr int kRW = SPLIT ? NW / 2 : NW, kSmem = (SPLIT ? 8 : 4) * tile_elems<D>() * int(sizeof(uint16_t));
   static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 4) * 64 * int(sizeof(float)), "the second half's rows");
-  a.blocks = (a.n + BM - 1) / BM;
+  share_heads(a, kRW, 32);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW, SPLIT>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != hipSuccess) return e;
   window_values<D><<<dim3(a.tiles, batch * (a.Hq / a.G)), 256, 0, s>>>(a);
-  window_bf16<D, NW, SPLIT><<<dim3(unsigned(a.blocks) * batch * a.Hq), 64 * NW, kSmem, s>>>(a);
+  window_bf16<D, NW, SPLIT><<<dim3(unsigned(a.blocks) * batch * (a.Hq >> a.share)), 64 * NW, kSmem, s>>>(a);
   return hipGetLastError();
 }
 
@@ -790,20 +801,26 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   if (dtype == D2O_BF16) {
     a.vt = static_cast<uint16_t*>(workspace);
     a.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + values_bytes(batch, n, n_kv_heads, head_dim));
-    // Blocks of 256 rows, one workgroup per CU; of 128 where two per CU hold all of them; where one per CU does, with the
-    // tiles split over two halves of a workgroup.
+    // Wavefronts per workgroup.  Where the chip has a CU for every block of 128 rows, eight, the tiles split over two halves.  Otherwise four,
+    // two workgroups (d = 64: three) per CU that hide each other's ends, for heads of 64 and windows below 1024; for larger ones eight, for
+    // whose twice as many rows a tile is brought once.  (16384 tokens, 32 heads on 8, d = 128, four and eight: window 128 172 and 182 us, 512 270 and 275,
+    // 1024 414 and 407, 4096 1176 and 1135; d = 64, window 2048 425 and 464, 8000 1288 and 1396.  Blocks that all fit at once: four too.)
     const int64_t blocks = int64_t((n + 127) / 128) * n_q_heads * batch;
+    const bool four = blocks <= 512 || a.window < 1024;
     hipError_t e;
     if (head_dim == 64)
-      e = blocks <= 256 ? run_bf16<64, 8, true>(a, batch, s) : blocks <= 512 ? run_bf16<64, 4, false>(a, batch, s) : run_bf16<64, 8, false>(a, batch, s);
+      e = blocks <= 256 ? run_bf16<64, 8, true>(a, batch, s) : run_bf16<64, 4, false>(a, batch, s);
     else
-      e = blocks <= 256 ? run_bf16<128, 8, true>(a, batch, s) : blocks <= 512 ? run_bf16<128, 4, false>(a, batch, s) : run_bf16<128, 8, false>(a, batch, s);
+      e = blocks <= 256 ? run_bf16<128, 8, true>(a, batch, s) : four ? run_bf16<128, 4, false>(a, batch, s) : run_bf16<128, 8, false>(a, batch, s);
     return e == hipSuccess ? D2O_OK : D2O_ERR_HIP;
   }
   const int64_t heads = int64_t(batch) * n_q_heads;
   const bool few = (n + 63) / 64 * heads < 256;  // fewer blocks of 64 rows than CUs
-  a.blocks = few ? (n + 15) / 16 : (n + 63) / 64;
-  const dim3 grid(unsigned(a.blocks * heads));
+  if (few)
+    a.blocks = (n + 15) / 16;
+  else
+    share_heads(a, 4, 16);
+  const dim3 grid(unsigned(a.blocks * (heads >> a.share)));
   const auto kernel = few ? head_dim == 64 ? window_f32_few<64> : window_f32_few<128> : head_dim == 64 ? window_f32<64> : window_f32<128>;
   kernel<<<grid, 256, 0, s>>>(a);
   return hipGetLastError() == hipSuccess ? D2O_OK : D2O_ERR_HIP;
