@@ -19,8 +19,8 @@ def inputs(dtype, B, Hq, Hkv, n, d, seed=0, qscale=1.5):
     return r(Hq, qscale), r(Hkv), r(Hkv)
 
 
-def check(Q, K, V, O, window, n_sink, lens=None):
-    """O (on the CPU) against the definition; rows behind a sequence's end are not looked at here."""
+def check(Q, K, V, O, window, n_sink, lens=None, heads=None):
+    """O (on the CPU) against the definition; rows behind a sequence's end are not looked at here, nor heads other than `heads`."""
     B, Hq, n, d = Q.shape
     G = Hq // K.shape[1]
     for b in range(B):
@@ -28,7 +28,7 @@ def check(Q, K, V, O, window, n_sink, lens=None):
         if m == 0:
             continue
         seen = ref.window_seen(m, window, n_sink)
-        for h in range(Hq):
+        for h in heads if heads is not None else range(Hq):
             q, k, v = (x[b, i, :m].double() for x, i in ((Q, h), (K, h // G), (V, h // G)))
             o, p = ref.attend64(q, k, v, seen)
             got = O[b, h, :m].double()
@@ -65,6 +65,23 @@ def test_window_attend(dtype, d, size):
     B, Hq, Hkv, n, window, n_sink = size
     Q, K, V = inputs(dtype, B, Hq, Hkv, n, d, seed=n)
     check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("dtype,d,heads,n,window,n_sink,lens", [
+    (BF16, 128, (64, 16), 1111, 1029, 5, None), (BF16, 128, (60, 60), 1100, 0, 0, None), (BF16, 128, (60, 10), 1090, 1088, 70, [1090, 777]),
+    (BF16, 128, (64, 8), 1200, 1150, 4, [1200, 65]), (BF16, 128, (60, 15), 700, 300, 4, None), (BF16, 128, (72, 24), 650, 33, 65, [640, 3]),
+    (BF16, 64, (60, 60), 700, 129, 4, None), (BF16, 64, (64, 8), 1111, 1029, 0, [1111, 1, 500]), (F32, 64, (24, 4), 700, 100, 4, None),
+    (F32, 128, (32, 32), 600, 0, 0, [600, 333]), (F32, 128, (16, 2), 1100, 257, 33, [1100, 64]), (F32, 64, (40, 10), 450, 1, 1, None),
+], ids=str)
+def test_many_heads(dtype, d, heads, n, window, n_sink, lens):
+    """Enough rows for every kernel's larger blocks and for several heads of a group in one; a few values are not finite."""
+    Q, K, V = inputs(dtype, len(lens) if lens else 1, *heads, n, d, seed=n)
+    for h, j in ((0, 3), (heads[1] - 1, 100), (heads[1] - 1, n // 2)):
+        V[0, h, j, j % d] = math.inf
+    lens = torch.tensor(lens, dtype=torch.int32) if lens else None
+    got = run(Q, K, V, window, n_sink, lens)
+    G = heads[0] // heads[1]
+    check(Q, K, V, got, window, n_sink, lens, heads=sorted({0, G - 1, heads[0] // 2, heads[0] - G, heads[0] - 1}))
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
