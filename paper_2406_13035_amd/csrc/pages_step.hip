@@ -307,8 +307,9 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
 // WIDE: a tile lies in one page, whose number and address are the same for all lanes and live in scalar registers; a lane adds a
 // displacement of 32 bits that never changes.  Rows of V are read once and past the caches (16 lanes take whole lines; 131072 entries
 // 104 -> 98 us), K's are not: an instruction takes half lines, and with the hint the other half came from memory again.  Two wavefronts per
-// SIMD at least (16 heads per group of bf16 rows: 84 -> 72 us, of fp32 rows, which would spill, 104 -> 140; three: 65 -> 71 us for four).  (With an address per lane and row, computed for every tile, the vector ALU was as busy with
-// addresses as with sums: 4 x 32 heads x 4100 entries of 8-bit rows took 71 us, now 25.)
+// SIMD at least (16 heads per group of bf16 rows: 84 -> 72 us, of fp32 rows, which would spill, 104 -> 140; three: 65 -> 71 us for
+// four).  (With an address per lane and row, computed for every tile, the vector ALU was as busy with addresses as with sums: 4 x 32 heads x
+// 4100 entries of 8-bit rows took 71 us, now 25.)
 template <typename T, typename CT, int D, int GM, int U, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM > 8 && sizeof(CT) == 4 ? 1 : 2))) void step_part(StepArgs a) {
   typedef Rows<CT, D> R;

@@ -141,9 +141,10 @@ __global__ __launch_bounds__(256) void window_values(WindowArgs a) {
   uint32_t all = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) all = max(all, top[i]);
-  // exponent of the largest magnitude, brought to 13 (biased exponents; subnormal values count as the lowest)
+  // Exponent of the largest magnitude, brought to 13 (biased exponents; subnormal values count as the lowest).  A tile of zeros: low, so that
+  // its keys, however heavy, do not push the probabilities of others out of fp16, and not so low that their own leave fp32.
   auto exponent = [](uint32_t bits) { return max(int(bits >> 23), 1) - 127 - 13; };
-  const int e_tile = all ? exponent(all) : 0;
+  const int e_tile = all ? exponent(all) : -60;
   auto group_exponent = [&](int gr) __attribute__((always_inline)) {
     const int e = top[gr] ? exponent(top[gr]) : e_tile;
     return e < e_tile - 12 ? e : e_tile;

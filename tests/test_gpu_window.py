@@ -184,6 +184,19 @@ def test_sharp_and_flat_attention(dtype):
     check(Q, K, V, run(Q, K, V, 90, 2), 90, 2)
 
 
+@pytest.mark.parametrize("scale", [1e-10, 1e-6, 1.0, 1e10])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_runs_of_tokens_whose_values_are_zero(dtype, scale):
+    """They take their share of the weights and change nothing about the accuracy of the others."""
+    Q, K, V = inputs(dtype, 1, 2, 1, 500, 64)
+    V = (V.float() * scale).to(dtype)
+    V[:, :, 64:128] = 0
+    V[:, :, 250:400] = 0
+    check(Q, K, V, run(Q, K, V, 150, 3), 150, 3)
+    V[:, :, :64] = 0
+    check(Q, K, V, run(Q, K, V, 0, 0), 0, 0)
+
+
 def test_two_runs_and_another_stream_give_the_same_bits():
     Q, K, V = (x.cuda() for x in inputs(BF16, 2, 8, 2, 900, 128))
     first = binding.d2o_window_attend(Q, K, V, 300, 4)
