@@ -14,7 +14,7 @@ namespace d2o {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kFloor = -1e30f;  // exponent reference before a row has seen a key
+constexpr float kFloor = -3e38f;  // exponent reference before a row has seen a key
 
 struct WindowArgs {
   View q, k, v, o;
@@ -96,6 +96,7 @@ __device__ __forceinline__ int at128(int row, int chunk) { return (row >> 3) * k
 
 constexpr float kPShift = 12.f;  // probabilities are formed as 2^12 * p before the fp16 rounding
 constexpr float kLazy = 3.f;     // log2 of the growth the exponent reference tolerates before it moves
+constexpr float kFar = 1048576.f;  // exponents whose spacing, 1/8 and more, could let 2^12 * p leave fp16
 
 // MFMA row -> key offset inside 32 keys, such that accumulator registers 8 kb .. 8 kb + 7 of lane half h hold the keys 16 kb + 8 h .. + 7.
 __device__ __forceinline__ int perm_key(int m) { return (m & ~0xC) | ((m & 4) << 1) | ((m & 8) >> 1); }
@@ -256,11 +257,35 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
   // mrun: exponent reference of o; el: the sum is kept relative to mrun - el
   float mrun = kFloor, el = 0.f, lsum = 0.f;
+  // A row whose maximum lies beyond kFar has `away`, that maximum or an earlier one, taken from its logits first: what follows sees small numbers.
+  // (Looking for such rows takes 1 to 2.5%: 32768 tokens 2.46 -> 2.49 ms.)
+  float away = 0.f;  // as an exponent; 0: not such a row
+  bool far = false;  // the wavefront has such rows
   f32x16 s[2];
   f16x8 pb[2][2];
   auto active = [&](int t) __attribute__((always_inline)) {
     const int k0 = tile_of(t) * 64;
     return any_seen(a, wr0, wr0 + 31, k0, k0 + 63);
+  };
+  // `moves`: rows whose `away` becomes the tile's maximum; `takes`: rows it is taken from
+  auto take_away = [&](auto moves, auto takes) __attribute__((always_inline)) {
+#pragma clang fp contract(off)  // (a product that is rounded, so that the maximum less itself is zero)
+    float x = -INFINITY;
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x = fmaxf(x, s[st][r]);
+    x = max_halves(x) * scale2;
+    const float unscale = 1.f / scale2;
+    if (moves(x)) {
+      mrun -= x - away;
+      away = x;
+    }
+    const bool is = takes();
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[st][r] = is ? (s[st][r] * scale2 - away) * unscale : s[st][r];
   };
   // probabilities of one group of eight registers (sub-tile st, half kb) with exponent reference c
   auto form = [&](int st, int kb, float c) __attribute__((always_inline)) {
@@ -304,27 +329,38 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
       }
     }
-    float mx[4];
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        float x = s[st][8 * kb];
-#pragma unroll
-        for (int r = 1; r < 8; ++r) x = fmaxf(x, s[st][8 * kb + r]);
-        mx[st * 2 + kb] = x;
-      }
+    if (__builtin_expect(far, false)) take_away([&](float x) { return away != 0.f && x > away + kFar; }, [&] { return away != 0.f; });
     const float e0 = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(ex[0])));
     const bool one = __all(ex[0] == e0 && ex[1] == e0 && ex[2] == e0 && ex[3] == e0);
-    float top;
-    if (one)
-      top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), scale2, e0);
-    else
-      top = fmaxf(fmaxf(fmaf(mx[0], scale2, ex[0]), fmaf(mx[1], scale2, ex[1])),
-                  fmaxf(fmaf(mx[2], scale2, ex[2]), fmaf(mx[3], scale2, ex[3])));
-    const float cand = max_halves(top) - kPShift;
-    const bool grew = cand > mrun + kLazy;
+    auto reference = [&]() __attribute__((always_inline)) {  // that the tile asks for
+      float mx[4];
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          float x = s[st][8 * kb];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) x = fmaxf(x, s[st][8 * kb + r]);
+          mx[st * 2 + kb] = x;
+        }
+      float top;
+      if (one)
+        top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), scale2, e0);
+      else
+        top = fmaxf(fmaxf(fmaf(mx[0], scale2, ex[0]), fmaf(mx[1], scale2, ex[1])),
+                    fmaxf(fmaf(mx[2], scale2, ex[2]), fmaf(mx[3], scale2, ex[3])));
+      return max_halves(top) - kPShift;
+    };
+    float cand = reference();
+    bool grew = cand > mrun + kLazy;
     if (__any(grew)) {  // wavefront-uniform: no rescale when no row's maximum moved
+      const bool leap = grew && away == 0.f && fabsf(cand) > kFar && fabsf(cand) < INFINITY;
+      if (__builtin_expect(__any(leap), 0)) {
+        far = true;
+        take_away([&](float) { return leap; }, [&] { return leap; });
+        cand = reference();
+        grew = cand > mrun + kLazy;
+      }
       const float mnew = grew ? cand : mrun, enew = grew ? e0 : el;
       const float f = __builtin_amdgcn_exp2f(mrun - mnew);
       lsum *= __builtin_amdgcn_exp2f((mrun - mnew) - (el - enew));
@@ -422,17 +458,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
   if constexpr (SPLIT) {
     // the second half's rows to LDS (the tiles are done with), the first half adds them to its own
-    float* os = reinterpret_cast<float*>(smem) + ws * (kDC * 16 + 4) * 64 + lane;
+    float* os = reinterpret_cast<float*>(smem) + ws * (kDC * 16 + 5) * 64 + lane;
     if (half) {
       each<kDC>([&](auto dc) { each<16>([&](auto r) { os[(dc * 16 + r) * 64] = o[dc][decltype(r)::value]; }); });
       os[kDC * 16 * 64] = mrun;
       os[(kDC * 16 + 1) * 64] = el;
       os[(kDC * 16 + 2) * 64] = lsum;
       os[(kDC * 16 + 3) * 64] = flag;
+      os[(kDC * 16 + 4) * 64] = away;
     }
     __syncthreads();
     if (half) return;
-    const float m1 = os[kDC * 16 * 64], el1 = os[(kDC * 16 + 1) * 64], l1 = os[(kDC * 16 + 2) * 64];
+    const float m1 = os[kDC * 16 * 64] == kFloor ? kFloor : os[kDC * 16 * 64] + (os[(kDC * 16 + 4) * 64] - away), el1 = os[(kDC * 16 + 1) * 64], l1 = os[(kDC * 16 + 2) * 64];
     flag = fmaxf(flag, os[(kDC * 16 + 3) * 64]);
     const float M = fmaxf(mrun, m1), E = mrun >= m1 ? el : el1;
     const float f0 = __builtin_amdgcn_exp2f(mrun - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
@@ -747,7 +784,7 @@ void share_heads(WindowArgs& a, int waves, int rows) {
 template <int D, int NW, bool SPLIT>
 hipError_t run_bf16(WindowArgs& a, int batch, hipStream_t s) {
   constexpr int kRW = SPLIT ? NW / 2 : NW, kSmem = (SPLIT ? 8 : 4) * tile_elems<D>() * int(sizeof(uint16_t));
-  static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 4) * 64 * int(sizeof(float)), "the second half's rows");
+  static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 5) * 64 * int(sizeof(float)), "the second half's rows");
   share_heads(a, kRW, 32);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW, SPLIT>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);

@@ -132,6 +132,42 @@ def test_step_with_pages_whose_rows_lie_by_token(dtype, fp8):
     step_case(dtype, 128, 2, 4, 2, 16, [100, 37], fp8=fp8, order="token")
 
 
+@pytest.mark.parametrize("total", [14, 30, 100])
+@pytest.mark.parametrize("dtype,fp8", FORMS, ids=["f32", "bf16", "fp8"])
+def test_step_with_logits_of_any_size(dtype, fp8, total):
+    """Logits of up to 15 times 2^total, exact in fp32 and steps of 2^total / sqrt(d) apart: a head attends to its highest entry, or to
+    those that share its value, alone.  Heads in turn: of such logits, of their negatives, of all-zero ones and of small ones."""
+    d, n, Hkv, G = 128, 700, 2, 4
+    t = ref.make_pages(1, Hkv, d, 16, n // 16 + 1, dtype, total, fp8)
+    t["pos"] = None
+    g = torch.Generator().manual_seed(total)
+    K = torch.zeros(t["k"].shape)
+    K[..., 0] = torch.randint(1, 16, K.shape[:3], generator=g).float() * 2.0 ** (total // 2)
+    if fp8:
+        t["k"], t["k_exp"] = ref.encode(K.to(BF16))
+    else:
+        t["k"] = K.to(dtype)
+    q = torch.zeros(1, Hkv * G, d)
+    q[0, :, 0] = torch.tensor([2.0 ** (total - total // 2), -2.0 ** (total - total // 2), 0.0, 2.0 ** -(total // 2)]).repeat(Hkv)
+    q = q.to(dtype)
+    lens = torch.tensor([n], dtype=torch.int32)
+    gt = on_gpu(t)
+    out = torch.empty_like(q, device="cuda:0")
+    pages_of(gt, Hkv * G).d2o_pages_step(q.cuda(), None, None, lens.cuda(), out)
+    p, r = ref.entries(t, 0, n)
+    # the small heads' logits, at most 2, rounded three times, all of them scaled and their exponentials rounded: in the sum and in the normaliser
+    rel = 2 * (2 * 3 * 2.0 ** -24 + 2.0 ** -22 + n * 2.0 ** -24)
+    for h in range(Hkv):
+        k, v = (ref.rows64(t[x], t[x + "_exp"], p, h, r) for x in ("k", "v"))
+        o, pr = ref.attend64(q[0, h * G:(h + 1) * G].double(), k, v, torch.ones((G, n), dtype=torch.bool))
+        err = (out[0, h * G:(h + 1) * G].cpu().double() - o).abs()
+        tol = pr @ v.abs() * rel + o.abs() * ref.HALF_STEP[dtype]
+        assert bool((err <= tol).all()), (h, float((err / tol).max()))
+        old, now = t["score"][p, h, r].double(), gt["score"].cpu()[p, h, r].double()
+        tol = pr.sum(0) * rel + (G + 1) * 2.0 ** -24 * (pr.sum(0) + old) + 1e-38
+        assert bool(((now - old - pr.sum(0)).abs() <= tol).all())
+
+
 def spoil_behind(t, lens):
     """What lies behind a sequence's end, and in pages that nobody has, is NaN and infinite."""
     used = torch.zeros(t["k"].shape[0], t["k"].shape[2], dtype=torch.bool)

@@ -184,6 +184,56 @@ def test_sharp_and_flat_attention(dtype):
     check(Q, K, V, run(Q, K, V, 90, 2), 90, 2)
 
 
+@pytest.mark.parametrize("total", [14, 20, 27, 40, 115])
+@pytest.mark.parametrize("dtype,d,heads,n,window,n_sink", [
+    (F32, 64, (2, 1), 300, 90, 2), (F32, 128, (24, 4), 700, 300, 70), (BF16, 64, (2, 1), 300, 90, 2), (BF16, 128, (2, 1), 300, 0, 0),
+    (BF16, 64, (60, 60), 700, 300, 4), (BF16, 128, (60, 60), 700, 300, 70), (BF16, 128, (64, 16), 1111, 1029, 5),
+], ids=str)
+def test_logits_of_any_size(dtype, d, heads, n, window, n_sink, total):
+    """Logits of up to 255 times 2^total: products of one pair of numbers, so exact in fp32, and steps of 2^total / sqrt(d) apart, so a
+    row attends to its highest key, or to those that share its value, alone.  Rows in turn: of such logits, of their negatives, of all-zero
+    ones and of small ones.  A wavefront holds all four, and meets the huge ones in any tile of its window."""
+    g = torch.Generator().manual_seed(total)
+    Q, K = torch.zeros((1, heads[0], n, d)), torch.zeros((1, heads[1], n, d))
+    K[0, :, :, 0] = torch.randint(1, 256, (heads[1], n), generator=g).float() * 2.0 ** (total // 2)
+    Q[0, :, :, 0] = torch.tensor([2.0 ** (total - total // 2), -2.0 ** (total - total // 2), 0.0, 2.0 ** -(total // 2)]).repeat(n)[:n]
+    V = torch.randn((1, heads[1], n, d), generator=g).to(dtype)
+    Q, K, seen = Q.to(dtype), K.to(dtype), ref.window_seen(n, window, n_sink)
+    O = run(Q, K, V, window, n_sink)
+    # the small rows' logits, at most 32, rounded three times, all of them scaled and their exponentials rounded: in the sum and in the normaliser
+    rel = 2 * (32 * 3 * 2.0 ** -24 + 2.0 ** -22 + n * 2.0 ** -24) + (2.0 ** -11 if dtype == BF16 else 0)
+    for h in (0, heads[0] // 2, heads[0] - 1):
+        q, k, v = (x[0, i].double() for x, i in ((Q, h), (K, h * heads[1] // heads[0]), (V, h * heads[1] // heads[0])))
+        o, p = ref.attend64(q, k, v, seen)
+        tol = p @ v.abs() * rel + o.abs() * ref.HALF_STEP[dtype] + (float(v.abs().max()) * n * 2.0 ** -36 if dtype == BF16 else 0)
+        err = (O[0, h].double() - o).abs()
+        assert bool((err <= tol).all()), (h, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("start", [-200, -7, 4096, 1 << 20])
+@pytest.mark.parametrize("dtype,heads,window", [(F32, 2, 0), (BF16, 2, 0), (BF16, 2, 200), (BF16, 60, 200)], ids=str)
+def test_large_logits_that_grow_along_the_prompt(dtype, heads, window, start):
+    """Logits near 5814543, whose exponents lie near 2^20, and beyond, exact in fp32: 20 more every 64 tokens, where the tokens before still weigh."""
+    n, d = 1280, 64
+    Q, K, V = inputs(dtype, 1, heads, heads, n, d)
+    Q[:], K[:] = 0, 0
+    Q[..., :4] = 2048
+    Q[..., 4:7] = 1
+    for c, x in enumerate((2048, 768, 23, max(start, 0) / 2048, 271 - 256 + min(start, 0), 256)):
+        K[..., c] = x
+    K[..., 6] = (torch.arange(n) // 64 * 20).to(dtype)
+    assert float(Q[0, 0, 0].double() @ K[0, 0, 64].double()) == 5814543 + start + 20
+    O, seen = run(Q, K, V, window, 0), ref.window_seen(n, window, 0)
+    # an exponent of up to 2^21 is rounded to fp32: by 2^-4 at most, in the sum and in the normaliser; the rest is below 2^-9
+    rel = 2 * (2.0 ** 2.0 ** -4 - 1) + 2.0 ** -9
+    for h in (0, heads - 1):
+        q, k, v = (x[0, h].double() for x in (Q, K, V))
+        o, p = ref.attend64(q, k, v, seen)
+        err = (O[0, h].double() - o).abs()
+        tol = p @ v.abs() * rel + o.abs() * ref.HALF_STEP[dtype]
+        assert bool((err <= tol).all()), (h, float((err / tol).max()))
+
+
 @pytest.mark.parametrize("scale", [1e-10, 1e-6, 1.0, 1e10])
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_runs_of_tokens_whose_values_are_zero(dtype, scale):
