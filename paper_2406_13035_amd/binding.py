@@ -499,7 +499,7 @@ class Pages:
     [n_pages, Hkv, page_size] (8-bit rows of bfloat16 tensors); page_table int32 [B, max_pages]; score float32 and pos int32
     [n_pages, Hkv, page_size] where accumulated attention and token positions are kept.  max_len: the most entries a sequence
     (or tokens a prompt) will have in any call, the page table's capacity if None.  Calls on one object
-    share its workspace: on streams that overlap in time, use an object each."""
+    share its workspace: on streams (or in graphs) that overlap in time, use an object each, and keep it until they are done."""
 
     def __init__(self, K, V, page_table, n_q_heads, K_exp=None, V_exp=None, score=None, pos=None, max_len=None):
         self.lib = load_library()

@@ -278,6 +278,104 @@ def test_step_repeats_bit_for_bit(dtype, fp8):
         assert torch.equal(got["out"], first["out"])
 
 
+@pytest.mark.parametrize("dtype,fp8", FORMS, ids=["f32", "bf16", "fp8"])
+def test_step_over_pages_that_sequences_share(dtype, fp8):
+    """Three sequences with one prompt's pages in front and a page each of their own, where the new rows go; no scores are kept."""
+    t = ref.make_pages(3, 2, 64, 16, 8, dtype, 12, fp8, score=False, pos=False)
+    t["table"][1:, :6] = t["table"][0, :6]
+    g = torch.Generator().manual_seed(12)
+    q, kn, vn = (torch.randn((3, h, 64), generator=g).to(dtype) for h in (6, 2, 2))
+    lens = torch.tensor([100, 97, 112], dtype=torch.int32)
+    want, tol, new, _, _ = ref.step_ref(t, q, kn, vn, lens, None, 0, 0, 128, dtype)
+    gt = on_gpu(t)
+    out = torch.zeros((3, 6, 64), dtype=dtype, device="cuda:0")
+    pages_of(gt, 6).d2o_pages_step(*cuda(q, kn, vn, lens), out)
+    assert bool(((out.cpu().double() - want).abs() <= tol).all())
+    same(gt, new)
+
+
+@pytest.mark.parametrize("positions", [[5, 0], [199, 35], [260, 45], [0x7FFFFFFF, 41]], ids=str)
+def test_step_positions_that_are_not_the_entry(positions):
+    """Pages without positions: entry s has position s, and the window ends at the position that is given."""
+    step_case(BF16, 64, 2, 4, 2, 16, [200, 40], window=70, n_sink=3, positions=torch.tensor(positions, dtype=torch.int32))
+
+
+def test_step_exponents_at_odd_addresses():
+    t = ref.make_pages(2, 2, 128, 32, 8, BF16, 5, fp8=True)
+    g = torch.Generator().manual_seed(5)
+    q, kn, vn = (torch.randn((2, h, 128), generator=g).to(BF16).cuda() for h in (8, 2, 2))
+    lens = torch.tensor([230, 33], dtype=torch.int32, device="cuda:0")
+    got = []
+    for shift in (0, 1, 3):
+        gt = on_gpu(t)
+        for x in ("k_exp", "v_exp"):
+            flat = torch.empty(t[x].numel() + shift, dtype=torch.int8, device="cuda:0")[shift:]
+            gt[x] = flat.view(t[x].shape)
+            gt[x].copy_(t[x])
+        out = torch.zeros((2, 8, 128), dtype=BF16, device="cuda:0")
+        pages_of(gt, 8).d2o_pages_step(q, kn, vn, lens, out)
+        got.append((out, {x: (None if y is None else y.cpu()) for x, y in gt.items()}))
+    for out, tensors in got[1:]:
+        assert torch.equal(out, got[0][0])
+        same(tensors, got[0][1])
+
+
+def test_two_caches_at_once_on_two_streams():
+    """An object each, the same pages read by both: neither disturbs the other."""
+    t = ref.make_pages(4, 4, 128, 64, 64, BF16, 14, score=False, pos=False)
+    gt = on_gpu(t)
+    g = torch.Generator().manual_seed(14)
+    qs = [torch.randn((4, 16, 128), generator=g).to(BF16).cuda() for _ in range(2)]
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda:0") for x in ([4096, 4000, 77, 1], [900, 4096, 4096, 4095])]
+    pages, outs, want = [pages_of(gt, 16) for _ in range(2)], [], []
+    for p, q, n in zip(pages, qs, lens):
+        want.append(torch.zeros_like(q))
+        p.d2o_pages_step(q, None, None, n, want[-1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(20):
+        for j in range(2):
+            with torch.cuda.stream(streams[j]):
+                outs.append(torch.zeros_like(qs[j]))
+                pages[j].d2o_pages_step(qs[j], None, None, lens[j], outs[-1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want[i % 2]) for i, out in enumerate(outs))
+
+
+def test_fill_and_evictions_captured_and_replayed():
+    """A graph of a prompt in slices, a shorter one and evictions with moves in a launch of their own and without, replayed with new inputs."""
+    n, B, Hkv, d = 20000, 2, 2, 64
+    t = ref.make_pages(B, Hkv, d, 64, 41, BF16, 15)
+    a, b = on_gpu(t), on_gpu(t)
+    pa, pb = pages_of(a, Hkv, n), pages_of(b, Hkv, n)
+    K, V = (torch.zeros((B, Hkv, n, d), dtype=BF16, device="cuda:0") for _ in range(2))
+    sc = torch.zeros((B, Hkv, n), device="cuda:0")
+    lens, kept = (torch.zeros(B, dtype=torch.int32, device="cuda:0") for _ in range(2))
+    half = n // 2
+
+    def work(p):
+        p.d2o_pages_fill(K, V, 2600, 300, 4, score=sc, lens=lens)
+        p.d2o_pages_evict(kept, 1300, 100, 4)
+        p.d2o_pages_fill(K[:, :, :half], V[:, :, :half], 1000, 10, 0, score=sc[:, :, :half].contiguous(), lens=lens)
+        p.d2o_pages_evict(kept.clamp(max=1000), 999, 10, 0)
+
+    g = torch.Generator().manual_seed(15)
+    work(pa), work(pb)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work(pa)
+    for m in ([20000, 2700], [12000, 15], [0, 20000], [2601, 19000]):
+        K.copy_(torch.randn(K.shape, generator=g)), V.copy_(torch.randn(V.shape, generator=g))
+        sc.copy_(torch.rand(sc.shape, generator=g))
+        lens.copy_(torch.tensor(m, dtype=torch.int32)), kept.copy_(lens.clamp(max=2600))
+        graph.replay()
+        torch.cuda.synchronize()
+        work(pb)
+        torch.cuda.synchronize()
+        same(a, {x: (None if y is None else y.cpu()) for x, y in b.items()})
+
+
 def test_step_captured_and_replayed():
     """A graph of two steps and an eviction sharing a workspace, replayed with new inputs and lengths."""
     t = ref.make_pages(2, 2, 128, 16, 30, BF16, 4)
