@@ -326,13 +326,14 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * without Eq. 9-12), over a cache that lies in pages of a pool shared by all sequences.  No
  * context is needed: the caller owns pools, page table, lengths and workspace.  All of these calls
  * enqueue only, allocate nothing, keep nothing between calls and may be captured into a graph.
+ * Rows are contiguous and start at 16-byte boundaries: pointers and strides of every view are such, and no stride is negative.
  * A workspace (16-byte aligned) belongs to one call at a time: calls that overlap in time need one each. */
 
 /* Causal prompt attention in which query i sees the keys j <= i with j > i - window or j < n_sink:
  * O = softmax(Q K^T / sqrt(d)) V over those.  window = 0: no window (every j <= i).
  * Q, O: [B][Hq][n][d]; K, V: [B][Hkv][n][d]; O in `dtype`.  lens: device [B], the tokens of each sequence
  * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
- * its keys behind the end take no part.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
+ * its keys behind the end take no part.  An infinity or NaN in V reaches the rows that see it, whatever its weight, and no others.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
  * INVALID_ARG, UNSUPPORTED (also a row stride of K of 2^24 elements or more), CAPACITY (workspace smaller than
  * d2o_window_workspace_bytes says; where it says 0, NULL will do), HIP. */
 int d2o_window_workspace_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
@@ -384,7 +385,8 @@ int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, co
  * the softmax rows of the Hq / Hkv query heads are added to the entries' scores (Eq. 6).  positions: device
  * [B], NULL: lens[b] - 1.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
  * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
- * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry.
+ * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry (or only
+ * logits of minus infinity).
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_len beyond the page table, workspace too small), HIP. */
 int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view v_new, const int32_t* lens,
                    const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
