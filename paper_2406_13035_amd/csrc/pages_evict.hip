@@ -402,7 +402,11 @@ struct EvictArgs {
   const int32_t* lens;
   int32_t* moves;  // [B][Hkv][2][most] entries below the budget that are given up, kept entries behind it, rising
   int32_t* count;  // [B][Hkv] pairs
-  int32_t max_len, budget, recent, n_sink, most;
+  // long caches, by slices:
+  int32_t* newest;   // [B][Hkv][slices] largest position of a slice
+  int32_t* guarded;  // [B][Hkv][slices] its protected entries
+  uint32_t* cand;    // [B][Hkv][slices * extra][3] its lowest entries, as many as the sequence gives up: score's key, position's, entry | protected << 31
+  int32_t max_len, budget, recent, n_sink, most, slices, extra;
 };
 constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself (256 rows of 32 heads: 15.7 us,
                               // in a launch of their own 18)
@@ -482,6 +486,94 @@ __device__ __forceinline__ int block_max(int v, int* buf) {
   for (int i = 0; i < NT / 64; ++i) v = max(v, buf[i]);
   __syncthreads();
   return v;
+}
+
+// The lowest of the entries that each_rank(f) hands to f(entry, rank) on all threads together; of equals the last.
+struct Lowest {
+  uint32_t key, low;
+  int at;
+  __device__ __forceinline__ void take(uint32_t k, uint32_t l, int j) {
+    if (k < key || (k == key && (l < low || (l == low && j > at)))) key = k, low = l, at = j;
+  }
+};
+template <int NT, typename F>
+__device__ __forceinline__ Lowest lowest_entry(SelectShared& sh, const F& each_rank) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  Lowest x{0xFFFFFFFFu, 0xFFFFFFFFu, -1};
+  each_rank([&](int j, const Rank& r) __attribute__((always_inline)) { x.take(r.key, r.low, j); });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1)
+    x.take(uint32_t(__shfl_xor(int(x.key), o, 64)), uint32_t(__shfl_xor(int(x.low), o, 64)), __shfl_xor(x.at, o, 64));
+  if (lane == 0) {
+    sh.hist[w] = int(x.key);
+    sh.hist[16 + w] = int(x.low);
+    sh.hist[32 + w] = x.at;
+  }
+  __syncthreads();
+  for (int i = 0; i < NT / 64; ++i) x.take(uint32_t(sh.hist[i]), uint32_t(sh.hist[16 + i]), sh.hist[32 + i]);
+  __syncthreads();
+  return x;
+}
+
+// Which of the entries that each_rank(f) hands to f(entry, rank) are the `keep` highest; `guarded` of them have the key kProtected.
+// few: LDS of kFew words.
+struct Threshold {
+  uint32_t t, tl;
+  int ts;
+  __device__ __forceinline__ bool stays(const Rank& x, int j) const { return x.key > t || (x.key == t && (x.low > tl || (x.low == tl && j <= ts))); }
+};
+constexpr int kFew = 256;
+template <int NT, typename F>
+__device__ __forceinline__ Threshold threshold(SelectShared& sh, uint64_t* few, int keep, int guarded, const F& each_rank) {
+  static_assert(kFew <= NT, "a thread each");
+  const int tid = threadIdx.x;
+  // among the entries that are not protected (which share one key, at whose bin thousands would queue)
+  int equal = keep, same = guarded;
+  uint32_t t = kProtected;
+  if (guarded != keep)
+    t = nth_largest<NT>(sh, keep - guarded, equal, same, [&](auto f) __attribute__((always_inline)) {
+      each_rank([&](int, const Rank& x) {
+        if (x.key != kProtected) f(x.key);
+      });
+    });
+  // Of several entries with the threshold's key only some stay: those with the lowest positions, of equal positions the first entries; (tl, ts)
+  // are the last one's.  A few are ranked against each other, many selected digit by digit.
+  uint32_t tl = 0;
+  int ts = INT32_MAX;
+  if (equal < same && same <= kFew) {
+    if (tid == 0) sh.bin = 0;
+    __syncthreads();
+    each_rank([&](int j, const Rank& x) {
+      if (x.key == t) few[atomicAdd(&sh.bin, 1)] = uint64_t(x.low) << 32 | ~uint32_t(j);  // larger: kept before
+    });
+    __syncthreads();
+    if (tid < same) {
+      const uint64_t mine = few[tid];
+      int before = 0;
+#pragma unroll 8
+      for (int i = 0; i < same; ++i) before += few[i] > mine;
+      if (before == equal - 1) {
+        sh.left = int(mine >> 32);
+        sh.above = int(~uint32_t(mine));
+      }
+    }
+    __syncthreads();
+    tl = sh.left;
+    ts = sh.above;
+  } else if (equal < same) {
+    tl = nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
+      each_rank([&](int, const Rank& x) {
+        if (x.key == t) f(x.low);
+      });
+    });
+    if (equal < same)
+      ts = ~int(nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
+        each_rank([&](int j, const Rank& x) {
+          if (x.key == t && x.low == tl) f(~uint32_t(j));
+        });
+      }));
+  }
+  return {t, tl, ts};
 }
 
 // One workgroup per head, entries u * NT + thread: in registers (PT of them per thread) or, PT = 0, read again for every use.
@@ -576,22 +668,7 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   };
 
   if (n == S + 1) {  // one entry goes: the lowest, of equals the last
-    uint32_t key = 0xFFFFFFFFu, low = 0xFFFFFFFFu;
-    int at = -1;
-    auto take = [&](uint32_t k, uint32_t l, int j) __attribute__((always_inline)) {
-      if (k < key || (k == key && (l < low || (l == low && j > at)))) key = k, low = l, at = j;
-    };
-    each_rank([&](int j, const Rank& x) { take(x.key, x.low, j); });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-      take(uint32_t(__shfl_xor(int(key), o, 64)), uint32_t(__shfl_xor(int(low), o, 64)), __shfl_xor(at, o, 64));
-    if (lane == 0) {
-      sh.hist[w] = int(key);
-      sh.hist[16 + w] = int(low);
-      sh.hist[32 + w] = at;
-    }
-    __syncthreads();
-    for (int i = 0; i < NT / 64; ++i) take(uint32_t(sh.hist[i]), uint32_t(sh.hist[16 + i]), sh.hist[32 + i]);
+    const int at = lowest_entry<NT>(sh, each_rank).at;
     if (!here) {
       if (tid == 0) {
         int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
@@ -605,56 +682,8 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
     return;
   }
 
-  // the threshold, among the entries that are not protected (which share one key, at whose bin thousands would queue)
-  int equal = S, same = guarded;
-  uint32_t t = kProtected;
-  if (guarded != S)
-    t = nth_largest<NT>(sh, crowded ? S : S - guarded, equal, same, [&](auto f) __attribute__((always_inline)) {
-      each_rank([&](int, const Rank& x) {
-        if (x.key != kProtected) f(x.key);
-      });
-    });
-  // Of several entries with the threshold's key only some stay: those with the lowest positions, of equal positions the first entries; (tl, ts)
-  // are the last one's.  A few are ranked against each other, many selected digit by digit.
-  uint32_t tl = 0;
-  int ts = INT32_MAX;
-  constexpr int kFew = 256;
-  static_assert(kFew <= NT && 2 * kFew <= 2 * kInline, "a thread and two words each");
-  if (equal < same && same <= kFew) {
-    uint64_t* few = reinterpret_cast<uint64_t*>(lists);  // larger: kept before
-    if (tid == 0) sh.bin = 0;
-    __syncthreads();
-    each_rank([&](int j, const Rank& x) {
-      if (x.key == t) few[atomicAdd(&sh.bin, 1)] = uint64_t(x.low) << 32 | ~uint32_t(j);
-    });
-    __syncthreads();
-    if (tid < same) {
-      const uint64_t mine = few[tid];
-      int before = 0;
-#pragma unroll 8
-      for (int i = 0; i < same; ++i) before += few[i] > mine;
-      if (before == equal - 1) {
-        sh.left = int(mine >> 32);
-        sh.above = int(~uint32_t(mine));
-      }
-    }
-    __syncthreads();
-    tl = sh.left;
-    ts = sh.above;
-  } else if (equal < same) {
-    tl = nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
-      each_rank([&](int, const Rank& x) {
-        if (x.key == t) f(x.low);
-      });
-    });
-    if (equal < same)
-      ts = ~int(nth_largest<NT>(sh, equal, equal, same, [&](auto f) __attribute__((always_inline)) {
-        each_rank([&](int j, const Rank& x) {
-          if (x.key == t && x.low == tl) f(~uint32_t(j));
-        });
-      }));
-  }
-  auto stays = [&](const Rank& x, int j) { return x.key > t || (x.key == t && (x.low > tl || (x.low == tl && j <= ts))); };
+  static_assert(2 * kFew <= 2 * kInline, "two words each");
+  const Threshold kept = threshold<NT>(sh, reinterpret_cast<uint64_t*>(lists), S, crowded ? 0 : guarded, each_rank);
   int32_t *hole = lists, *from = lists + kInline;
   if (!here) {
     hole = a.moves + int64_t(bh) * 2 * a.most;
@@ -672,7 +701,7 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
         x[u] = r[u];
       else
         x[u] = rank_at(j);
-      keep |= uint32_t(j < n && stays(x[u], j)) << u;
+      keep |= uint32_t(j < n && kept.stays(x[u], j)) << u;
     }
     __syncthreads();
     // holes below the budget and kept rows behind it
@@ -715,13 +744,187 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int lanes) {
                a.count[bh], threadIdx.x % lanes);
 }
 
+// Caches that a workgroup does not hold in registers and that give up few entries, in slices of kSlice entries.  The entries that go are among
+// the lowest of each slice, as many as go in all: the largest position of each slice, ...
+__global__ __launch_bounds__(kSliceThreads) void evict_newest(EvictArgs a) {
+  __shared__ int buf[kSliceThreads / 64];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, j0 = blockIdx.x * kSlice + threadIdx.x;
+  const int n = min(a.lens[b], a.max_len);
+  if (n <= a.budget || int(blockIdx.x) * kSlice >= n) return;
+  int page[kSlicePer], pos[kSlicePer], newest = -INT32_MAX;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) page[u] = a.pool.page_of(b, min(j0 + u * kSliceThreads, n - 1));
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) pos[u] = a.pool.pos[page[u] >= 0 ? a.pool.at(page[u], hk, min(j0 + u * kSliceThreads, n - 1)) : 0];
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u)
+    if (page[u] >= 0) newest = max(newest, pos[u]);
+  newest = block_max<kSliceThreads>(newest, buf);
+  if (threadIdx.x == 0) a.newest[int64_t(bh) * a.slices + blockIdx.x] = newest;
+}
+
+// ... the lowest entries of each slice in the order (protected, score, position, entry), which both orders of Rank agree with on what
+// goes: protected entries that go at all go by score, and then every other entry goes ...
+__global__ __launch_bounds__(kSliceThreads) void evict_lowest(EvictArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ uint64_t few[kFew];
+  __shared__ uint32_t cnt[kSlicePer * (kSliceThreads / 64) + 1];
+  const int bh = blockIdx.y, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j0 = blockIdx.x * kSlice;
+  const int n = min(a.lens[b], a.max_len), have = min(kSlice, n - j0), goes = min(n - a.budget, have);
+  if (n <= a.budget || j0 >= n) return;
+  int page[kSlicePer], pos[kSlicePer], newest = -INT32_MAX;
+  float score[kSlicePer];
+  uint32_t present = 0, guard = 0;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) page[u] = a.pool.page_of(b, min(j0 + u * kSliceThreads + tid, n - 1));
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const int j = j0 + u * kSliceThreads + tid;
+    const bool there = j < n && page[u] >= 0;
+    const int64_t at = there ? a.pool.at(page[u], hk, j) : 0;
+    score[u] = a.pool.score[at];
+    pos[u] = a.pool.pos[at];
+    present |= uint32_t(there) << u;
+  }
+  for (int i = tid; i * kSlice < n; i += kSliceThreads) newest = max(newest, a.newest[int64_t(bh) * a.slices + i]);
+  const int64_t late = int64_t(block_max<kSliceThreads>(newest, sh.wave)) - a.recent;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) guard |= uint32_t((present >> u & 1) && is_guarded(a, pos[u], late)) << u;
+  const int guarded = block_total<kSliceThreads>(__popc(guard), sh.wave);
+  const bool crowded = have - guarded < goes;
+  Rank r[kSlicePer];
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    r[u] = rank_of(a, score[u], pos[u], late, crowded);
+    if (!(present >> u & 1)) r[u] = {0, 0};
+  }
+  auto each_rank = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kSlicePer; ++u)
+      if (u * kSliceThreads + tid < have) f(u * kSliceThreads + tid, r[u]);
+  };
+  Threshold kept{0xFFFFFFFFu, 0xFFFFFFFFu, -1};  // none
+  if (goes == 1) {
+    const Lowest x = lowest_entry<kSliceThreads>(sh, each_rank);
+    kept = {x.key, x.low, x.at - 1};
+  } else if (goes < have) {
+    kept = threshold<kSliceThreads>(sh, few, have - goes, crowded ? 0 : guarded, each_rank);
+  }
+  uint32_t gone = 0;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const int j = u * kSliceThreads + tid;
+    gone |= uint32_t(j < have && !kept.stays(r[u], j)) << u;
+    const uint64_t m = __ballot(gone >> u & 1);
+    if (lane == 0) cnt[u * (kSliceThreads / 64) + w] = __popcll(m);
+  }
+  prefix_counts<kSliceThreads, kSlicePer>(cnt);
+  uint32_t* out = a.cand + (int64_t(bh) * a.slices + blockIdx.x) * a.extra * 3;
+#pragma unroll
+  for (int u = 0; u < kSlicePer; ++u) {
+    const bool is = gone >> u & 1;
+    const int at = cnt[u * (kSliceThreads / 64) + w] + lanes_before(__ballot(is));
+    if (is && at < a.extra) {
+      const bool there = present >> u & 1;
+      out[at * 3] = there ? score_key(score[u]) : 0;
+      out[at * 3 + 1] = r[u].low;
+      out[at * 3 + 2] = uint32_t(j0 + u * kSliceThreads + tid) | (guard >> u & 1) << 31;
+    }
+  }
+  if (tid == 0) a.guarded[int64_t(bh) * a.slices + blockIdx.x] = guarded;
+}
+
+// ... and the lowest of those, with the moves that follow: a workgroup per head, at most NT * PT candidates.
+constexpr int kPick = 16384;
+template <int NT, int PT>
+__global__ __launch_bounds__(NT) void evict_pick(EvictArgs a, int lanes) {
+  __shared__ SelectShared sh;
+  __shared__ uint64_t few[kFew];
+  __shared__ uint32_t cnt[PT * (NT / 64) + 1];
+  __shared__ int hole[kInline], from[kInline], gone[kInline];
+  static_assert(kInline <= NT, "a thread per entry behind the budget");
+  const int bh = blockIdx.x, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = min(a.lens[b], a.max_len), S = a.budget, goes = n - S;
+  if (goes <= 0) return;
+  const int slices = (n + kSlice - 1) / kSlice, count = (slices - 1) * goes + min(goes, n - (slices - 1) * kSlice);
+  uint32_t key[PT], entry[PT];
+  Rank r[PT];
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const int i = min(u * NT + tid, count - 1);
+    const uint32_t* c = a.cand + ((int64_t(bh) * a.slices + i / goes) * a.extra + i % goes) * 3;
+    key[u] = c[0];
+    r[u].low = c[1];
+    entry[u] = c[2];
+  }
+  int guarded = 0, mine = 0;  // in all; of the candidates
+  for (int i = tid; i < slices; i += NT) guarded += a.guarded[int64_t(bh) * a.slices + i];
+  if (tid < goes) gone[tid] = 0;
+  const bool crowded = block_total<NT>(guarded, sh.wave) > S;
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const bool guard = entry[u] >> 31;
+    r[u].key = key[u] == 0 ? 0 : crowded ? (guard ? key[u] : 1u) : guard ? kProtected : key[u];
+    mine += u * NT + tid < count && r[u].key == kProtected;
+  }
+  mine = block_total<NT>(mine, sh.wave);
+  auto each_rank = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < PT; ++u)
+      if (u * NT + tid < count) f(u * NT + tid, r[u]);
+  };
+  Threshold kept{0xFFFFFFFFu, 0xFFFFFFFFu, -1};  // none
+  if (goes == 1) {
+    const Lowest x = lowest_entry<NT>(sh, each_rank);
+    kept = {x.key, x.low, x.at - 1};
+  } else if (goes < count) {
+    kept = threshold<NT>(sh, few, count - goes, mine, each_rank);
+  }
+  uint32_t is_hole = 0;
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const int i = u * NT + tid, j = int(entry[u] & 0x7FFFFFFFu);
+    const bool goner = i < count && !kept.stays(r[u], i);
+    if (goner && j >= S) gone[j - S] = 1;
+    is_hole |= uint32_t(goner && j < S && key[u] != 0) << u;
+    const uint64_t m = __ballot(is_hole >> u & 1);
+    if (lane == 0) cnt[u * (NT / 64) + w] = __popcll(m);
+  }
+  prefix_counts<NT, PT>(cnt);
+#pragma unroll
+  for (int u = 0; u < PT; ++u) {
+    const bool is = is_hole >> u & 1;
+    const int at = cnt[u * (NT / 64) + w] + lanes_before(__ballot(is));
+    if (is && at < kInline) hole[at] = int(entry[u] & 0x7FFFFFFFu);
+  }
+  const int holes = cnt[PT * (NT / 64)];
+  // the entries behind the budget that stay
+  const bool row = tid < goes && !gone[tid] && a.pool.page_of(b, S + tid) >= 0;
+  const uint64_t m = __ballot(row);
+  if (lane == 0) sh.wave[w] = __popcll(m);
+  __syncthreads();
+  int at = lanes_before(m), rows = 0;
+  for (int i = 0; i < NT / 64; ++i) {
+    if (i < w) at += sh.wave[i];
+    rows += sh.wave[i];
+  }
+  if (row) from[at] = S + tid;
+  __syncthreads();
+  move_rows<4>(a, b, hk, from, hole, tid / lanes, NT / lanes, min(min(holes, rows), kInline), tid % lanes);
+}
+
 // Workspace of a fill: a list of kept positions; of a long prompt also the slices' histograms and counts, and the candidates.
 size_t fill_bytes(size_t bh, size_t n) {
   const size_t list = round256(bh * n * sizeof(int32_t)), slices = (n + kSlice - 1) / kSlice;
   if (n <= kFillSelect) return list;
   return 2 * list + round256(bh * slices * kBins * sizeof(uint16_t)) + round256(bh * slices * sizeof(int32_t)) + round256(bh * 4 * sizeof(int32_t));
 }
-size_t moves_bytes(size_t bh, size_t n) { return round256(bh * 2 * n * sizeof(int32_t)) + round256(bh * sizeof(int32_t)); }
+// Of an eviction: the moves, or what the slices leave.
+size_t moves_bytes(size_t bh, size_t n) {
+  const size_t moves = round256(bh * 2 * n * sizeof(int32_t)) + round256(bh * sizeof(int32_t)), slices = (n + kSlice - 1) / kSlice;
+  if (n <= kFillSelect) return moves;
+  return std::max(moves, 2 * round256(bh * slices * sizeof(int32_t)) + bh * std::min<size_t>(kPick, slices * kInline) * 3 * sizeof(uint32_t));
+}
 }  // namespace
 
 size_t pages_evict_bytes(const d2o_pages* p, int32_t max_len) {
@@ -826,20 +1029,36 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
   a.recent = recent;
   a.n_sink = n_sink;
   a.most = std::min(budget, max_len - budget);
+  a.extra = max_len - budget;
+  a.slices = (max_len + kSlice - 1) / kSlice;
   a.moves = static_cast<int32_t*>(workspace);
   a.count = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + round256(size_t(bh) * 2 * max_len * sizeof(int32_t)));
+  a.newest = a.moves;
+  a.guarded = a.newest + round256(size_t(bh) * a.slices * sizeof(int32_t)) / sizeof(int32_t);
+  a.cand = reinterpret_cast<uint32_t*>(a.guarded + round256(size_t(bh) * a.slices * sizeof(int32_t)) / sizeof(int32_t));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int lanes = pages->head_dim * (pages->cache_fp8 ? 1 : pages->dtype == D2O_BF16 ? 2 : 4) / 16;
   const dim3 heads{unsigned(bh)};
+  // More than the registers of a workgroup hold: in slices where few go (one of 8 x 26214 entries 24 us, by a workgroup per head that reads them
+  // again for every use 44; of 8 x 131072 25 and 184; 256 of 8 x 26214 42 and 100), by that workgroup where slices would leave as many candidates.
+  const bool by_slices = max_len > 16384 && a.extra <= kInline && int64_t(a.slices) * a.extra <= kPick && a.slices <= kMaxSlices;
   if (max_len <= 2048)
     evict_select<256, 8><<<heads, 256, 0, s>>>(a, lanes);
   else if (max_len <= 4096)
     evict_select<1024, 4><<<heads, 1024, 0, s>>>(a, lanes);
   else if (max_len <= 16384)
     evict_select<1024, 16><<<heads, 1024, 0, s>>>(a, lanes);
-  else
+  else if (by_slices) {
+    const dim3 grid(a.slices, unsigned(bh));
+    evict_newest<<<grid, kSliceThreads, 0, s>>>(a);
+    evict_lowest<<<grid, kSliceThreads, 0, s>>>(a);
+    if (a.slices * a.extra <= 1024)
+      evict_pick<1024, 1><<<heads, 1024, 0, s>>>(a, lanes);
+    else
+      evict_pick<1024, 16><<<heads, 1024, 0, s>>>(a, lanes);
+  } else
     evict_select<1024, 0><<<heads, 1024, 0, s>>>(a, lanes);
-  if (a.most > kInline) {
+  if (a.most > kInline) {  // (by slices: never)
     const int per = 256 / lanes;
     evict_move<<<dim3((a.most + per - 1) / per, unsigned(bh)), 256, 0, s>>>(a, lanes);
   }

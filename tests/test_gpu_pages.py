@@ -620,6 +620,57 @@ def test_evict_long_caches(lens, budget):
     evict_case(BF16, 64, 1, 1, 64, lens, budget, budget // 4, 4)
 
 
+def _equal(t, lens):
+    t["score"].fill_(0.25)
+
+
+def _one_position(t, lens):
+    t["score"].fill_(0.25)
+    t["pos"].fill_(9)
+
+
+def _not_finite(t, lens):
+    for i, x in enumerate((math.nan, math.inf, -math.inf, -0.0, 0.0)):
+        for b, n in enumerate(lens):
+            p, r = ref.entries(t, b, n)
+            t["score"][p[i::9], :, r[i::9]] = x
+            t["pos"][p[5::18], :, r[5::18]] = -3
+
+
+def _protected(t, lens):
+    """Nearly all entries have the newest position."""
+    for b, n in enumerate(lens):
+        p, r = ref.entries(t, b, n)
+        t["pos"][p[10:], :, r[10:]] = 1 << 20
+        t["score"][p[::3], :, r[::3]] = 0.5
+
+
+def _no_pages(t, lens):
+    for b, n in enumerate(lens):
+        t["table"][b, 1 + b], t["table"][b, (n - 1) // 64], t["table"][b, 100] = -1, 1 << 30, -5
+
+
+def _ascending(t, lens):
+    """Everything that goes lies in one slice."""
+    for b, n in enumerate(lens):
+        p, r = ref.entries(t, b, n)
+        t["score"][p, :, r] = (torch.arange(n) if b == 0 else n - torch.arange(n)).float()[:, None].expand(-1, t["score"].shape[1])
+
+
+@pytest.mark.parametrize("spoil", [None, _equal, _one_position, _not_finite, _protected, _no_pages, _ascending],
+                         ids=lambda f: f.__name__[1:] if f else "plain")
+@pytest.mark.parametrize("budget,over", [(16384, 1), (17000, 37), (20470, 512), (33000, 513), (16390, 200)], ids=str)
+def test_evict_a_few_of_long_caches(budget, over, spoil):
+    """Sequences that give up as many as there may be, half of them, one and none."""
+    evict_case(BF16, 64, 4, 1, 64, [budget + over, budget + max(1, over // 2), budget + 1, budget], budget, 300, 4, spoil=spoil, ties=over == 37,
+               max_len=budget + over, seed=over)
+
+
+@pytest.mark.parametrize("dtype,fp8", FORMS, ids=["f32", "bf16", "fp8"])
+def test_evict_one_of_a_long_cache_of_many_heads(dtype, fp8):
+    evict_case(dtype, 128, 1, 5, 16, [70001], 70000, 17500, 4, fp8, max_len=70016)
+
+
 def test_evict_rows_by_token_and_lengths_beyond_max_len():
     evict_case(BF16, 128, 2, 2, 16, [100, 130], 90, 20, 2, order="token")
     # a sequence that claims more than max_len is cut to it
