@@ -114,6 +114,13 @@ __device__ __forceinline__ float sum_rows(float v) {
   return __int_as_float(b[0]) + __int_as_float(b[1]);
 }
 
+__device__ __forceinline__ float max_rows(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+  v = fmaxf(__int_as_float(a[0]), __int_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return fmaxf(__int_as_float(b[0]), __int_as_float(b[1]));
+}
+
 // What a lane holds of rows of type CT with D elements.  K: lane l has row l % 16 of a tile, chunks of 16 bytes that the four rows of
 // lanes take in turn; V: the 16 lanes of a row of lanes share a row of V, D / 16 elements each.
 template <typename CT, int D>
@@ -302,18 +309,20 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
 // holds 16 bytes of row l % 16 at a time, and the order of the products' terms is free.  A lane of the result has head
 // l % 16 and four entries of its row of lanes, and that row of lanes reads the rows of V of just these entries: every row of lanes keeps a
 // softmax of its own over the entries it meets, with nothing exchanged in the loop; a probability reaches the lanes of
-// its row by a register broadcast.  P V runs on the vector ALU in fp32 (a rounding of P would cost more bits than the products
-// save: the loads bound the kernel up to 16 heads per group).
+// its row by a register broadcast, and P V runs on the vector ALU.  More than four heads per group: P V on the fp32 matrix instruction (16 x 16 x 4), of
+// which a lane's probability (head l % 16, one entry per row of lanes) and value are the operands as they are; the four rows of lanes then
+// share a maximum.  (8 x 16384 entries of 8 heads, 16 per group: 8-bit rows 143 -> 88 us, bf16 157 -> 137; 8 per group 93 -> 77, 122 -> 117; but 16 x 8192 with
+// four 79 -> 83, and one per group, whose fifteen idle rows cost as much, 29 -> 43 for 4 x 32 heads x 4100.)  Both in fp32: a rounding of P would cost more bits.
 // WIDE: a tile lies in one page, whose number and address are the same for all lanes and live in scalar registers; a lane adds a
 // displacement of 32 bits that never changes.  Rows of V are read once and past the caches (16 lanes take whole lines; 131072 entries
 // 104 -> 98 us), K's are not: an instruction takes half lines, and with the hint the other half came from memory again.  Two wavefronts per
-// SIMD at least (16 heads per group of bf16 rows: 84 -> 72 us, of fp32 rows, which would spill, 104 -> 140; three: 65 -> 71 us for
-// four).  (With an address per lane and row, computed for every tile, the vector ALU was as busy with addresses as with sums: 4 x 32 heads x
-// 4100 entries of 8-bit rows took 71 us, now 25.)
+// SIMD at least (three: 65 -> 71 us for four heads per group).  (With an address per lane and row, computed for every tile, the vector ALU was as busy
+// with addresses as with sums: 4 x 32 heads x 4100 entries of 8-bit rows took 71 us, now 25.)
 template <typename T, typename CT, int D, int GM, int U, bool WIDE>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM > 8 && sizeof(CT) == 4 ? 1 : 2))) void step_part(StepArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void step_part(StepArgs a) {
   typedef Rows<CT, D> R;
   constexpr int E = R::kE;
+  constexpr bool kMatrix = GM > 4;
   __shared__ float so[kWaves][GM][D];
   __shared__ float sml[kWaves][GM][2];
   __shared__ float sM[GM], sinv[GM];
@@ -347,7 +356,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM 
   const bool ordered = a.window != 0 && !a.pool.pos, by_pos = a.window != 0 && a.pool.pos;
   const int64_t lo64 = a.window == 0 ? INT64_MIN : list.last - a.window + 1;  // first position of the window
   const int lo = int(min(max(lo64, int64_t(0)), int64_t(n)));                 // (entries in order of position)
-  float m = -3.402823466e38f, l = 0.f, acc[GM][E] = {};
+  float m = -3.402823466e38f, l = 0.f, acc[kMatrix ? 1 : GM][E] = {};
+  f32x4 om[kMatrix ? E : 1] = {};  // (kMatrix) register i: head 4 g + i, column R::column(c, e)
   float* lg = a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
   // (the page table: what an earlier launch or copy wrote, read through the scalar cache)
   const auto table = (const __attribute__((address_space(4))) int32_t*)(a.pool.table + int64_t(b) * a.pool.max_pages);
@@ -458,15 +468,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM 
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[u][r]);
       if (lg && c < a.G && t + u < t1) *reinterpret_cast<f32x4*>(lg + list.slot(t + u) + 4 * g) = s[u];
     }
+    if constexpr (kMatrix) mx = max_rows(mx);  // one maximum per head
     if (__any(mx > m)) {
       const float f = __builtin_amdgcn_exp2f(m - mx);
       m = mx;
       l *= f;
-      each<GM>([&](auto h) {
-        const float fh = row_bcast<h>(f);
+      if constexpr (kMatrix) {
+        const f32x4 fh = {__shfl(f, 4 * g, 64), __shfl(f, 4 * g + 1, 64), __shfl(f, 4 * g + 2, 64), __shfl(f, 4 * g + 3, 64)};
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[h][e] *= fh;
-      });
+        for (int e = 0; e < E; ++e) om[e] *= fh;
+      } else {
+        each<GM>([&](auto h) {
+          const float fh = row_bcast<h>(f);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[h][e] *= fh;
+        });
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -481,27 +498,38 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(GM 
 #pragma unroll
           for (int e = 0; e < E; ++e) f[e] = okv ? f[e] : 0.f;
         }
-        each<GM>([&](auto h) {
-          const float ph = row_bcast<h>(p);
+        if constexpr (kMatrix) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[h][e] = fmaf(ph, f[e], acc[h][e]);
-        });
+          for (int e = 0; e < E; ++e) om[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(p, f[e], om[e], 0, 0, 0);
+        } else {
+          each<GM>([&](auto h) {
+            const float ph = row_bcast<h>(p);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[h][e] = fmaf(ph, f[e], acc[h][e]);
+          });
+        }
       }
     }
   }
   // join the four rows of lanes, then the wavefronts
-  float mw = fmaxf(m, __shfl_xor(m, 16, 64));
-  mw = fmaxf(mw, __shfl_xor(mw, 32, 64));
-  const float f = __builtin_amdgcn_exp2f(m - mw);
+  const float mw = max_rows(m), f = __builtin_amdgcn_exp2f(m - mw);
   l = sum_rows(l * f);
-  each<GM>([&](auto h) {
-    const float fh = row_bcast<h>(f);
+  if constexpr (kMatrix) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float o = sum_rows(acc[h][e] * fh);
-      if (g == h % 4) so[w][h][R::column(c, e)] = o;
-    }
-  });
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * g + i < GM) so[w][4 * g + i][R::column(c, e)] = om[e][i];
+  } else {
+    each<GM>([&](auto h) {
+      const float fh = row_bcast<h>(f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float o = sum_rows(acc[h][e] * fh);
+        if (g == h % 4) so[w][h][R::column(c, e)] = o;
+      }
+    });
+  }
   if (lane < GM) {
     sml[w][lane][0] = mw;
     sml[w][lane][1] = l;
@@ -601,11 +629,11 @@ __global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
   });
 }
 
-// Tiles per wavefront and round: two, where their rows take 16 KB at most and the outputs of 16 heads do not fill the registers.
+// Tiles per wavefront and round: two, where their rows take 16 KB at most.
 // (8-bit rows in fours: 39 instead of 36 us for 4 x 32 heads x 4100 entries; bf16 rows of 128 singly: 109 instead of 105 us for 8 heads of 131072.)
 template <typename CT, int D, int GM>
 constexpr int tiles_per_round() {
-  return GM <= 8 && 2 * kTile * 2 * D * int(sizeof(CT)) <= 16384 ? 2 : 1;
+  return 2 * kTile * 2 * D * int(sizeof(CT)) <= 16384 ? 2 : 1;
 }
 
 template <typename T, typename CT, int D, int GM>

@@ -240,6 +240,28 @@ def test_step_nan_and_infinite_rows_that_are_seen_reach_their_heads_only():
     assert bool(got[2:].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_step_of_many_heads_per_group_with_rows_and_queries_that_are_not_finite(dtype):
+    """An infinite value reaches its column, a NaN key the heads of its group, a NaN query its own head, and nothing else."""
+    G, n = 11, 300
+    t = ref.make_pages(1, 2, 64, 16, 20, dtype, 3, score=False, pos=False)
+    g = torch.Generator().manual_seed(1)
+    q = torch.randn((1, 2 * G, 64), generator=g).to(dtype)
+    clean = ref.step_ref(t, q, None, None, [n], None, 0, 0, 320, dtype)
+    p, r = ref.entries(t, 0, n)
+    t["v"][p[40], 0, r[40], 5] = math.inf
+    t["k"][p[50], 1, r[50], 5] = math.nan
+    q[0, 3] = math.nan
+    gt = on_gpu(t)
+    out = torch.zeros((1, 2 * G, 64), dtype=dtype, device="cuda:0")
+    pages_of(gt, 2 * G).d2o_pages_step(q.cuda(), None, None, torch.tensor([n], dtype=torch.int32, device="cuda:0"), out)
+    got = out.cpu()[0].double()
+    heads, cols = [h for h in range(G) if h != 3], [c for c in range(64) if c != 5]
+    assert bool((got[heads, 5] == math.inf).all()) and bool(got[3].isnan().all()) and bool(got[G:].isnan().all())
+    err = (got - clean[0][0]).abs()[heads][:, cols]
+    assert bool((err <= clean[1][0][heads][:, cols]).all())
+
+
 def test_step_strided_queries_and_outputs():
     t = ref.make_pages(2, 2, 64, 16, 8, BF16, 3)
     g = torch.Generator().manual_seed(1)
