@@ -100,6 +100,11 @@ struct TileList {
   }
   __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
   __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }
+  // Whether the window shows entry s, whose position is `pos` where the pages keep positions.
+  __device__ __forceinline__ bool sees(const StepArgs& a, int s, int32_t pos) const {
+    const int p = a.pool.pos ? pos : s;
+    return a.window == 0 || p > last - a.window || p < a.n_sink;
+  }
 };
 
 template <int L>
@@ -273,6 +278,8 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
   int s[N], page[N];
   float x[GM][N], old[N];
   int64_t at[N];
+  int32_t pos[N] = {};
+  const bool by_pos = a.window != 0 && a.pool.pos;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int i = i0 + u * step;
@@ -289,6 +296,7 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
   for (int u = 0; u < N; ++u) {
     at[u] = page[u] >= 0 ? a.pool.at(page[u], hk, s[u]) : 0;
     old[u] = a.pool.score[at[u]];
+    if (by_pos) pos[u] = a.pool.pos[at[u]];
   }
   totals();
   float add[N] = {};
@@ -298,10 +306,10 @@ __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& li
 #pragma unroll
       for (int u = 0; u < N; ++u) add[u] += __builtin_amdgcn_exp2f(x[h][u] - M[h]) * inv[h];
     }
-  // (an entry that is not seen has logits of -infinity and gets nothing; NaN is added)
+  // (only what is seen: the logit of -infinity of an entry that is not would become NaN beside a NaN or an infinity of its head)
 #pragma unroll
   for (int u = 0; u < N; ++u)
-    if (page[u] >= 0 && add[u] != 0.f) a.pool.score[at[u]] = old[u] + add[u];
+    if (page[u] >= 0 && list.sees(a, s[u], pos[u]) && add[u] != 0.f) a.pool.score[at[u]] = old[u] + add[u];
 }
 
 // One workgroup per (sequence, KV head, share of its tiles).  U tiles of 16 entries per wavefront and round: the logits of all
