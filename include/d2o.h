@@ -386,7 +386,7 @@ int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, co
  * [B], NULL: lens[b] - 1.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
  * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
  * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry (or only
- * logits of minus infinity).
+ * logits of minus infinity).  Values may be as large as their type allows; a weight below 2^-126 times twice the entries of the largest may count as zero.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_len beyond the page table, workspace too small), HIP. */
 int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view v_new, const int32_t* lens,
                    const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,

@@ -66,7 +66,7 @@ struct StepArgs {
   const int32_t* positions;
   float* logits;   // [B][Hq][pad] base-2 logits of the entries that are seen (scores kept)
   float* part_o;   // [B * Hkv][splits][G][D] outputs of a share, not normalised
-  float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum
+  float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum (outputs and sums: times 2^-TileList::bias)
   int32_t Hq, G, max_len, window, n_sink, pad, splits, joins;  // joins: workgroups of step_finish that join outputs
 };
 
@@ -75,14 +75,16 @@ struct StepArgs {
 struct TileList {
   int n, sink_tiles, rest0, tiles, share;  // entries, tiles of the first tokens, first tile behind them, tiles in all, tiles per workgroup
   int64_t last;                            // the new token's position
+  int bias;                                // n < 2^bias
   __device__ __forceinline__ TileList(const StepArgs& a, int b, int least) {
     n = min(a.lens[b], a.max_len);
     if (n <= 0) {
-      n = tiles = share = sink_tiles = rest0 = 0;
+      n = tiles = share = sink_tiles = rest0 = bias = 0;
       last = 0;
       return;
     }
     last = a.positions ? a.positions[b] : n - 1;
+    bias = 32 - __clz(n);
     const int all = (n + kTile - 1) / kTile;
     sink_tiles = rest0 = 0;
     if (a.window != 0 && !a.pool.pos) {
@@ -270,7 +272,7 @@ __device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int 
 
 // Adds the softmax rows of a (sequence, KV head) to the scores of entries i0, i0 + step, .. (in the order of the tiles) below `end`, N of them
 // (Eq. 6); the group's query heads in rising order.  What is read - logits, pages, old scores - is on its way before `totals` forms M and
-// inv, maximum and reciprocal sum of each head.
+// inv, maximum and reciprocal sum (of exp2(x - M)) of each head.
 template <int N, int GM, typename F>
 __device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& list, int b, int hk, int i0, int step, int end,
                                            const float* M, const float* inv, const F& totals) {
@@ -364,6 +366,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   const bool ordered = a.window != 0 && !a.pool.pos, by_pos = a.window != 0 && a.pool.pos;
   const int64_t lo64 = a.window == 0 ? INT64_MIN : list.last - a.window + 1;  // first position of the window
   const int lo = int(min(max(lo64, int64_t(0)), int64_t(n)));                 // (entries in order of position)
+  // Probabilities are formed as 2^-bias * p, so that no sum of them is above one and P V never above the largest value.  (What is 2^(126 - bias)
+  // below a head's highest entry is zero.)
+  const float bias = list.bias;
   float m = -3.402823466e38f, l = 0.f, acc[kMatrix ? 1 : GM][E] = {};
   f32x4 om[kMatrix ? E : 1] = {};  // (kMatrix) register i: head 4 g + i, column R::column(c, e)
   float* lg = a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
@@ -497,7 +502,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(s[u][r] - m);
+        const float p = __builtin_amdgcn_exp2f((s[u][r] - m) - bias);
         l += p;
         float f[E];
         R::values(v[u][r], ve[u][r], f);
@@ -565,7 +570,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     if (col == 0) {
       if (single) {
         sM[h] = M;
-        sinv[h] = L == 0.f ? 0.f : 1.f / L;
+        sinv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
       } else {
         a.part_ml[at * 2] = M;
         a.part_ml[at * 2 + 1] = L;
@@ -630,7 +635,7 @@ __global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
       total(a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2, ns, M, L);
       if (lane == 0) {
         sM[h] = M;
-        sinv[h] = L == 0.f ? 0.f : 1.f / L;
+        sinv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
       }
     }
     __syncthreads();
