@@ -20,6 +20,7 @@ struct WindowArgs {
   View q, k, v, o;
   const int32_t* lens;
   int32_t n, Hq, G, window, n_sink;  // window and n_sink: at most n; window: at least 1
+  float bias;  // a row sees fewer than 2^bias keys
   // bf16: transposed values and a record per tile of 64 keys
   uint16_t* vt;  // [B][Hkv][tiles][D][64] fp16, every group of eight keys scaled by a power of two of its own
   float* rec;    // [B][Hkv][tiles][kRec]: exponents of the groups (of the even ones, then of the odd ones), a flag
@@ -522,6 +523,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // Four wavefronts of 16 query rows, tiles of 32 keys, all products on the fp32 matrix instruction (16 x 16 x 4): S^T of 16 keys
 // leaves the four keys 4 g + r in register r of lane row g, and register r is the operand of the product whose V rows are
 // 4 g + r.  Tiles pass through registers on their way to LDS; an infinity or NaN of V counts as zero there and is added at the end.
+// Probabilities are formed as 2^-bias * p: no sum of them is above one, and P V never above the largest value.
 template <int D>
 __global__ __launch_bounds__(256) void window_f32(WindowArgs a) {
   constexpr int BN = 32, BM = 64, kLd = D + 4, kLoads = BN * D / 4 / 256;
@@ -610,7 +612,7 @@ __global__ __launch_bounds__(256) void window_f32(WindowArgs a) {
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(s[r] - m);
+        const float p = __builtin_amdgcn_exp2f((s[r] - m) - a.bias);
         l += p;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
@@ -709,7 +711,7 @@ __global__ __launch_bounds__(256) void window_f32_few(WindowArgs a) {
     for (int i = 0; i < kI; ++i) o[i] *= f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float p = __builtin_amdgcn_exp2f(s[r] - m);
+      const float p = __builtin_amdgcn_exp2f((s[r] - m) - a.bias);
       l += p;
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
@@ -833,6 +835,7 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   a.G = n_q_heads / n_kv_heads;
   a.window = window == 0 || window > n ? n : window;
   a.n_sink = std::min(n_sink, n);
+  a.bias = float(32 - __builtin_clz(unsigned(std::min<int64_t>(n, int64_t(a.window) + a.n_sink))));
   a.tiles = (n + 63) / 64;
   a.reverse = a.window > n / 2;
   const hipStream_t s = static_cast<hipStream_t>(stream);

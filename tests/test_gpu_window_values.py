@@ -1,0 +1,110 @@
+"""Windowed prompt attention of values whose magnitudes differ: by element, column, token and tile, up to the largest number of
+the type.  Every element is held to a bound that is relative to what its row sees in its own column, sum_j p_j |v_jc|."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_13035_amd import binding
+
+from . import pages_ref as ref
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+FORMS = [  # a case for every kernel: dtype, d, heads, n, window, n_sink
+    (F32, 64, (2, 1), 300, 90, 2), (F32, 128, (24, 4), 700, 300, 70), (F32, 64, (2, 1), 300, 0, 0), (F32, 64, (60, 60), 700, 0, 0),
+]
+form = pytest.mark.parametrize("dtype,d,heads,n,window,n_sink", FORMS, ids=str)
+
+
+def inputs(dtype, heads, n, d, seed, flat=False):
+    g = torch.Generator().manual_seed(seed)
+    Q, K, V = ((torch.randn((1, h, n, d), generator=g) * s).to(dtype) for h, s in ((heads[0], 0.0 if flat else 1.5), (heads[1], 1), (heads[1], 1)))
+    return Q, K, V, g
+
+
+def run(Q, K, V, window, n_sink):
+    O = binding.d2o_window_attend(Q.cuda(), K.cuda(), V.cuda(), window, n_sink)
+    torch.cuda.synchronize()
+    return O.cpu()
+
+
+def bound(q, k, v, seen, o, p, dtype):
+    """Logits: fp32 sums of d products, (d + 3) half steps of 2^-24 of the sum of their magnitudes; exponentials 2^-22 and the argument's
+    rounding; sums of as many terms as a row sees; all of it in the numerator and in the normaliser.  bf16: probabilities in two bf16
+    terms, whose second is rounded by half a step of a number below 2^-8 of the first: 2^-16.  The output is rounded once.  Last, fp32 products below
+    its normal numbers, of probabilities divided by up to 32 times the terms."""
+    d, n = q.shape[-1], int(seen.sum(-1).max())
+    mag = (q.abs() @ k.abs().transpose(-1, -2)) / math.sqrt(d)
+    mag = torch.where(seen, mag, torch.zeros_like(mag)).amax(-1, keepdim=True)
+    rel = 2 * (mag * (d + 3) * 2.0 ** -24 + mag * 2.0 ** -22 + 2.0 ** -22 + n * 2.0 ** -24) + (2.0 ** -16 if dtype == BF16 else 0)
+    return p @ v.abs() * rel + o.abs() * ref.HALF_STEP[dtype] + 32.0 * n * n * 2.0 ** -149
+
+
+def check(Q, K, V, O, window, n_sink):
+    Hq, n = Q.shape[1:3]
+    G, seen = Hq // K.shape[1], ref.window_seen(n, window, n_sink)
+    for h in sorted({0, Hq // 2, Hq - 1}):
+        q, k, v = (x[0, i].double() for x, i in ((Q, h), (K, h // G), (V, h // G)))
+        o, p = ref.attend64(q, k, v, seen)
+        err = (O[0, h].double() - o).abs()
+        worst = err / bound(q, k, v, seen, o, p, Q.dtype)
+        assert bool((worst <= 1).all()), (h, float(worst.max()), [int(x) for x in (worst == worst.max()).nonzero()[0]])
+
+
+@pytest.mark.parametrize("power", [20, 30, 40, 127])
+@form
+def test_one_element_far_above_the_others(dtype, d, heads, n, window, n_sink, power):
+    Q, K, V, _ = inputs(dtype, heads, n, d, power)
+    V[0, :, 1, 3] = V[0, :, 75, 5] = 2.0 ** power
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("power", [20, 30, 40, 100])
+@form
+def test_one_column_far_above_the_others(dtype, d, heads, n, window, n_sink, power):
+    Q, K, V, _ = inputs(dtype, heads, n, d, power)
+    V[..., 7] = torch.ldexp(V[..., 7].float(), torch.tensor(power)).to(dtype)
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@form
+def test_columns_and_tokens_of_any_magnitude(dtype, d, heads, n, window, n_sink):
+    Q, K, V, g = inputs(dtype, heads, n, d, 1)
+    e = torch.randint(-50, 51, (1, 1, n, 1), generator=g) + torch.randint(-40, 41, (1, 1, 1, d), generator=g)
+    V = torch.ldexp(V.float(), e).to(dtype)
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@form
+def test_a_window_of_one_token_gives_its_values(dtype, d, heads, n, window, n_sink):
+    """In bf16 as they are; in fp32 but for the product with the weight and the division by it."""
+    Q, K, V, g = inputs(dtype, heads, n, d, 2)
+    V = torch.ldexp(V.float(), torch.randint(-90, 91, (1, 1, n, 1), generator=g) + torch.randint(-20, 21, (1, 1, 1, d), generator=g)).to(dtype)
+    O, want = run(Q, K, V, 1, 0), V.repeat_interleave(heads[0] // heads[1], 1)
+    if dtype == BF16:
+        assert torch.equal(O, want)
+    else:
+        assert bool(((O.double() - want.double()).abs() <= want.double().abs() * 4 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("first,later", [(1e28, 0.0), (3e38, 0.0), (1e30, 1e-10), (0.0, 1e-25), (0.0, 1e-33), (1e-25, 0.0), (1e-20, 1e20)], ids=str)
+@pytest.mark.parametrize("flat", [True, False], ids=["equal", "random"])
+@form
+def test_runs_of_tokens_of_one_magnitude(dtype, d, heads, n, window, n_sink, first, later, flat):
+    """The first 64 tokens, and those from 200 on, of one, the others of the other: the weights do not depend on either."""
+    Q, K, V, _ = inputs(dtype, heads, n, d, 3, flat)
+    big = torch.zeros(n, dtype=torch.bool)
+    big[:64] = big[200:] = True
+    V = torch.where(big[:, None], V.sign().float() * first, V.sign().float() * later).to(dtype)
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("flat", [True, False], ids=["equal", "random"])
+@form
+def test_values_near_the_largest_number(dtype, d, heads, n, window, n_sink, flat):
+    """A mean is no larger than what it is taken of, however many there are."""
+    Q, K, V, _ = inputs(dtype, heads, n, d, 4, flat)
+    V[:] = 3e38
+    V[..., ::2] = -3e38
+    check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
