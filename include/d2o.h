@@ -333,7 +333,10 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * O = softmax(Q K^T / sqrt(d)) V over those.  window = 0: no window (every j <= i).
  * Q, O: [B][Hq][n][d]; K, V: [B][Hkv][n][d]; O in `dtype`.  lens: device [B], the tokens of each sequence
  * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
- * its keys behind the end take no part.  An infinity or NaN in V reaches the rows that see it, whatever its weight, and no others.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16, d = 64 or 128, any Hq / Hkv.  Errors:
+ * its keys behind the end take no part.  An infinity or NaN in V reaches the rows that see it, whatever its weight, and no others.
+ * Finite values may be of any magnitude, side by side; a weight holds 24 bits (D2O_BF16: 16), sums 24, and a weight below 2^-126 times sixteen times the
+ * keys that a row sees, relative to the row's largest, may count as zero.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16,
+ * d = 64 or 128, any Hq / Hkv.  Errors:
  * INVALID_ARG, UNSUPPORTED (also a row stride of K of 2^24 elements or more), CAPACITY (workspace smaller than
  * d2o_window_workspace_bytes says; where it says 0, NULL will do), HIP. */
 int d2o_window_workspace_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,

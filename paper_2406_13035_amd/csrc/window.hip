@@ -13,6 +13,7 @@
 namespace d2o {
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -3e38f;  // exponent reference before a row has seen a key
 
@@ -21,12 +22,11 @@ struct WindowArgs {
   const int32_t* lens;
   int32_t n, Hq, G, window, n_sink;  // window and n_sink: at most n; window: at least 1
   float bias;  // a row sees fewer than 2^bias keys
-  // bf16: transposed values and a record per tile of 64 keys
-  uint16_t* vt;  // [B][Hkv][tiles][D][64] fp16, every group of eight keys scaled by a power of two of its own
-  float* rec;    // [B][Hkv][tiles][kRec]: exponents of the groups (of the even ones, then of the odd ones), a flag
+  // bf16: transposed values and a flag per tile of 64 keys
+  uint16_t* vt;  // [B][Hkv][tiles][D][64], infinities and NaN as zero
+  float* odd;    // [B][Hkv][tiles] 1 where the tile had any
   int32_t tiles, blocks, reverse, share;  // share: log2 of the query heads of a block
 };
-constexpr int kRec = 16;  // floats per record
 
 // The tiles of BN keys that the rows [r0, r1] see: `sinks` tiles of first tokens, then those from `rest0`.
 struct Tiles {
@@ -55,7 +55,7 @@ __device__ __forceinline__ bool all_seen(const WindowArgs& a, int r0, int r1, in
 }
 
 // A block's rows are those of BM / 2^share tokens and 2^share query heads of a group, wavefront by wavefront: the heads share K and V, and fewer
-// tokens see fewer tiles (8192 tokens, 32 heads on 8, window 1024: 220 -> 201 us).
+// tokens see fewer tiles (8192 tokens, 32 heads on 8, window 1024: 249 -> 226 us).
 // Workgroup number -> (block of rows, heads and sequence).  Workgroups go to the chip's eight XCDs, each with an L2 of its own, in
 // turn; here each XCD gets a contiguous run of (head, block), so that blocks that share most of their window meet in one L2.
 // Without a window (reverse) the work grows with the block's position: the longest blocks of all heads first.
@@ -82,11 +82,11 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 }
 
 // ---- bf16 ----------------------------------------------------------------------------------
-// The product with V runs in fp16: probabilities rounded to bf16 would cost 2^-8 each, as much as the output's own rounding; in
-// fp16 they cost 2^-11.  V is converted once, in a transposing pass, each group of eight keys divided by a power of two 2^e that
-// brings its largest magnitude to [2^13, 2^14) (exact: bf16 has eight significant bits), and the probabilities of the group
-// are multiplied by 2^e in the exponent.  (One e for the head would lose rows whose window holds small values
-// only.)  A group less than 2^12 below its tile's largest keeps the tile's e, so that nearly every tile has one e.  Infinities and NaN of V count as zero here and are added to the rows that see them at the end.
+// V goes to the matrix core as it is, in bf16, and a probability as the sum of two bf16 terms, p rounded and what that left of it, which hold
+// sixteen bits: 2^-17 of p, where one bf16 term would cost 2^-8, as much as the output's own rounding, and one fp16 term 2^-11.  (fp16 also needs
+// V brought into its range by powers of two, which no scaling per tile does for values that differ by more than 2^30.)  P V thus takes two
+// products per operand read from LDS (32 heads x 32768 tokens, window 4096: 2.28 ms with the first term alone, 2.96 with both).  An infinity or
+// NaN of V would reach rows that do not see it (0 x inf): it counts as zero here and is added to the rows that see it at the end.
 
 constexpr int kGroupLd = 512 + 32;  // LDS elements from one group of rows (1 KB, one load instruction) to the next
 // A tile's rows of 256 (128) bytes lie four (eight) to a group; chunk k (16 bytes) of a row sits at k ^ x within its four, x from the row:
@@ -95,76 +95,43 @@ __device__ __forceinline__ int swz(int chunk, int x) { return ((chunk & ~3) << 3
 __device__ __forceinline__ int at256(int row, int chunk) { return (row >> 2) * kGroupLd + (row & 3) * 128 + swz(chunk, row & 3); }
 __device__ __forceinline__ int at128(int row, int chunk) { return (row >> 3) * kGroupLd + (row & 7) * 64 + swz(chunk, (row >> 1) & 3); }
 
-constexpr float kPShift = 12.f;  // probabilities are formed as 2^12 * p before the fp16 rounding
-constexpr float kLazy = 3.f;     // log2 of the growth the exponent reference tolerates before it moves
-constexpr float kFar = 1048576.f;  // exponents whose spacing, 1/8 and more, could let 2^12 * p leave fp16
+constexpr float kLazy = 3.f;       // log2 of the growth the exponent reference tolerates before it moves
+constexpr float kFar = 1048576.f;  // exponents whose spacing, 1/8 and more, would blur the reference
 
 // MFMA row -> key offset inside 32 keys, such that accumulator registers 8 kb .. 8 kb + 7 of lane half h hold the keys 16 kb + 8 h .. + 7.
 __device__ __forceinline__ int perm_key(int m) { return (m & ~0xC) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
-// V [b][h][n][D] -> vt and rec.  One workgroup per tile.
+// V [b][h][n][D] -> vt and odd.  One workgroup per tile.
 template <int D>
 __global__ __launch_bounds__(256) void window_values(WindowArgs a) {
   __shared__ uint16_t t[64][D + 2];
-  __shared__ uint32_t top[8];
   __shared__ int odd;
   const int tile = blockIdx.x, Hkv = a.Hq / a.G, bh = blockIdx.y, b = bh / Hkv, hk = bh % Hkv, tid = threadIdx.x;
   const int n = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
   if (tile * 64 >= n) return;
   constexpr int kChunks = D / 8, kRows = 256 / kChunks, kRound = 64 / kRows;  // chunks per row, rows per round, rounds
   const uint16_t* src = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
-  if (tid < 8) top[tid] = 0;
-  if (tid == 8) odd = 0;
+  if (tid == 0) odd = 0;
   u32x4 v[kRound];
-  uint32_t m[kRound];
   bool bad = false;
 #pragma unroll
   for (int u = 0; u < kRound; ++u) {
     const int row = u * kRows + tid / kChunks, col = tid % kChunks * 8;
     v[u] = u32x4{0, 0, 0, 0};
     if (tile * 64 + row < n) v[u] = *reinterpret_cast<const u32x4*>(src + int64_t(tile * 64 + row) * a.v.sn + col);
-    m[u] = 0;
+  }
+#pragma unroll
+  for (int u = 0; u < kRound; ++u) {
+    const int row = u * kRows + tid / kChunks, col = tid % kChunks * 8;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if ((v[u][i] & 0x7F800000u) == 0x7F800000u) v[u][i] &= 0x0000FFFFu, bad = true;
       if ((v[u][i] & 0x7F80u) == 0x7F80u) v[u][i] &= 0xFFFF0000u, bad = true;
-      m[u] = max(m[u], max(v[u][i] & 0x7FFF0000u, v[u][i] << 16 & 0x7FFF0000u));
+      *reinterpret_cast<uint32_t*>(&t[row][col + 2 * i]) = v[u][i];
     }
-    // the lanes of eight rows: at most a wavefront
-#pragma unroll
-    for (int o = 1; o < kChunks; o <<= 1) m[u] = max(m[u], uint32_t(__shfl_xor(int(m[u]), o, 64)));
   }
   __syncthreads();
-#pragma unroll
-  for (int u = 0; u < kRound; ++u)
-    if (tid % kChunks == 0) atomicMax(&top[(u * kRows + tid / kChunks) / 8], m[u]);
   if (bad) odd = 1;
-  __syncthreads();
-  uint32_t all = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) all = max(all, top[i]);
-  // Exponent of the largest magnitude, brought to 13 (biased exponents; subnormal values count as the lowest).  A tile of zeros: low, so that
-  // its keys, however heavy, do not push the probabilities of others out of fp16, and not so low that their own leave fp32.
-  auto exponent = [](uint32_t bits) { return max(int(bits >> 23), 1) - 127 - 13; };
-  const int e_tile = all ? exponent(all) : -60;
-  auto group_exponent = [&](int gr) __attribute__((always_inline)) {
-    const int e = top[gr] ? exponent(top[gr]) : e_tile;
-    return e < e_tile - 12 ? e : e_tile;
-  };
-  float* rec = a.rec + (int64_t(bh) * a.tiles + tile) * kRec;
-  if (tid < 8) rec[(tid & 1) * 4 + tid / 2] = float(group_exponent(tid));
-  if (tid == 8) rec[8] = odd ? 1.f : 0.f;
-#pragma unroll
-  for (int u = 0; u < kRound; ++u) {
-    const int row = u * kRows + tid / kChunks, col = tid % kChunks * 8, e = group_exponent(row / 8);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const _Float16 lo = (_Float16)ldexpf(__uint_as_float(v[u][i] << 16), -e);
-      const _Float16 hi = (_Float16)ldexpf(__uint_as_float(v[u][i] & 0xFFFF0000u), -e);
-      *reinterpret_cast<uint32_t*>(&t[row][col + 2 * i]) = __builtin_bit_cast(uint16_t, lo) | uint32_t(__builtin_bit_cast(uint16_t, hi)) << 16;
-    }
-  }
-  __syncthreads();
   uint16_t* dst = a.vt + (int64_t(bh) * a.tiles + tile) * D * 64;
   for (int c = tid; c < D * 8; c += 256) {
     const int dd = c >> 3, kc = (c & 7) * 8;
@@ -173,6 +140,8 @@ __global__ __launch_bounds__(256) void window_values(WindowArgs a) {
     for (int i = 0; i < 4; ++i) o[i] = t[kc + 2 * i][dd] | uint32_t(t[kc + 2 * i + 1][dd]) << 16;
     *reinterpret_cast<u32x4*>(dst + dd * 64 + kc) = o;
   }
+  __syncthreads();
+  if (tid == 0) a.odd[int64_t(bh) * a.tiles + tile] = odd ? 1.f : 0.f;
 }
 
 template <int D>
@@ -204,7 +173,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const uint16_t* kbase = static_cast<const uint16_t*>(a.k.ptr) + b * a.k.sb + hk * a.k.sh;
   const int64_t vt0 = (int64_t(b) * Hkv + hk) * a.tiles;
   const uint16_t* vtbase = a.vt + vt0 * D * 64;
-  const float* rec = a.rec + vt0 * kRec;
+  const float* odd = a.odd + vt0;
   // A tile of K is 64 rows of 2 D bytes, one of V^T D rows of 128 bytes; an instruction brings 1 KB.  Through buffer descriptors: rows
   // behind the prompt's end read as zero, a lane's displacement never changes, and the compiler lets the LDS reads of the products
   // return one by one while such loads are on their way (behind global_load_lds, which counts as a flat access, it waits for all).
@@ -241,29 +210,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
   if (!SPLIT || ntile > 0) load_v(0);
   if (ntile > 1) load_k(1);
-  auto exps_of = [&](int t) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(rec + int64_t(tile_of(t)) * kRec + h * 4); };
-  auto flag_of = [&](int t) __attribute__((always_inline)) { return rec[int64_t(tile_of(t)) * kRec + 8]; };
-  f32x4 ex = {0.f, 0.f, 0.f, 0.f}, ex_next;
   float flag = 0.f, flag_next = 0.f;
-  if (!SPLIT || ntile > 0) {
-    ex = exps_of(0);
-    flag_next = flag_of(0);
-  }
-  ex_next = ex;
+  if (!SPLIT || ntile > 0) flag_next = odd[tile_of(0)];
 
   f32x16 o[kDC];
 #pragma unroll
   for (int i = 0; i < kDC; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
-  // mrun: exponent reference of o; el: the sum is kept relative to mrun - el
-  float mrun = kFloor, el = 0.f, lsum = 0.f;
+  // mrun: exponent reference of o and lsum, at least `shift` - kLazy = a.bias above the row's maximum: no sum of probabilities is above one, and P V
+  // never above the largest value
+  const float shift = a.bias + kLazy;
+  float mrun = kFloor, lsum = 0.f;
   // A row whose maximum lies beyond kFar has `away`, that maximum or an earlier one, taken from its logits first: what follows sees small numbers.
-  // (Looking for such rows takes 1 to 2.5%: 32768 tokens 2.46 -> 2.49 ms.)
+  // (Looking for such rows takes about 1%: 32768 tokens, window 4096 2.91 -> 2.96 ms.)
   float away = 0.f;  // as an exponent; 0: not such a row
   bool far = false;  // the wavefront has such rows
   f32x16 s[2];
-  f16x8 pb[2][2];
+  bf16x8 pb[2][2][2];  // sub-tile, half, term
   auto active = [&](int t) __attribute__((always_inline)) {
     const int k0 = tile_of(t) * 64;
     return any_seen(a, wr0, wr0 + 31, k0, k0 + 63);
@@ -288,15 +252,22 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[st][r] = is ? (s[st][r] * scale2 - away) * unscale : s[st][r];
   };
-  // probabilities of one group of eight registers (sub-tile st, half kb) with exponent reference c
-  auto form = [&](int st, int kb, float c) __attribute__((always_inline)) {
+  // probabilities of one group of eight registers (sub-tile st, half kb)
+  auto form = [&](int st, int kb) __attribute__((always_inline)) {
     float sum = 0.f;
+    u32x4 hi, lo;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(s[st][8 * kb + r], scale2, -c));
-      sum += p;
-      pb[st][kb][r] = (_Float16)p;
+    for (int r = 0; r < 8; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[st][8 * kb + r], scale2, -mrun)), p1 = __builtin_amdgcn_exp2f(fmaf(s[st][8 * kb + r + 1], scale2, -mrun));
+      sum += p0;
+      sum += p1;
+      uint32_t x = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
+      asm("" : "+v"(x));  // (one conversion of both, of which the compiler would make a third of p0 alone)
+      hi[r / 2] = x;
+      lo[r / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(p0 - __uint_as_float(x << 16)), (__bf16)(p1 - __uint_as_float(x & 0xFFFF0000u))});
     }
+    pb[st][kb][0] = __builtin_bit_cast(bf16x8, hi);
+    pb[st][kb][1] = __builtin_bit_cast(bf16x8, lo);
     return sum;
   };
   auto softmax = [&](int t) __attribute__((always_inline)) {
@@ -331,26 +302,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
     }
     if (__builtin_expect(far, false)) take_away([&](float x) { return away != 0.f && x > away + kFar; }, [&] { return away != 0.f; });
-    const float e0 = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(ex[0])));
-    const bool one = __all(ex[0] == e0 && ex[1] == e0 && ex[2] == e0 && ex[3] == e0);
     auto reference = [&]() __attribute__((always_inline)) {  // that the tile asks for
-      float mx[4];
+      float x = s[0][0];
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          float x = s[st][8 * kb];
-#pragma unroll
-          for (int r = 1; r < 8; ++r) x = fmaxf(x, s[st][8 * kb + r]);
-          mx[st * 2 + kb] = x;
-        }
-      float top;
-      if (one)
-        top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), scale2, e0);
-      else
-        top = fmaxf(fmaxf(fmaf(mx[0], scale2, ex[0]), fmaf(mx[1], scale2, ex[1])),
-                    fmaxf(fmaf(mx[2], scale2, ex[2]), fmaf(mx[3], scale2, ex[3])));
-      return max_halves(top) - kPShift;
+        for (int r = 0; r < 16; ++r) x = fmaxf(x, s[st][r]);
+      return fmaf(max_halves(x), scale2, shift);
     };
     float cand = reference();
     bool grew = cand > mrun + kLazy;
@@ -362,27 +320,20 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         cand = reference();
         grew = cand > mrun + kLazy;
       }
-      const float mnew = grew ? cand : mrun, enew = grew ? e0 : el;
+      const float mnew = grew ? cand : mrun;
       const float f = __builtin_amdgcn_exp2f(mrun - mnew);
-      lsum *= __builtin_amdgcn_exp2f((mrun - mnew) - (el - enew));
+      lsum *= f;
       mrun = mnew;
-      el = enew;
 #pragma unroll
       for (int i = 0; i < kDC; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] *= f;
     }
-    if (one) {
-      const float c = mrun - e0;
-      float sum = form(0, 0, c);
-      sum += form(0, 1, c);
-      sum += form(1, 0, c);
-      sum += form(1, 1, c);
-      lsum += ldexpf(sum, int(el - e0));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) lsum += ldexpf(form(i >> 1, i & 1, mrun - ex[i]), int(el - ex[i]));
-    }
+    float sum = form(0, 0);
+    sum += form(0, 1);
+    sum += form(1, 0);
+    sum += form(1, 1);
+    lsum += sum;
   };
   // o += V^T P^T of tile t, then S^T = K Q^T of tile t + 1; LDS operands are fetched two batches of four ahead
   constexpr int kPV = 4 * kDC, kQK = 2 * kKS;
@@ -395,12 +346,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int st = (idx - kPV) & 1, ks = (idx - kPV) >> 1, row = st * 32 + m, chunk = ks * 2 + h;
     return *reinterpret_cast<const u32x4*>(&Ks[((t + 1) & 1) * kElems + (D == 128 ? at256(row, chunk) : at128(row, chunk))]);
   };
-  auto issue = [&](auto i, const u32x4& x) __attribute__((always_inline)) {
+  auto issue = [&](auto i, auto term, const u32x4& x) __attribute__((always_inline)) {
     constexpr int idx = decltype(i)::value;
     if constexpr (idx < kPV) {
       constexpr int st = idx / (2 * kDC), kb = idx / kDC % 2, dc = idx % kDC;
-      o[dc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), pb[st][kb], o[dc], 0, 0, 0);
-    } else {
+      o[dc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb[st][kb][term], o[dc], 0, 0, 0);
+    } else if constexpr (term == 0) {
       constexpr int st = (idx - kPV) & 1, ks = (idx - kPV) >> 1;
       const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       s[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), bq[ks], ks == 0 ? zero : s[st], 0, 0, 0);
@@ -412,7 +363,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     each<8>([&](auto i) { A[i / 4][i % 4] = operand(t, std::integral_constant<int, i0 + i>{}); });
     each<NB>([&](auto bt) {
       __builtin_amdgcn_sched_barrier(0);
-      each<4>([&](auto i) { issue(std::integral_constant<int, i0 + 4 * bt + i>{}, A[bt & 1][i]); });
+      each<2>([&](auto term) { each<4>([&](auto i) { issue(std::integral_constant<int, i0 + 4 * bt + i>{}, term, A[bt & 1][i]); }); });
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (bt + 2 < NB)
         each<4>([&](auto i) { A[bt & 1][i] = operand(t, std::integral_constant<int, i0 + 4 * (bt + 2) + i>{}); });
@@ -444,13 +395,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       if (t + 2 < ntile) load_k(t + 2);
       if (more) {
         load_v(t + 1);
-        ex_next = exps_of(t + 1);
-        flag_next = flag_of(t + 1);
+        flag_next = odd[tile_of(t + 1)];
       }
     }
     if (late && now) softmax(t);
     matrix(t, now, next);
-    ex = ex_next;
     if (!late && next) softmax(t + 1);
     now = next;
     wait_vm<0>();  // this wavefront's part of the next tiles is in LDS
@@ -459,23 +408,21 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
   if constexpr (SPLIT) {
     // the second half's rows to LDS (the tiles are done with), the first half adds them to its own
-    float* os = reinterpret_cast<float*>(smem) + ws * (kDC * 16 + 5) * 64 + lane;
+    float* os = reinterpret_cast<float*>(smem) + ws * (kDC * 16 + 4) * 64 + lane;
     if (half) {
       each<kDC>([&](auto dc) { each<16>([&](auto r) { os[(dc * 16 + r) * 64] = o[dc][decltype(r)::value]; }); });
       os[kDC * 16 * 64] = mrun;
-      os[(kDC * 16 + 1) * 64] = el;
-      os[(kDC * 16 + 2) * 64] = lsum;
-      os[(kDC * 16 + 3) * 64] = flag;
-      os[(kDC * 16 + 4) * 64] = away;
+      os[(kDC * 16 + 1) * 64] = lsum;
+      os[(kDC * 16 + 2) * 64] = flag;
+      os[(kDC * 16 + 3) * 64] = away;
     }
     __syncthreads();
     if (half) return;
-    const float m1 = os[kDC * 16 * 64] == kFloor ? kFloor : os[kDC * 16 * 64] + (os[(kDC * 16 + 4) * 64] - away), el1 = os[(kDC * 16 + 1) * 64], l1 = os[(kDC * 16 + 2) * 64];
-    flag = fmaxf(flag, os[(kDC * 16 + 3) * 64]);
-    const float M = fmaxf(mrun, m1), E = mrun >= m1 ? el : el1;
+    const float m1 = os[kDC * 16 * 64] == kFloor ? kFloor : os[kDC * 16 * 64] + (os[(kDC * 16 + 3) * 64] - away), l1 = os[(kDC * 16 + 1) * 64];
+    flag = fmaxf(flag, os[(kDC * 16 + 2) * 64]);
+    const float M = fmaxf(mrun, m1);
     const float f0 = __builtin_amdgcn_exp2f(mrun - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
-    lsum = lsum * __builtin_amdgcn_exp2f((mrun - M) - (el - E)) + l1 * __builtin_amdgcn_exp2f((m1 - M) - (el1 - E));
-    el = E;
+    lsum = lsum * f0 + l1 * f1;
     each<kDC>([&](auto dc) {
       each<16>([&](auto r) { o[dc][decltype(r)::value] = o[dc][decltype(r)::value] * f0 + os[(dc * 16 + r) * 64] * f1; });
     });
@@ -484,7 +431,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     // infinities and NaN of V, which counted as zero above: a row that sees one takes it as it is, whatever its weight
     const uint16_t* vsrc = static_cast<const uint16_t*>(a.v.ptr) + b * a.v.sb + hk * a.v.sh;
     for (int t = 0; t < tl.count; ++t) {
-      if (rec[int64_t(tl.tile(t)) * kRec + 8] == 0.f) continue;
+      if (odd[tl.tile(t)] == 0.f) continue;
       const int k0 = tl.tile(t) * 64;
       for (int j = k0; j < min(k0 + 64, n); ++j) {
         if (!sees(a, q_row, j)) continue;
@@ -502,7 +449,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   if (q_row >= n) return;
   // registers 4 rg .. 4 rg + 3 hold columns 32 dc + 8 rg + 4 h + 0..3: the lanes of a row swap halves of a register pair, so that
   // each stores eight consecutive columns
-  const int ie = int(el);
   uint16_t* out = static_cast<uint16_t*>(a.o.ptr) + b * a.o.sb + hq * a.o.sh + int64_t(q_row) * a.o.sn;
 #pragma unroll
   for (int dc = 0; dc < kDC; ++dc)
@@ -511,8 +457,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       uint32_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        x[i] = Elem<uint16_t>::from_f32(ldexpf(o[dc][8 * h2 + 2 * i] * inv, ie)) |
-               uint32_t(Elem<uint16_t>::from_f32(ldexpf(o[dc][8 * h2 + 2 * i + 1] * inv, ie))) << 16;
+        x[i] = Elem<uint16_t>::from_f32(o[dc][8 * h2 + 2 * i] * inv) | uint32_t(Elem<uint16_t>::from_f32(o[dc][8 * h2 + 2 * i + 1] * inv)) << 16;
       const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
       const auto s1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
       *reinterpret_cast<u32x4*>(out + dc * 32 + h2 * 16 + h * 8) = u32x4{s0[0], s1[0], s0[1], s1[1]};
@@ -772,7 +717,7 @@ size_t values_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_d
 }
 size_t window_bytes(int32_t batch, int32_t n, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
   if (dtype == D2O_F32) return 0;
-  return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * kRec * sizeof(float);
+  return values_bytes(batch, n, n_kv_heads, head_dim) + size_t(batch) * n_kv_heads * ((n + 63) / 64) * sizeof(float);
 }
 
 // Query heads that a block of `waves` wavefronts shares, and its blocks of rows.
@@ -786,7 +731,7 @@ void share_heads(WindowArgs& a, int waves, int rows) {
 template <int D, int NW, bool SPLIT>
 hipError_t run_bf16(WindowArgs& a, int batch, hipStream_t s) {
   constexpr int kRW = SPLIT ? NW / 2 : NW, kSmem = (SPLIT ? 8 : 4) * tile_elems<D>() * int(sizeof(uint16_t));
-  static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 5) * 64 * int(sizeof(float)), "the second half's rows");
+  static_assert(!SPLIT || kSmem >= NW / 2 * (D / 32 * 16 + 4) * 64 * int(sizeof(float)), "the second half's rows");
   share_heads(a, kRW, 32);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(window_bf16<D, NW, SPLIT>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -841,11 +786,11 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == D2O_BF16) {
     a.vt = static_cast<uint16_t*>(workspace);
-    a.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + values_bytes(batch, n, n_kv_heads, head_dim));
+    a.odd = reinterpret_cast<float*>(static_cast<char*>(workspace) + values_bytes(batch, n, n_kv_heads, head_dim));
     // Wavefronts per workgroup.  Where the chip has a CU for every block of 128 rows, eight, the tiles split over two halves.  Otherwise four,
     // two workgroups (d = 64: three) per CU that hide each other's ends, for heads of 64 and windows below 1024; for larger ones eight, for
-    // whose twice as many rows a tile is brought once.  (16384 tokens, 32 heads on 8, d = 128, four and eight: window 128 172 and 182 us, 512 270 and 275,
-    // 1024 414 and 407, 4096 1176 and 1135; d = 64, window 2048 425 and 464, 8000 1288 and 1396.  Blocks that all fit at once: four too.)
+    // whose twice as many rows a tile is brought once.  (16384 tokens, 32 heads on 8, d = 128, four and eight: window 128 185 and 198 us, 512 299 and 302,
+    // 1024 467 and 462, 4096 1405 and 1354; d = 64, window 2048 499 and 565, 8000 1442 and 1583.  Blocks that all fit at once: four too.)
     const int64_t blocks = int64_t((n + 127) / 128) * n_q_heads * batch;
     const bool four = blocks <= 512 || a.window < 1024;
     hipError_t e;

@@ -11,8 +11,9 @@ from . import pages_ref as ref
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
-FORMS = [  # a case for every kernel: dtype, d, heads, n, window, n_sink
-    (F32, 64, (2, 1), 300, 90, 2), (F32, 128, (24, 4), 700, 300, 70), (F32, 64, (2, 1), 300, 0, 0), (F32, 64, (60, 60), 700, 0, 0),
+FORMS = [  # a case for every kernel and block form: dtype, d, heads, n, window, n_sink
+    (F32, 64, (2, 1), 300, 90, 2), (F32, 128, (24, 4), 700, 300, 70), (BF16, 64, (2, 1), 300, 90, 2), (BF16, 128, (2, 1), 300, 0, 0),
+    (BF16, 64, (60, 60), 700, 300, 4), (BF16, 128, (60, 60), 700, 300, 70), (BF16, 128, (64, 16), 1111, 1029, 5),
 ]
 form = pytest.mark.parametrize("dtype,d,heads,n,window,n_sink", FORMS, ids=str)
 
@@ -108,3 +109,25 @@ def test_values_near_the_largest_number(dtype, d, heads, n, window, n_sink, flat
     V[:] = 3e38
     V[..., ::2] = -3e38
     check(Q, K, V, run(Q, K, V, window, n_sink), window, n_sink)
+
+
+@pytest.mark.parametrize("d,heads,n", [(64, (2, 1), 300), (128, (2, 1), 300), (64, (60, 60), 700), (128, (60, 60), 700), (128, (64, 16), 1111)], ids=str)
+def test_probabilities_hold_sixteen_bits(d, heads, n):
+    """Every row sees two keys whose parts of the sum nearly cancel, so that the output's own rounding hides nothing.  Logits are products
+    of one pair of numbers."""
+    Q, K, V, g = inputs(BF16, heads, n, d, 5)
+    Q, K = torch.zeros_like(Q), torch.zeros_like(K)
+    K[..., ::2, 0] = 1.0  # a row sees an odd and an even token
+    Q[..., 0] = torch.rand(Q.shape[:3], generator=g).to(BF16) * 8
+    x = Q[0, ::heads[0] // heads[1], :, 0].double() / math.sqrt(d)
+    V[0, :, ::2] = 1.0
+    V[0, :, 1::2] = -torch.exp(x[:, 1::2, None]).expand(-1, -1, d).to(BF16)
+    O, seen, G = run(Q, K, V, 2, 0), ref.window_seen(n, 2, 0), heads[0] // heads[1]
+    for h in (0, heads[0] - G):
+        q, k, v = (y[0, i].double() for y, i in ((Q, h), (K, h // G), (V, h // G)))
+        o, p = ref.attend64(q, k, v, seen)
+        # logits of at most 1 rounded three times, two terms
+        rel = 2 * (3 * 2.0 ** -24 + 2.0 ** -22 + 2 * 2.0 ** -24) + 2.0 ** -16
+        err = (O[0, h].double() - o).abs()
+        tol = p @ v.abs() * rel + o.abs() * ref.HALF_STEP[BF16]
+        assert bool((err <= tol).all()), (h, float((err / tol).max()))
