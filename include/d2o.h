@@ -356,6 +356,7 @@ typedef struct {
   int32_t head_dim;    /* d: 64 or 128                                                      */
   int32_t dtype;       /* d2o_dtype of q, k, v and out, and of the rows unless cache_fp8    */
   int32_t cache_fp8;   /* 1: a row is d E4M3 codes and one power of two, as in d2o_config   */
+                       /* (an infinity or NaN of a row is stored as NaN, the rest as without) */
   int32_t page_size;   /* rows of a page: a power of two, 1 to 1024                         */
   int32_t n_pages;     /* pages of the pool                                                 */
   int32_t max_pages;   /* columns of page_table                                             */

@@ -45,7 +45,10 @@ inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 size_t pages_step_bytes(const d2o_pages* p, int32_t max_len);   // workspace of d2o_pages_step
 size_t pages_evict_bytes(const d2o_pages* p, int32_t max_len);  // of d2o_pages_fill and d2o_pages_evict
 
-// 8-bit rows: x as codes with the row's exponent (fp64 inside, exact), one element.
-__device__ __forceinline__ uint8_t fp8_code(float x, int e) { return fp8_encode(ldexp(double(x), -e)); }
+// 8-bit rows: x as codes with the row's exponent (fp64 inside, exact), one element; infinities and NaN as NaN, and the exponent is
+// that of the others.
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+__device__ __forceinline__ uint8_t fp8_code(float x, int e) { return is_finite(x) ? fp8_encode(ldexp(double(x), -e)) : uint8_t(0x7F); }
+__device__ __forceinline__ float fp8_magnitude(float x) { return is_finite(x) ? fabsf(x) : 0.f; }
 
 }  // namespace d2o

@@ -367,7 +367,7 @@ __device__ __forceinline__ void put_row(const FillArgs& a, int bh, int b, int hk
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
         f[i] = __uint_as_float(i & 1 ? t[which][i / 2] & 0xFFFF0000u : t[which][i / 2] << 16);
-        m = fmaxf(m, fabsf(f[i]));
+        m = fmaxf(m, fp8_magnitude(f[i]));
       }
 #pragma unroll
       for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));

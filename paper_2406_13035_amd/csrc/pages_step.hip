@@ -256,7 +256,7 @@ __device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int 
     CT* dst = reinterpret_cast<CT*>(which ? a.pool.v_at(page, hk, s) : a.pool.k_at(page, hk, s));
     if constexpr (sizeof(CT) == 1) {
       float m = 0.f;
-      for (int i = lane; i < D; i += 64) m = fmaxf(m, fabsf(Elem<T>::to_f32(src[i])));
+      for (int i = lane; i < D; i += 64) m = fmaxf(m, fp8_magnitude(Elem<T>::to_f32(src[i])));
       const int e = fp8_row_exponent(wave_max(m));
       for (int i = lane; i < D; i += 64) dst[i] = fp8_code(Elem<T>::to_f32(src[i]), e);
       if (lane == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at] = int8_t(e);
