@@ -327,6 +327,7 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * context is needed: the caller owns pools, page table, lengths and workspace.  All of these calls
  * enqueue only, allocate nothing, keep nothing between calls and may be captured into a graph.
  * Rows are contiguous and start at 16-byte boundaries: pointers and strides of every view are such, and no stride is negative.
+ * Rows that a call writes (O, out, a pool that is filled, evicted from or given a new token) are apart: no stride between them is below d.
  * A workspace (16-byte aligned) belongs to one call at a time: calls that overlap in time need one each. */
 
 /* Causal prompt attention in which query i sees the keys j <= i with j > i - window or j < n_sink:

@@ -40,6 +40,9 @@ struct PagePool {
 int check_pages(const d2o_pages* p, PagePool* out);
 // A view of q, k, v or out tensors of `esize` bytes per element: present, 16-byte aligned, strides in whole 16 bytes, not negative.
 bool dense_view_ok(const d2o_view& v, int esize, bool rows);
+// The same of a view that is written, of counts[i] batches (pages), heads and rows of d elements: no two of them start at one place or inside each other.
+bool rows_apart(const d2o_view& v, const int32_t (&counts)[3], int d);
+bool pages_apart(const d2o_pages* p);  // of both pools
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 size_t pages_step_bytes(const d2o_pages* p, int32_t max_len);   // workspace of d2o_pages_step

@@ -946,6 +946,7 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
   if (n < 1 || budget < 1 || recent < 0 || n_sink < 0 || int64_t(recent) + n_sink > budget) return D2O_ERR_INVALID_ARG;
   if (!scores && budget < n) return D2O_ERR_INVALID_ARG;
   if (!dense_view_ok(K, es, true) || !dense_view_ok(V, es, true)) return D2O_ERR_INVALID_ARG;
+  if (!pages_apart(pages)) return D2O_ERR_INVALID_ARG;
   const int most = std::min(n, budget);
   if (most > int64_t(pages->max_pages) * pages->page_size) return D2O_ERR_CAPACITY;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
@@ -1015,7 +1016,7 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
   EvictArgs a;
   const int rc = check_pages(pages, &a.pool);
   if (rc != D2O_OK) return rc;
-  if (!lens || !pages->score || !pages->pos || max_len < 1) return D2O_ERR_INVALID_ARG;
+  if (!lens || !pages->score || !pages->pos || max_len < 1 || !pages_apart(pages)) return D2O_ERR_INVALID_ARG;
   if (budget < 1 || recent < 0 || n_sink < 0 || int64_t(recent) + n_sink > budget) return D2O_ERR_INVALID_ARG;
   if (max_len > int64_t(pages->max_pages) * pages->page_size) return D2O_ERR_CAPACITY;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;

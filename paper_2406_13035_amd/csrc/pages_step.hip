@@ -13,6 +13,17 @@ bool dense_view_ok(const d2o_view& v, int esize, bool rows) {
   return v.stride_b % al == 0 && v.stride_h % al == 0 && (!rows || v.stride_n % al == 0);
 }
 
+bool rows_apart(const d2o_view& v, const int32_t (&counts)[3], int d) {
+  const int64_t strides[3] = {v.stride_b, v.stride_h, v.stride_n};
+  for (int i = 0; i < 3; ++i)
+    if (counts[i] > 1 && strides[i] < d) return false;
+  return true;
+}
+bool pages_apart(const d2o_pages* p) {
+  const int32_t counts[3] = {p->n_pages, p->n_kv_heads, p->page_size};
+  return rows_apart(p->K, counts, p->head_dim) && rows_apart(p->V, counts, p->head_dim);
+}
+
 int check_pages(const d2o_pages* p, PagePool* out) {
   if (!p) return D2O_ERR_INVALID_ARG;
   if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_pages < 1 || p->max_pages < 1) return D2O_ERR_INVALID_ARG;
@@ -724,6 +735,7 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   if (!dense_view_ok(q, es, false) || !dense_view_ok(out, es, false)) return D2O_ERR_INVALID_ARG;
   if (!k_new.ptr != !v_new.ptr) return D2O_ERR_INVALID_ARG;
   if (k_new.ptr && (!dense_view_ok(k_new, es, false) || !dense_view_ok(v_new, es, false))) return D2O_ERR_INVALID_ARG;
+  if (!rows_apart(out, {pages->batch, pages->n_q_heads, 1}, pages->head_dim) || (k_new.ptr && !pages_apart(pages))) return D2O_ERR_INVALID_ARG;
   if (max_len > int64_t(pages->max_pages) * pages->page_size) return D2O_ERR_CAPACITY;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return D2O_ERR_INVALID_ARG;
   if (workspace_bytes < pages_step_bytes(pages, max_len)) return D2O_ERR_CAPACITY;

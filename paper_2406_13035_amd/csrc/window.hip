@@ -764,6 +764,7 @@ extern "C" int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, in
   if (n_q_heads < 1 || n_q_heads % n_kv_heads || window < 0 || n_sink < 0) return D2O_ERR_INVALID_ARG;
   for (const d2o_view* v : {&Q, &K, &V, &O})
     if (!dense_view_ok(*v, es, true)) return D2O_ERR_INVALID_ARG;
+  if (!rows_apart(O, {batch, n_q_heads, n}, head_dim)) return D2O_ERR_INVALID_ARG;
   const size_t need = window_bytes(batch, n, n_kv_heads, head_dim, dtype);
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return D2O_ERR_INVALID_ARG;
   if (workspace_bytes < need) return D2O_ERR_CAPACITY;
