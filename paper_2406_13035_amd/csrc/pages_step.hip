@@ -746,9 +746,11 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   a.lens = lens;
   a.positions = positions;
   const int64_t bh = int64_t(pages->batch) * pages->n_kv_heads, hq = int64_t(pages->batch) * pages->n_q_heads;
-  if (bh > 65535 || bh * ((max_len + kFinishEntries - 1) / kFinishEntries) > 0x3FFFFFFF) return D2O_ERR_UNSUPPORTED;
+  if (bh > 65535) return D2O_ERR_UNSUPPORTED;
   a.pad = (max_len + kTile - 1) / kTile * kTile;
   a.splits = step_splits(bh, most_tiles(pages, max_len, window, n_sink));
+  // (step_finish: a grid holds fewer than 2^32 threads)
+  if (a.splits > 1 && hq + (pages->score ? bh * ((max_len + kFinishEntries - 1) / kFinishEntries) : 0) > 0xFFFFFF) return D2O_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
   a.logits = reinterpret_cast<float*>(ws);
   ws += round256(pages->score ? size_t(hq) * a.pad * sizeof(float) : 0);
