@@ -736,7 +736,7 @@ __global__ __launch_bounds__(NT) void evict_select(EvictArgs a, int lanes) {
   move_rows<4>(a, b, hk, from, hole, tid / lanes, NT / lanes, pairs, tid % lanes);
 }
 
-// The moves of heads that have many: `lanes` lanes of 16 bytes per row.
+// The moves of heads that have many: `lanes` lanes of 16 bytes per row, again and again where a grid (below 2^32 threads) does not hold them.
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int lanes) {
   const int bh = blockIdx.y, per = 256 / lanes;
   const int32_t* hole = a.moves + int64_t(bh) * 2 * a.most;
@@ -1061,7 +1061,7 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
     evict_select<1024, 0><<<heads, 1024, 0, s>>>(a, lanes);
   if (a.most > kInline) {  // (by slices: never)
     const int per = 256 / lanes;
-    evict_move<<<dim3((a.most + per - 1) / per, unsigned(bh)), 256, 0, s>>>(a, lanes);
+    evict_move<<<dim3(std::min((a.most + per - 1) / per, 65536), unsigned(bh)), 256, 0, s>>>(a, lanes);
   }
   return hipGetLastError() == hipSuccess ? D2O_OK : D2O_ERR_HIP;
 }
