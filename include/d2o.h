@@ -388,7 +388,8 @@ int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, co
  * (k_new, v_new) is stored as entry lens[b] - 1 with score 0 and position positions[b]; then q attends over the
  * entries with position > positions[b] - window or position < n_sink (window = 0: all) and, where the pages keep scores,
  * the softmax rows of the Hq / Hkv query heads are added to the entries' scores (Eq. 6).  positions: device
- * [B], NULL: lens[b] - 1.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
+ * [B], NULL: lens[b] - 1, which is the new token's position only while every token before it has its entry: once a fill or an eviction has given some
+ * up, pages that keep positions need it given, or later windows and evictions take the new token for an old one.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
  * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
  * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry (or only
  * logits of minus infinity).  Values may be as large as their type allows; a weight below 2^-126 times twice the entries of the largest may count as zero.

@@ -556,7 +556,8 @@ class Pages:
 
     def d2o_pages_step(self, q, k_new, v_new, lens, out, positions=None, window=0, n_sink=0):
         """One new token per sequence: q, out [B, Hq, d]; k_new, v_new [B, Hkv, d], or None: attention only; lens int32
-        [B], the new token included."""
+        [B], the new token included; positions int32 [B], None: lens - 1, which pages with positions must not rely on once
+        a fill or an eviction has given tokens up."""
         shape = (self.batch, self.n_q_heads, self.head_dim)
         new = (self.batch, self.n_kv_heads, self.head_dim)
         _tensor_ok(q, shape, self.dtype, self.device, "q")
