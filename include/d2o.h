@@ -336,7 +336,7 @@ int d2o_prefill_events(d2o_ctx* ctx, int32_t layer, int32_t b, int32_t kv_head,
  * of a padded batch (NULL: n each; values are taken within [0, n]); rows of O behind a sequence's end are left as they were,
  * its keys behind the end take no part.  An infinity or NaN in V reaches the rows that see it, whatever its weight, and no others.
  * Finite values may be of any magnitude, side by side; a weight holds 24 bits (D2O_BF16: 16), sums 24, and a weight below 2^-126 times sixteen times the
- * keys that a row sees, relative to the row's largest, may count as zero.  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16,
+ * keys that a row sees, relative to the row's largest, may count as zero (means: below 2^-149 times as much).  O may be Q itself, but may not overlap K or V.  D2O_F32 and D2O_BF16,
  * d = 64 or 128, any Hq / Hkv.  Errors:
  * INVALID_ARG, UNSUPPORTED (also a row stride of K of 2^24 elements or more), CAPACITY (workspace smaller than
  * d2o_window_workspace_bytes says; where it says 0, NULL will do), HIP. */
@@ -392,7 +392,8 @@ int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, co
  * up, pages that keep positions need it given, or later windows and evictions take the new token for an old one.  q, out: [B][Hq][d]; k_new, v_new: [B][Hkv][d] (stride_n unused; both ptr NULL: nothing is stored and
  * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
  * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry (or only
- * logits of minus infinity).  Values may be as large as their type allows; a weight below 2^-126 times twice the entries of the largest may count as zero.
+ * logits of minus infinity).  Values may be as large as their type allows; a weight below 2^-126 times twice the
+ * entries of the largest may count as zero, and means end at 2^-149 times twice the entries.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_len beyond the page table, workspace too small), HIP. */
 int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view v_new, const int32_t* lens,
                    const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
