@@ -1,0 +1,586 @@
+"""What stands around attention over a cache in pages whose rows are held in 4 bits, as cases that can be timed and compared.
+
+A case is one call (of `put`: two) of an operator of `paper_2406_13035_amd.binding`:
+
+  norm    queries and keys of every head to length sqrt(d) times a weight per channel, then rotated by their positions
+          (`d2o_qk_norm_rope`);
+  map     block tables and slot maps from the lengths of requests: sequences gain or lose tokens, pages come from and go back to a
+          list of free ones, every new token learns its slot (`d2o_pages_map`);
+  put     new tokens' K and V into the slots of a map and back again (`d2o_pages_put`, `d2o_pages_get`), in rows of the tensors'
+          type, of 8 bits or of 4;
+  step    one query token per sequence over pages of 4-bit rows, its softmax row added to the entries' scores (`d2o_pages_step`);
+  attend  several query tokens per sequence, each of which sees the entries up to its own (`d2o_pages_attend`).
+
+A 4-bit row is d codes of the float format E2M1 (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4 and 6), two to a byte, the even element in the low
+half, and one power of two for every 32 of them: the smallest that brings the block's largest magnitude to 6 or below.  The largest work
+is the block of 2048 tokens on a cache of 32768; `draw` spreads over what lies between and beside the listed sizes.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+EPS = 1e-6
+GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def listed():
+    mha = {"q_heads": 32, "kv_heads": 32, "d": 128}
+    gqa = {"q_heads": 32, "kv_heads": 8, "d": 128}
+    return [
+        # one token of one fp32 sequence (latency)
+        dict(name="norm_f32_token", kind="norm", dtype="f32", batch=1, q_heads=4, kv_heads=4, d=64, n=1, rot=64, base=10000.0,
+             far=1000, packed=False),
+        # a generation step of a serving batch: packed rows, positions of their own
+        dict(name="norm_gqa_b64", kind="norm", dtype="bf16", batch=64, **gqa, n=1, rot=128, base=10000.0, far=131072,
+             packed=True),
+        # the long prompt of the benchmark's shape
+        dict(name="norm_7b_32k", kind="norm", dtype="bf16", batch=1, **mha, n=32768, rot=128, base=10000.0, far=1,
+             packed=False),
+        # a generation step of a serving batch: one token each (latency)
+        dict(name="map_one_b64", kind="map", batch=64, have=8192, add=1, page=64, done=0.0, cut=0.0, spare=1.0),
+        # a server under load: prompts arrive, sequences end or are cut back, and the pool runs out before the last of them
+        dict(name="map_prompts_b256", kind="map", batch=256, have=8192, add=4096, page=64, done=0.2, cut=0.1, spare=0.8),
+        # one new token of every sequence of a serving batch, stored and read back (latency)
+        dict(name="put_fp4_b64", kind="put", dtype="bf16", rows="fp4", tokens=64, kv_heads=8, d=128, page=64, idle=0.0),
+        # the prompts of a serving batch, packed, some rows of the packing unused
+        dict(name="put_fp4_64k", kind="put", dtype="bf16", rows="fp4", tokens=65536, kv_heads=8, d=128, page=64, idle=0.05),
+        # the shortest step: one sequence of 129 entries, scores kept (latency)
+        dict(name="step_fp4_129", kind="step", batch=1, q_heads=4, kv_heads=4, d=64, length=129, page=16, window=0, n_sink=0,
+             scores=True, ragged=False),
+        # a serving batch of different lengths, scores kept for eviction
+        dict(name="step_fp4_gqa_8k_b16", kind="step", batch=16, **gqa, length=8192, page=64, window=0, n_sink=0, scores=True,
+             ragged=True),
+        # one sequence with a very long cache: few heads, the length has to be split
+        dict(name="step_fp4_gqa_128k", kind="step", batch=1, **gqa, length=131072, page=128, window=0, n_sink=0, scores=False,
+             ragged=False),
+        # a serving batch in which some sequences have one new token and others a dialogue turn of up to 48
+        dict(name="attend_fp4_mixed_b16", kind="attend", batch=16, **gqa, tokens=48, length=8192, page=64, window=0, n_sink=0,
+             ragged=True),
+        # a block of a long prompt, behind all the tokens before it
+        dict(name="attend_fp4_2k_on_32k", kind="attend", batch=1, **gqa, tokens=2048, length=32768, page=128, window=0, n_sink=0,
+             ragged=False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "map", "put", "step", "step", "attend", "attend"])
+    d = rng.choice([64, 128, 128])
+    kv = rng.choice([1, 2, 4, 8, 8, 16, 32])
+    group = rng.choice([1, 1, 2, 4, 4, 8, 3, 5, 16])
+    while kv * group > 64:
+        group = rng.choice([1, 2, 4])
+    page = rng.choice([1, 8, 16, 16, 32, 64, 64, 128, 256])
+    sink = rng.choice([0, 0, 1, 4, 4, 17, 100])
+    heads = {"q_heads": kv * group, "kv_heads": kv, "d": d}
+    if kind == "norm":
+        dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+        batch, n = rng.choice([1, 1, 2, 3, 16, 64]), _log(rng, 1, 32768)
+        while batch * n * (kv * group + kv) * d * (2 if dtype == "f32" else 1) > 64 * 32768 * 128:
+            n = max(1, n * 2 // 3)
+        return dict(kind=kind, dtype=dtype, batch=batch, **heads, n=n, rot=rng.choice([d, d, d, d // 2, 16]),
+                    base=rng.choice([10000.0, 10000.0, 500000.0]), far=_log(rng, 1, 1 << 24), packed=rng.random() < 0.5)
+    if kind == "map":
+        batch = _log(rng, 1, 2048)
+        add = rng.choice([1, 1, _log(rng, 1, 8192)])
+        while batch * add > 256 * 4096:
+            add = max(1, add * 2 // 3)
+        have = _log(rng, 1, 16384)
+        while batch * (have + add) > 256 * 16384 * page:
+            have, add = max(1, have * 2 // 3), max(1, add * 2 // 3)
+        return dict(kind=kind, batch=batch, have=have, add=add, page=page, done=rng.choice([0.0, 0.2]),
+                    cut=rng.choice([0.0, 0.1]), spare=rng.choice([1.0, 1.0, 0.5, 0.1]))
+    if kind == "put":
+        rows = rng.choice(["fp4", "fp4", "fp8", "own"])
+        dtype = rng.choice(["bf16", "f32"]) if rows == "own" else "bf16"
+        tokens = _log(rng, 1, 65536)
+        while tokens * kv * d * (2 if dtype == "f32" else 1) > 65536 * 8 * 128:
+            tokens = max(1, tokens * 2 // 3)
+        return dict(kind=kind, dtype=dtype, rows=rows, tokens=tokens, kv_heads=kv, d=d, page=page, idle=rng.choice([0.0, 0.05, 0.5]))
+    if kind == "step":
+        batch = rng.choice([1, 1, 2, 4, 16, 64])
+        length = _log(rng, 1, 131072)
+        while batch * kv * length > 8 * 131072:
+            length = max(1, length * 2 // 3)
+        return dict(kind=kind, batch=batch, **heads, length=length, page=page, window=rng.choice([0, 0, _log(rng, 1, 4096)]),
+                    n_sink=sink, scores=rng.random() < 0.5, ragged=batch > 1)
+    batch = rng.choice([1, 1, 2, 4, 16, 64])
+    tokens, length = _log(rng, 1, 2048), _log(rng, 1, 131072)
+    # an eighth of the largest listed case at most
+    while batch * kv * group * min(tokens, length) * length > 32 * 2048 * 32768 // 8 or batch * kv * length > 8 * 131072:
+        tokens, length = max(1, tokens * 3 // 4), max(1, length * 3 // 4)
+    return dict(kind=kind, batch=batch, **heads, tokens=min(tokens, length), length=length, page=page,
+                window=rng.choice([0, 0, _log(rng, 1, 4096)]), n_sink=sink, ragged=batch > 1)
+
+
+def _lengths(case):
+    """The entries of a batch's sequences: all alike, or falling from the longest to about a fifth of it."""
+    n, B = case["length"], case["batch"]
+    if not case["ragged"]:
+        return [n] * B
+    return [max(1, n - (n * 4 * b) // (5 * B) - (b % 3 if n > 8 else 0)) for b in range(B)]
+
+
+def _news(case):
+    """The query tokens of a batch's sequences: every second has one, one has none where there are many, the others fewer and fewer."""
+    m, B, lens = case["tokens"], case["batch"], _lengths(case)
+    if not case["ragged"]:
+        return [min(m, n) for n in lens]
+    some = [1 if b % 2 else max(1, m - (m * b) // B) for b in range(B)]
+    if B > 4:
+        some[4] = 0
+    return [min(a, n) for a, n in zip(some, lens)]
+
+
+def _pairs(case, lens, news):
+    """(Query token, entry) pairs that are seen, of all sequences."""
+    W, T, total = case["window"], case["n_sink"], 0
+    for n, m in zip(lens, news):
+        for i in range(n - m, n):
+            low = 0 if W == 0 else max(0, i - W + 1)
+            total += i + 1 - low + min(low, T)
+    return total
+
+
+def _row_bytes(rows, dtype, d):
+    return {"fp4": d // 2 + d // 32, "fp8": d + 1, "own": d * (4 if dtype == "f32" else 2)}[rows]
+
+
+def work(case):
+    c = case
+    if c["kind"] == "norm":
+        es = 4 if c["dtype"] == "f32" else 2
+        values = c["batch"] * c["n"] * (c["q_heads"] + c["kv_heads"]) * c["d"]
+        return {"bytes": 2 * es * values + 4 * c["batch"] * c["n"], "flops": 8 * values}
+    if c["kind"] == "map":
+        tokens = int(c["batch"] * c["add"] * ((1.0 - c["done"] - c["cut"]) if c["add"] > 1 else 1.0) * (0.5 if c["add"] > 1 else 1.0))
+        pages = tokens // c["page"] + c["batch"] * (c["done"] + c["cut"]) * c["have"] / c["page"] / 2
+        return {"bytes": 12 * c["batch"] * c["add"] + 16 * c["batch"] + 8 * pages, "flops": 0}
+    if c["kind"] == "put":
+        es = 4 if c["dtype"] == "f32" else 2
+        rows = 2 * c["tokens"] * (1.0 - c["idle"]) * c["kv_heads"]
+        return {"bytes": rows * (2 * c["d"] * es + 2 * _row_bytes(c["rows"], c["dtype"], c["d"])) + 16 * c["tokens"], "flops": 0}
+    Hq, Hkv, d = c["q_heads"], c["kv_heads"], c["d"]
+    lens = _lengths(c)
+    news = [1] * c["batch"] if c["kind"] == "step" else _news(c)
+    W, entries = c["window"], 0
+    for n, m in zip(lens, news):
+        low = 0 if W == 0 else max(0, n - m - W + 1)
+        entries += (n - low + min(low, c["n_sink"])) if m else 0
+    row = 2 * _row_bytes("fp4", "bf16", d) + (8 if c.get("scores") else 0)
+    return {"bytes": Hkv * entries * row + 4 * sum(news) * Hq * d, "flops": 4 * d * Hq * _pairs(c, lens, news)}
+
+
+# ---- rows of 4 and 8 bits, in elementary operations ----------------------------------------
+
+def _exponents4(x):
+    """The power of two of every 32 values: the smallest that brings the largest of them to 6 = 0.75 * 2^3 or below."""
+    amax = x.abs().amax(-1)
+    fr, ex = torch.frexp(amax)
+    e = torch.where(fr <= 0.75, ex - 3, ex - 2).clamp(min=-120)
+    return torch.where(amax > 0, e, torch.zeros_like(e))
+
+
+def _encode4(x):
+    """[.., d] as codes [.., d / 2] (uint8) and powers of two [.., d / 32] (int8)."""
+    x = x.float().unflatten(-1, (-1, 32))
+    e = _exponents4(x)
+    y = torch.ldexp(x, -e[..., None])
+    a = y.abs()
+    # to the nearest magnitude; in the middle of two, to the one with the even code
+    code = ((a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0))
+    code = torch.where((y < 0) & (code > 0), code + 8, code).flatten(-2)
+    return code[..., 0::2] | (code[..., 1::2] << 4), e.to(torch.int8)
+
+
+def _decode4(codes, e):
+    both = torch.stack([codes & 15, codes >> 4], -1).flatten(-2).long()
+    values = torch.tensor(GRID + tuple(-v for v in GRID), device=DEV)[both]
+    return torch.ldexp(values.unflatten(-1, (-1, 32)), e[..., None].to(torch.int32)).flatten(-2)
+
+
+def _encode8(x):
+    amax = x.float().abs().amax(-1)
+    fr, ex = torch.frexp(amax)
+    e = torch.where(fr <= 0.875, ex - 9, ex - 8).clamp(min=-120)
+    e = torch.where(amax > 0, e, torch.zeros_like(e))
+    return torch.ldexp(x.float(), -e[..., None]).to(torch.float8_e4m3fn).view(torch.uint8), e.to(torch.int8)
+
+
+def _decode8(codes, e):
+    return torch.ldexp(codes.view(torch.float8_e4m3fn).float(), e[..., None].to(torch.int32))
+
+
+# ---- inputs -------------------------------------------------------------------------------
+
+def prepare(case, seed):
+    c = case
+    gen = torch.Generator(device=DEV).manual_seed(1 + 7919 * int(seed))
+    st = dict(case=c)
+
+    def rnd(*shape, scale=1.0, dtype="bf16"):
+        return (torch.randn(shape, generator=gen, device=DEV) * scale).to(DTYPES[dtype])
+
+    def channels(heads, d):
+        # a few channels of keys are much larger than the others
+        return torch.exp(0.7 * torch.randn((heads, d), generator=gen, device=DEV))
+
+    def chance(*shape):
+        return torch.rand(shape, generator=gen, device=DEV)
+
+    if c["kind"] == "norm":
+        B, n, d, dt = c["batch"], c["n"], c["d"], c["dtype"]
+        for x, h in (("Q", c["q_heads"]), ("K", c["kv_heads"])):
+            if c["packed"]:  # [tokens][head][d] in memory
+                st[x] = (torch.randn((B, n, h, d), generator=gen, device=DEV) * 2.0 * channels(h, d)).to(DTYPES[dt]).transpose(1, 2)
+                st[x + "_out"] = torch.zeros((B, n, h, d), dtype=DTYPES[dt], device=DEV).transpose(1, 2)
+            else:
+                st[x] = (torch.randn((B, h, n, d), generator=gen, device=DEV) * 2.0 * channels(h, d)[:, None]).to(DTYPES[dt])
+                st[x + "_out"] = torch.zeros((B, h, n, d), dtype=DTYPES[dt], device=DEV)
+        st["wq"], st["wk"] = (1.0 + 0.3 * rnd(d, dtype="f32")).to(DTYPES[dt]), (1.0 + 0.3 * rnd(d, dtype="f32")).to(DTYPES[dt])
+        first = (chance(B, 1) * c["far"]).long()
+        st["positions"] = (first + torch.arange(n, device=DEV)).to(torch.int32).contiguous()
+        return st
+
+    if c["kind"] == "map":
+        B, page = c["batch"], c["page"]
+        cap = -(-(c["have"] + c["add"]) // page)
+        lens = (chance(B) * (c["have"] + 1)).long().clamp(max=c["have"])
+        what = chance(B)
+        add = 1 + (chance(B) * c["add"]).long().clamp(max=c["add"] - 1)
+        less = torch.where(what < c["done"], lens, (chance(B) * lens).long())
+        change = torch.where(what < c["done"] + c["cut"], -less, add)
+        used = -(-lens // page)
+        need = (-(-(lens + change.clamp(min=0)) // page) - used).sum()
+        # the pool: what the sequences hold now and `spare` of what they ask for, at the most of any seed
+        n_pages = B * (-(-c["have"] // page)) + int(c["spare"] * B * (c["add"] // (2 * page) + 1)) + 1
+        order = torch.randperm(n_pages, generator=gen, device=DEV).to(torch.int32)
+        base = used.cumsum(0) - used
+        at = torch.arange(cap, device=DEV)[None, :]
+        held = at < used[:, None]
+        st["page_table"] = torch.where(held, order[(base[:, None] + at).clamp(max=n_pages - 1)], torch.full_like(order[:1], -1)).contiguous()
+        total = used.sum()
+        free = torch.minimum((need.double() * c["spare"]).long(), n_pages - total)
+        head = (chance(1) * n_pages).long().clamp(max=n_pages - 1)[0]
+        k = torch.arange(n_pages, device=DEV)
+        st["free_pages"] = torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+        st["free_pages"][(head + k) % n_pages] = torch.where(k < free, order[(total + k) % n_pages], torch.full_like(order, -1))
+        st["free_state"] = torch.stack([head, free]).to(torch.int32)
+        st["lens"], st["change"] = lens.to(torch.int32), change.to(torch.int32)
+        rows = B * c["add"]
+        st["first"] = torch.zeros(B + 1, dtype=torch.int32, device=DEV)
+        st["slots"] = torch.zeros(rows, dtype=torch.int64, device=DEV)
+        st["positions"] = torch.zeros(rows, dtype=torch.int32, device=DEV)
+        st["lens_out"], st["state_out"] = torch.zeros_like(st["lens"]), torch.zeros_like(st["free_state"])
+        return st
+
+    d, kv, page = c["d"], c["kv_heads"], c["page"]
+    if c["kind"] == "put":
+        T = c["tokens"]
+        n_pages = -(-T // page) + 3
+        st["K"] = (torch.randn((T, kv, d), generator=gen, device=DEV) * channels(kv, d)).to(DTYPES[c["dtype"]])
+        st["V"] = rnd(T, kv, d, dtype=c["dtype"])
+        st["slots"] = torch.randperm(n_pages * page, generator=gen, device=DEV)[:T]
+        # rows of sequences: runs of tokens in neighbouring rows of a page
+        runs = torch.randperm(-(-T // page) + 3, generator=gen, device=DEV)
+        t = torch.arange(T, device=DEV)
+        st["slots"] = runs[t // page] * page + t % page
+        st["slots"] = torch.where(chance(T) < c["idle"], torch.full_like(t, -1), st["slots"]).contiguous()
+        st["K_out"], st["V_out"] = (torch.zeros((T, kv, d), dtype=DTYPES[c["dtype"]], device=DEV) for _ in range(2))
+        st["page_table"] = torch.arange(n_pages, dtype=torch.int32, device=DEV)[None]
+        _empty_pool(st, n_pages)
+        return st
+
+    lens = _lengths(c)
+    per = -(-c["length"] // page)
+    n_pages = c["batch"] * per + 2
+    order = torch.randperm(n_pages, generator=gen, device=DEV)[:c["batch"] * per]
+    st["page_table"] = order.view(c["batch"], per).to(torch.int32).contiguous()
+    st["k"], st["k_exp"] = _encode4(torch.randn((n_pages, kv, page, d), generator=gen, device=DEV) * channels(kv, d)[:, None])
+    st["v"], st["v_exp"] = _encode4(torch.randn((n_pages, kv, page, d), generator=gen, device=DEV))
+    st["k"], st["v"] = st["k"].contiguous(), st["v"].contiguous()
+    st["score"] = None
+    if c.get("scores"):
+        s = torch.exp(1.5 * torch.randn((n_pages, kv, page), generator=gen, device=DEV))
+        st["score"] = torch.where(chance(n_pages, kv, page) < 0.1, torch.zeros_like(s), s)
+    st["lens"] = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    news = [1] * c["batch"] if c["kind"] == "step" else _news(c)
+    T = sum(news)
+    st["q"], st["out"] = rnd(T, c["q_heads"], d, scale=1.0), torch.zeros((T, c["q_heads"], d), dtype=torch.bfloat16, device=DEV)
+    first = [sum(news[:b]) for b in range(c["batch"] + 1)]
+    st["first"] = torch.tensor(first, dtype=torch.int32, device=DEV)
+    return st
+
+
+def _empty_pool(st, n_pages):
+    c = st["case"]
+    shape = (n_pages, c["kv_heads"], c["page"])
+    wide, dt = {"fp4": (c["d"] // 2, torch.uint8), "fp8": (c["d"], torch.uint8), "own": (c["d"], DTYPES[c["dtype"]])}[c["rows"]]
+    st["k"], st["v"] = (torch.zeros((*shape, wide), dtype=dt, device=DEV) for _ in range(2))
+    st["k_exp"] = st["v_exp"] = st["score"] = None
+    if c["rows"] != "own":
+        exps = (*shape, c["d"] // 32) if c["rows"] == "fp4" else shape
+        st["k_exp"], st["v_exp"] = (torch.zeros(exps, dtype=torch.int8, device=DEV) for _ in range(2))
+
+
+# ---- the framework's calls ----------------------------------------------------------------
+
+def _pages(st):
+    if "pages" not in st:
+        from paper_2406_13035_amd import binding
+        c = st["case"]
+        st["pages"] = binding.Pages(st["k"], st["v"], st["page_table"], c.get("q_heads", c["kv_heads"]), K_exp=st["k_exp"],
+                                    V_exp=st["v_exp"], score=st["score"], max_len=c.get("length"))
+    return st["pages"]
+
+
+def _run_own(st):
+    from paper_2406_13035_amd import binding
+    c = st["case"]
+    if c["kind"] == "norm":
+        binding.d2o_qk_norm_rope(st["Q"], st["K"], st["wq"], st["wk"], eps=EPS, positions=st["positions"], rope_base=c["base"],
+                                 rot_dim=c["rot"], Q_out=st["Q_out"], K_out=st["K_out"])
+        return [st["Q_out"], st["K_out"]]
+    if c["kind"] == "map":
+        binding.d2o_pages_map(st["page_table"], st["lens"], st["change"], st["free_pages"], st["free_state"], c["page"],
+                              first=st["first"], slots=st["slots"], positions=st["positions"], lens_out=st["lens_out"],
+                              free_state_out=st["state_out"])
+        return [st[x] for x in ("lens_out", "first", "slots", "positions", "page_table", "free_pages", "state_out")]
+    if c["kind"] == "put":
+        _pages(st).d2o_pages_put(st["K"], st["V"], st["slots"])
+        _pages(st).d2o_pages_get(st["slots"], st["K_out"], st["V_out"])
+        return [st["K_out"], st["V_out"]]
+    if c["kind"] == "step":
+        _pages(st).d2o_pages_step(st["q"], None, None, st["lens"], st["out"], window=c["window"], n_sink=c["n_sink"])
+        return [st["out"]] + ([st["score"]] if c["scores"] else [])
+    _pages(st).d2o_pages_attend(st["q"], st["first"], st["lens"], st["out"], window=c["window"], n_sink=c["n_sink"])
+    return [st["out"]]
+
+
+# ---- the plain forms ----------------------------------------------------------------------
+
+def _plain_norm(st):
+    c = st["case"]
+    half = c["rot"] // 2
+    # the angle in 64 bits: a far position times a small frequency keeps its fraction of a turn
+    freq = torch.tensor(float(c["base"]), dtype=torch.float64, device=DEV) ** (
+        -2.0 * torch.arange(half, dtype=torch.float64, device=DEV) / c["rot"])
+    angle = st["positions"].double()[:, None, :, None] * freq
+    cos, sin = angle.cos().float(), angle.sin().float()
+    for x, w in (("Q", st["wq"]), ("K", st["wk"])):
+        y = st[x].float()
+        y = y * torch.rsqrt(y.square().mean(-1, keepdim=True) + EPS) * w.float()
+        a, b, rest = y[..., :half], y[..., half:2 * half], y[..., 2 * half:]
+        st[x + "_out"].copy_(torch.cat([a * cos - b * sin, b * cos + a * sin, rest], -1))
+    return [st["Q_out"], st["K_out"]]
+
+
+def _plain_map(st):
+    c, page = st["case"], st["case"]["page"]
+    B, cap = st["page_table"].shape
+    rows, n_pages = st["slots"].numel(), st["free_pages"].numel()
+    head, count = st["free_state"][0].long(), st["free_state"][1].long()
+    lens, change = st["lens"].long(), st["change"].long()
+    pages = lambda n: (n + page - 1) // page  # noqa: E731
+    gain, loss = change.clamp(min=0), torch.minimum((-change).clamp(min=0), lens)
+    fits = lens + gain <= cap * page
+    gain = torch.where(fits, gain, torch.zeros_like(gain))
+    need = pages(lens + gain) - pages(lens)
+    # a sequence is served where its own wishes and those of all before it can be
+    served = (gain.cumsum(0) <= rows) & ((need == 0) | (need.cumsum(0) <= count))
+    got, take = torch.where(served, gain, torch.zeros_like(gain)), torch.where(served, need, torch.zeros_like(need))
+    after = lens + got - loss
+    st["lens_out"].copy_(after)
+    st["first"][1:] = got.cumsum(0)
+    # pages from the list's head, page after page of sequence after sequence
+    t0 = take.cumsum(0) - take
+    at = torch.arange(cap, device=DEV)[None, :]
+    k = at - pages(lens)[:, None]
+    new = (k >= 0) & (k < take[:, None])
+    table = torch.where(new, st["free_pages"][(head + (t0[:, None] + k).clamp(min=0)) % n_pages], st["page_table"])
+    # pages that hold no entry any more to its end
+    gone = (loss > 0)[:, None] & (at >= pages(after)[:, None]) & (at < pages(lens)[:, None])
+    back = st["page_table"][gone]
+    room = torch.arange(back.numel(), device=DEV)
+    st["free_pages"][(head + count + room) % n_pages] = back
+    st["page_table"].copy_(table)
+    taken = take.sum()
+    st["state_out"].copy_(torch.stack([(head + taken) % n_pages, count - taken + back.numel()]))
+    i = torch.arange(rows, device=DEV)
+    b = torch.searchsorted(st["first"][1:].long(), i, right=True)
+    there = b < B
+    b = b.clamp(max=B - 1)
+    p = lens[b] + i - st["first"][b].long()
+    slot = st["page_table"].long().view(-1)[(b * cap + p // page).clamp(max=B * cap - 1)] * page + p % page
+    st["slots"].copy_(torch.where(there, slot, torch.full_like(slot, -1)))
+    st["positions"].copy_(torch.where(there, p, torch.zeros_like(p)))
+    return [st[x] for x in ("lens_out", "first", "slots", "positions", "page_table", "free_pages", "state_out")]
+
+
+def _plain_put(st):
+    c, page = st["case"], st["case"]["page"]
+    encode = {"fp4": _encode4, "fp8": _encode8, "own": lambda x: (x, None)}[c["rows"]]
+    decode = {"fp4": _decode4, "fp8": _decode8, "own": lambda x, e: x}[c["rows"]]
+    used = st["slots"] >= 0
+    at = st["slots"][used]
+    rows = (at // page, slice(None), at % page)
+    for x, pool in (("K", "k"), ("V", "v")):
+        codes, e = encode(st[x][used])
+        st[pool][rows] = codes
+        if e is not None:
+            st[pool + "_exp"][rows] = e
+    for x, pool in (("K_out", "k"), ("V_out", "v")):
+        st[x][used] = decode(st[pool][rows], None if c["rows"] == "own" else st[pool + "_exp"][rows]).to(st[x].dtype)
+    return [st["K_out"], st["V_out"]]
+
+
+def _values(st, pool):
+    """The values of a pool's pages in the sequences' order: [B, Hkv, entries, d]."""
+    c, table = st["case"], st["page_table"].long()
+    codes, e = (x[table].transpose(1, 2).flatten(2, 3) for x in (st[pool], st[pool + "_exp"]))
+    return _decode4(codes, e)
+
+
+def _plain_attend(st):
+    """Sequences padded to the most query tokens of any; a query head's rows stand beside those of its group."""
+    c = st["case"]
+    B, Hq, Hkv, d = c["batch"], c["q_heads"], c["kv_heads"], c["d"]
+    G = Hq // Hkv
+    lens, first = st["lens"].long(), st["first"].long()
+    news = first[1:] - first[:-1]
+    m = min(c.get("tokens", 1), c["length"])
+    i = torch.arange(m, device=DEV)[None, :]
+    real = i < news[:, None]
+    row = (first[:-1, None] + i).clamp(max=st["q"].shape[0] - 1)
+    q = st["q"].float()[row].view(B, m, Hkv, G, d).permute(0, 2, 3, 1, 4).reshape(B, Hkv, G * m, d)
+    K = _values(st, "k")
+    n = K.shape[2]
+    s = torch.matmul(q, K.transpose(-1, -2).contiguous()).mul_(1.0 / math.sqrt(d)).view(B, Hkv, G, m, n)
+    mine = (lens[:, None] - news[:, None] + i)[..., None]
+    at = torch.arange(n, device=DEV)
+    seen = at <= mine
+    if c["window"]:
+        seen = seen & ((at > mine - c["window"]) | (at < c["n_sink"]))
+    s.masked_fill_(~seen[:, None, None], -math.inf)
+    s.sub_(s.amax(-1, keepdim=True)).exp_()
+    s.div_(s.sum(-1, keepdim=True))
+    o = torch.matmul(s.view(B, Hkv, G * m, n), _values(st, "v"))
+    o = o.view(B, Hkv, G, m, d).permute(0, 3, 1, 2, 4).reshape(B, m, Hq, d)
+    st["out"][row[real]] = o[real].to(st["out"].dtype)
+    if not c.get("scores"):
+        return [st["out"]]
+    p = s.view(B, Hkv, G, n).sum(2)
+    page, h = st["page_table"].long()[:, at // c["page"]], torch.arange(Hkv, device=DEV)
+    rows = (page[:, None], h[None, :, None], (at % c["page"])[None, None])
+    st["score"][rows] += torch.where(seen[:, 0, None], p, torch.zeros_like(p))
+    return [st["out"], st["score"]]
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"norm": _plain_norm, "map": _plain_map, "put": _plain_put, "step": _plain_attend, "attend": _plain_attend}[
+        state["case"]["kind"]](state)
+
+
+# ---- the definitions, in 64 bits ----------------------------------------------------------
+
+def _exact_norm(st):
+    c = st["case"]
+    done = []
+    turn = 2.0 * math.pi
+    for x, w in (("Q", st["wq"]), ("K", st["wk"])):
+        out = torch.empty(st[x].shape, dtype=torch.float64, device=DEV)
+        for h in range(st[x].shape[1]):
+            y = st[x][:, h].double()
+            out[:, h] = w.double() * y / torch.sqrt((y * y).sum(-1, keepdim=True) / c["d"] + EPS)
+            for i in range(c["rot"] // 2):
+                # turns, so that the sine is asked for less than one of them
+                t = st["positions"].double() * (math.exp(-2.0 * i / c["rot"] * math.log(c["base"])) / turn)
+                z = torch.polar(torch.ones_like(t), (t - t.floor()) * turn) * torch.complex(out[:, h, :, i], out[:, h, :, i + c["rot"] // 2])
+                out[:, h, :, i], out[:, h, :, i + c["rot"] // 2] = z.real, z.imag
+        done.append(out)
+    return done
+
+
+def _nearest(x, grid):
+    """Nearest of the rising magnitudes in `grid`; in the middle, the one of even number."""
+    a, best, off = x.abs(), torch.zeros_like(x), torch.full_like(x, math.inf)
+    for k, g in enumerate(grid):
+        d = (a - g).abs()
+        take = (d < off) | ((d == off) & (k % 2 == 0))
+        best, off = torch.where(take, torch.full_like(x, g), best), torch.where(take, d, off)
+    return torch.where(x < 0, -best, best)
+
+
+def _exact_put(st):
+    c = st["case"]
+    if c["rows"] == "fp4":
+        block, most, grid = 32, 6.0, [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+    else:
+        block, most = c["d"], 448.0
+        grid = [m / 512.0 for m in range(8)] + [(1.0 + m / 8.0) * 2.0 ** e for e in range(-6, 9) for m in range(8)][:-1]
+    done = []
+    for x in ("K", "V"):
+        y = st[x].double()
+        if c["rows"] != "own":
+            y = y.unflatten(-1, (-1, block))
+            top = y.abs().amax(-1, keepdim=True)
+            e = torch.ceil(torch.log2(top.clamp(min=1e-300) / most)).clamp(min=-120.0)
+            e = torch.where(top > most * torch.exp2(e), e + 1, e)
+            e = torch.where((top <= most * torch.exp2(e - 1)) & (e > -120.0), e - 1, e)
+            e = torch.where(top > 0, e, torch.zeros_like(e))
+            y = (_nearest(y / torch.exp2(e), grid) * torch.exp2(e)).flatten(-2)
+        done.append(torch.where((st["slots"] >= 0)[:, None, None], y, torch.zeros_like(y)))
+    return done
+
+
+def _exact_attend(st):
+    c, page = st["case"], st["case"]["page"]
+    G, d = c["q_heads"] // c["kv_heads"], c["d"]
+    out = torch.zeros(st["out"].shape, dtype=torch.float64, device=DEV)
+    score = st["score"].double() if c.get("scores") else None
+    lens, first, table = _lengths(c), st["first"].tolist(), st["page_table"].long()
+    grid = torch.tensor([s * g for s in (1.0, -1.0) for g in GRID], dtype=torch.float64, device=DEV)
+    for b in range(c["batch"]):
+        n, q0, q1 = lens[b], first[b], first[b + 1]
+        j = torch.arange(n, device=DEV)
+        pg, r = table[b, j // page], j % page
+        for h in range(c["kv_heads"] if q1 > q0 else 0):
+            x = []
+            for pool in ("k", "v"):
+                byte = st[pool][pg, h, r].long()
+                y = torch.empty((n, d), dtype=torch.float64, device=DEV)
+                y[:, 0::2], y[:, 1::2] = grid[byte % 16], grid[byte // 16]
+                x.append(y * torch.exp2(st[pool + "_exp"][pg, h, r].double()).repeat_interleave(32, 1))
+            for a in range(q0, q1, 512):
+                z = min(a + 512, q1)
+                i = torch.arange(n - q1 + a, n - q1 + z, device=DEV)[:, None]
+                seen = j[None, :] <= i
+                if c["window"]:
+                    seen &= (j[None, :] > i - c["window"]) | (j[None, :] < c["n_sink"])
+                for g in range(G):
+                    s = st["q"][a:z, h * G + g].double() @ x[0].T / math.sqrt(d)
+                    s = torch.where(seen, s, -math.inf)
+                    p = torch.exp(s - s.max(-1, keepdim=True).values)
+                    p = p / p.sum(-1, keepdim=True)
+                    out[a:z, h * G + g] = p @ x[1]
+                    if score is not None:
+                        score[pg, h, r] += p.sum(0)
+    return [out] + ([score] if score is not None else [])
+
+
+def exact(case, seed):
+    if case["kind"] == "map":
+        return None  # whole numbers only: nothing is rounded
+    st = prepare(case, seed)
+    return {"norm": _exact_norm, "put": _exact_put, "step": _exact_attend, "attend": _exact_attend}[case["kind"]](st)
