@@ -289,9 +289,8 @@ def prepare(case, seed):
         n_pages = -(-T // page) + 3
         st["K"] = (torch.randn((T, kv, d), generator=gen, device=DEV) * channels(kv, d)).to(DTYPES[c["dtype"]])
         st["V"] = rnd(T, kv, d, dtype=c["dtype"])
-        st["slots"] = torch.randperm(n_pages * page, generator=gen, device=DEV)[:T]
         # rows of sequences: runs of tokens in neighbouring rows of a page
-        runs = torch.randperm(-(-T // page) + 3, generator=gen, device=DEV)
+        runs = torch.randperm(n_pages, generator=gen, device=DEV)
         t = torch.arange(T, device=DEV)
         st["slots"] = runs[t // page] * page + t % page
         st["slots"] = torch.where(chance(T) < c["idle"], torch.full_like(t, -1), st["slots"]).contiguous()
