@@ -362,13 +362,20 @@ typedef struct {
   int32_t n_pages;     /* pages of the pool                                                 */
   int32_t max_pages;   /* columns of page_table                                             */
   d2o_view K, V;       /* the pool: stride_b between pages, stride_h between KV heads,      */
-                       /* stride_n between rows, in elements (bytes when cache_fp8)         */
+                       /* stride_n between rows, in elements (bytes when cache_fp8 or _fp4) */
   int8_t* K_exp;       /* [n_pages][Hkv][page_size] powers of two of fp8 rows, else NULL    */
   int8_t* V_exp;
   float* score;        /* [n_pages][Hkv][page_size] accumulated attention, NULL: not kept   */
   int32_t* pos;        /* [n_pages][Hkv][page_size] token position of an entry, NULL: entry */
                        /* s has position s                                                  */
   const int32_t* page_table; /* [B][max_pages]                                              */
+  int32_t cache_fp4;   /* 1: a row is d E2M1 codes (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4 and 6), two to a byte, the even   */
+                       /* element in the low half, and d / 32 powers of two: K_exp and V_exp are                         */
+                       /* [n_pages][Hkv][page_size][d / 32], from a 4-byte boundary, strides of K and V in bytes.  A     */
+                       /* block of 32 elements has the smallest power of two with which 6 reaches its largest            */
+                       /* magnitude, -120 to 125 (larger values become 6 * 2^125), its elements the nearest codes (in    */
+                       /* the middle of two the even one); a block with an infinity or NaN has -128, and is NaN as a     */
+                       /* whole.  D2O_BF16 only, and not together with cache_fp8.                                        */
 } d2o_pages;
 
 /* Bytes of the workspace that the three calls below need while no sequence (fill: no prompt) has more than
@@ -407,6 +414,62 @@ int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view 
  * max_len as for d2o_pages_step.  Errors: INVALID_ARG (budget < max(1, n_sink + recent)), UNSUPPORTED, CAPACITY, HIP. */
 int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int32_t max_len, int32_t budget, int32_t recent,
                     int32_t n_sink, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- What a server does around a step over pages: norms and rotation, block tables and slots, rows of single tokens ---- */
+
+/* Queries and keys of every head to unit length and into place: y = w x / sqrt(mean(x^2) + eps) over the d elements of a row, then for c < rot_dim / 2
+ * elements c and c + rot_dim / 2 are turned by the angle position * rope_base^(-2 c / rot_dim) (the pairs of d2o_qkv_project); elements from
+ * rot_dim on are not.  Q, Q_out: [batch][Hq][n][d]; K, K_out: [batch][Hkv][n][d] (views as for d2o_window_attend: packed tokens [token][head][d]
+ * are batch 1 with their strides; no Q or no K: 0 heads, its views are not looked at).  Q_out may be Q itself and K_out K, but no
+ * output may overlap an input otherwise.  q_weight, k_weight: device [d] in `dtype`, NULL: ones.  positions: device [batch][n], of any sign; NULL: pos0 + token.
+ * Angles are reduced in 64 bits, sums and the rest are fp32, and a result is rounded once; rows of finite values of any magnitude have finite norms.
+ * rot_dim: a multiple of 16 from 0 to d; eps from 1e-20 to 1; rope_base above 1.  D2O_F32 and D2O_BF16, d = 64 or 128.  Enqueues only.
+ * Errors: INVALID_ARG, UNSUPPORTED (also more than 2^28 tokens or 65535 heads), HIP. */
+int d2o_qk_norm_rope(int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                     d2o_view Q, d2o_view K, const void* q_weight, const void* k_weight, double eps, int32_t rot_dim,
+                     const int32_t* positions, int32_t pos0, double rope_base, d2o_view Q_out, d2o_view K_out,
+                     void* stream);
+
+/* Block tables and slots for the next call over pages.  Sequence b has lens[b] entries (taken within what its row of page_table can name) and gains
+ * change[b] tokens, or loses its last -change[b] entries (at most all it has).  What it gains lies behind its entries; it takes the pages that are missing from
+ * the list of free pages and enters them in page_table [batch][max_pages].  The list is a ring of n_pages places, free_pages, in which free_state[1] pages stand
+ * from place free_state[0] on: pages are taken from its head, and those that hold no entry any more go to its end, to be taken by later calls, in
+ * the order of sequences and pages.  A sequence gains all its tokens or none: all, if its own wishes and those of the sequences before it, whether they came true or not, are
+ * at most max_tokens tokens and free_state[1] pages (one that needs no page: the former alone); a wish beyond the row of the page table counts as none.
+ * Written are lens_out and free_state_out (which may be lens and free_state themselves), first [batch + 1] (the new tokens of sequence b are
+ * rows first[b] .. first[b + 1] - 1 of packed tokens) and, for each of max_tokens rows, its slot, page * page_size + row of the page, and its position, the
+ * entry's number (rows that no token has: slot -1, position 0).  Entries of page_table behind a sequence's last page are left as they were.
+ * All arrays are device memory and, but for the two pairs, apart.  Pages in the ring and in use have to be pages of the pool, once each: one outside it gives slot -1 (and
+ * stands for no page in the calls above), and what does not fit the ring is dropped.
+ * page_size: as in d2o_pages.  Enqueues only.  Errors: INVALID_ARG, UNSUPPORTED (batch * max_pages / 1024 beyond 2^24), CAPACITY (workspace smaller than
+ * d2o_pages_map_workspace_bytes says; where it says 0, NULL will do), HIP. */
+int d2o_pages_map_workspace_bytes(int32_t batch, int32_t max_pages, int32_t max_tokens, size_t* bytes);
+int d2o_pages_map(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max_pages, int32_t* page_table,
+                  const int32_t* lens, const int32_t* change, int32_t* free_pages, const int32_t* free_state,
+                  int32_t max_tokens, int32_t* lens_out, int32_t* free_state_out, int32_t* first, int64_t* slots,
+                  int32_t* positions, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of packed tokens into the pool and out of it.  K, V: [n_tokens][Hkv][d] in `dtype` (stride_n between tokens, stride_h between heads, stride_b unused);
+ * slots: device [n_tokens], page * page_size + row of the page; a token whose slot lies outside the pool is left out.
+ * put stores K and V in the rows' format, score 0, and positions[t] (device [n_tokens]; NULL only if the pages keep none).  Slots that are written are all different.
+ * get reads rows back as values (8-bit and 4-bit rows: exactly what they stand for); K and V of tokens that are left out stay as they were.
+ * pages->page_table is checked but not looked at.  Enqueues only, needs no workspace.  Errors: INVALID_ARG, UNSUPPORTED (also more than 2^26 tokens), HIP. */
+int d2o_pages_put(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_tokens, const int64_t* slots,
+                  const int32_t* positions, void* stream);
+int d2o_pages_get(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_tokens, const int64_t* slots, void* stream);
+
+/* Attention of several new tokens per sequence over pages of 4-bit rows (cache_fp4), which hold them already.  q, out: [n_tokens][Hq][d] packed (stride_n
+ * between tokens, stride_h between heads, stride_b unused); rows first[b] .. first[b + 1] - 1 (device [B + 1], taken within [0, n_tokens]) are the last tokens of
+ * sequence b, the newest of them its entry lens[b] - 1.  Each sees the entries up to its own that have a position > its own - window or < n_sink (window = 0: all);
+ * positions: device [n_tokens], NULL: the entry's number.  lens and max_len as for d2o_pages_step (a sequence that claims more is cut to it); tokens without an entry, or
+ * that see none, get zeros.  Rows of out that belong to no sequence are left as they were.  Scores are neither read nor added to.  A weight
+ * holds 16 bits, sums 24; NaN of a row reaches the tokens that see it and no others; out may be q itself.
+ * Errors: INVALID_ARG, UNSUPPORTED (rows that are not of 4 bits; too many tokens for a launch), CAPACITY (max_len beyond the page table; workspace smaller than
+ * d2o_pages_attend_workspace_bytes says, which grows with n_tokens up to a bound and falls again; where it says 0, NULL will do), HIP. */
+int d2o_pages_attend_workspace_bytes(const d2o_pages* pages, int32_t n_tokens, int32_t max_len, size_t* bytes);
+int d2o_pages_attend(const d2o_pages* pages, d2o_view q, int32_t n_tokens, const int32_t* first, const int32_t* lens,
+                     const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* Kernel timing aid for benchmarks (not part of the method).  While enabled (on >= 1), launches
  * of the kernels below are bracketed by two HIP events recorded on the launch stream: every

@@ -25,6 +25,8 @@ EXPORTS = [
     "d2o_prefill_events", "d2o_timing_enable", "d2o_timing_read",
     "d2o_window_workspace_bytes", "d2o_window_attend", "d2o_pages_workspace_bytes", "d2o_pages_fill",
     "d2o_pages_step", "d2o_pages_evict",
+    "d2o_qk_norm_rope", "d2o_pages_map_workspace_bytes", "d2o_pages_map", "d2o_pages_put", "d2o_pages_get",
+    "d2o_pages_attend_workspace_bytes", "d2o_pages_attend",
 ]
 
 
@@ -51,7 +53,7 @@ class d2o_pages(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("cache_fp8", C.c_int32),
                 ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
                 ("K", d2o_view), ("V", d2o_view), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p),
-                ("score", C.c_void_p), ("pos", C.c_void_p), ("page_table", C.c_void_p)]
+                ("score", C.c_void_p), ("pos", C.c_void_p), ("page_table", C.c_void_p), ("cache_fp4", C.c_int32)]
 
 
 _lib = None
@@ -107,6 +109,14 @@ def load_library() -> C.CDLL:
     lib.d2o_pages_fill.argtypes = [P(d2o_pages), d2o_view, d2o_view, i32, vp, vp, i32, i32, i32, vp, sz, vp]
     lib.d2o_pages_step.argtypes = [P(d2o_pages), d2o_view, d2o_view, d2o_view, vp, vp, i32, i32, i32, d2o_view, vp, sz, vp]
     lib.d2o_pages_evict.argtypes = [P(d2o_pages), vp, i32, i32, i32, i32, vp, sz, vp]
+    lib.d2o_qk_norm_rope.argtypes = [i32, i32, i32, i32, i32, i32, d2o_view, d2o_view, vp, vp, C.c_double, i32, vp, i32,
+                                     C.c_double, d2o_view, d2o_view, vp]
+    lib.d2o_pages_map_workspace_bytes.argtypes = [i32, i32, i32, P(sz)]
+    lib.d2o_pages_map.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.d2o_pages_put.argtypes = [P(d2o_pages), d2o_view, d2o_view, i32, vp, vp, vp]
+    lib.d2o_pages_get.argtypes = [P(d2o_pages), d2o_view, d2o_view, i32, vp, vp]
+    lib.d2o_pages_attend_workspace_bytes.argtypes = [P(d2o_pages), i32, i32, P(sz)]
+    lib.d2o_pages_attend.argtypes = [P(d2o_pages), d2o_view, i32, vp, vp, vp, i32, i32, i32, d2o_view, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("d2o_destroy", "d2o_last_error"):
             getattr(lib, name).restype = C.c_int
@@ -496,7 +506,8 @@ class Pages:
     """A cache in pages over the caller's tensors, and the workspace of the calls on it.
 
     K, V: pools [n_pages, Hkv, page_size, d], float32 or bfloat16, or uint8 codes with int8 K_exp, V_exp
-    [n_pages, Hkv, page_size] (8-bit rows of bfloat16 tensors); page_table int32 [B, max_pages]; score float32 and pos int32
+    [n_pages, Hkv, page_size] (8-bit rows of bfloat16 tensors), or uint8 pairs of codes [n_pages, Hkv, page_size, d / 2] with
+    K_exp, V_exp [n_pages, Hkv, page_size, d / 32] (4-bit rows); page_table int32 [B, max_pages]; score float32 and pos int32
     [n_pages, Hkv, page_size] where accumulated attention and token positions are kept.  max_len: the most entries a sequence
     (or tokens a prompt) will have in any call, the page table's capacity if None.  Calls on one object
     share its workspace: on streams (or in graphs) that overlap in time, use an object each, and keep it until they are done."""
@@ -504,21 +515,25 @@ class Pages:
     def __init__(self, K, V, page_table, n_q_heads, K_exp=None, V_exp=None, score=None, pos=None, max_len=None):
         self.lib = load_library()
         _need(isinstance(K, torch.Tensor) and K.is_cuda and K.dim() == 4, "K: a pool [n_pages, Hkv, page_size, d] on a GPU is needed")
-        fp8 = K.dtype == torch.uint8
-        _need(fp8 or K.dtype in _DTYPE_CODES, "pools hold float32 or bfloat16 rows, or uint8 codes")
-        self.device, self.dtype = K.device, torch.bfloat16 if fp8 else K.dtype
+        codes = K.dtype == torch.uint8
+        _need(codes or K.dtype in _DTYPE_CODES, "pools hold float32 or bfloat16 rows, or uint8 codes")
+        fp4 = codes and isinstance(K_exp, torch.Tensor) and K_exp.dim() == 4
+        fp8 = codes and not fp4
+        self.device, self.dtype = K.device, torch.bfloat16 if codes else K.dtype
         n_pages, Hkv, page_size, d = K.shape
+        d = 2 * d if fp4 else d
         _tensor_ok(K, K.shape, K.dtype, self.device, "K")
         _tensor_ok(V, K.shape, K.dtype, self.device, "V")
         _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table: an int32 tensor [B, max_pages] is needed")
         _vector_ok(page_table, page_table.shape, torch.int32, self.device, "page_table")
         per_row = (n_pages, Hkv, page_size)
-        _need((K_exp is not None and V_exp is not None) == fp8 and (fp8 or (K_exp is None and V_exp is None)),
+        _need((K_exp is not None and V_exp is not None) == codes and (codes or (K_exp is None and V_exp is None)),
               "K_exp and V_exp belong to pools of uint8 codes")
-        for t, dt, what in ((K_exp, torch.int8, "K_exp"), (V_exp, torch.int8, "V_exp"), (score, torch.float32, "score"),
-                            (pos, torch.int32, "pos")):
+        per_exp = (*per_row, d // 32) if fp4 else per_row
+        for t, shape, dt, what in ((K_exp, per_exp, torch.int8, "K_exp"), (V_exp, per_exp, torch.int8, "V_exp"),
+                                   (score, per_row, torch.float32, "score"), (pos, per_row, torch.int32, "pos")):
             if t is not None:
-                _vector_ok(t, per_row, dt, self.device, what)
+                _vector_ok(t, shape, dt, self.device, what)
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         B, max_pages = page_table.shape
         self.tensors = (K, V, page_table, K_exp, V_exp, score, pos)
@@ -527,7 +542,7 @@ class Pages:
         _int32_ok(n_q_heads, self.max_len, n_pages)
         self.desc = d2o_pages(B, n_q_heads, Hkv, d, _DTYPE_CODES[self.dtype], 1 if fp8 else 0, page_size, n_pages,
                               max_pages, _view_of(K), _view_of(V), ptr(K_exp), ptr(V_exp), ptr(score), ptr(pos),
-                              page_table.data_ptr())
+                              page_table.data_ptr(), 1 if fp4 else 0)
         self._ref = C.byref(self.desc)
         self._bound = min(self.max_len, max_pages * page_size)  # of every sequence's entries
         need = C.c_size_t()
@@ -578,6 +593,136 @@ class Pages:
         _int32_ok(budget, recent, n_sink)
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_evict(
             self._ref, self._lens(lens), self._bound, budget, recent, n_sink, *self._ws, stream)), "d2o_pages_evict")
+
+    def _packed(self, t, heads, what, n=None):
+        """A view of packed tokens [n, heads, d]."""
+        _need(isinstance(t, torch.Tensor) and t.dim() == 3, f"{what}: a tensor [tokens, heads, d] is needed")
+        _tensor_ok(t, (t.shape[0] if n is None else n, heads, self.head_dim), self.dtype, self.device, what)
+        return d2o_view(t.data_ptr(), 0, t.stride(1) if heads > 1 else 0, t.stride(0) if t.shape[0] > 1 else 0)
+
+    def _slots(self, K, V, slots):
+        k = self._packed(K, self.n_kv_heads, "K")
+        n = K.shape[0]
+        _vector_ok(slots, (n,), torch.int64, self.device, "slots")
+        return k, self._packed(V, self.n_kv_heads, "V", n), n, slots.data_ptr()
+
+    def d2o_pages_put(self, K, V, slots, positions=None):
+        """Tokens' rows K, V [n, Hkv, d] into slots (int64 [n], as d2o_pages_map gives them; outside the pool: left out), with score 0 and, where
+        the pages keep positions, positions (int32 [n])."""
+        k, v, n, at = self._slots(K, V, slots)
+        if positions is not None:
+            _vector_ok(positions, (n,), torch.int32, self.device, "positions")
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_put(
+            self._ref, k, v, n, at, None if positions is None else positions.data_ptr(), stream)), "d2o_pages_put")
+
+    def d2o_pages_get(self, slots, K, V):
+        """Rows of slots (int64 [n]) as values into K, V [n, Hkv, d]; rows of slots outside the pool stay as they were."""
+        k, v, n, at = self._slots(K, V, slots)
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_get(self._ref, k, v, n, at, stream)), "d2o_pages_get")
+
+    def d2o_pages_attend(self, q, first, lens, out, positions=None, window=0, n_sink=0):
+        """Attention of several new tokens per sequence, whose rows the pages (of 4-bit rows) hold already: q, out [n, Hq, d] packed;
+        first int32 [B + 1]: rows first[b] .. first[b + 1] - 1 are the last tokens of sequence b; lens int32 [B], those included;
+        positions int32 [n], None: the entries' numbers."""
+        qv = self._packed(q, self.n_q_heads, "q")
+        n = q.shape[0]
+        ov = self._packed(out, self.n_q_heads, "out", n)
+        _vector_ok(first, (self.batch + 1,), torch.int32, self.device, "first")
+        at = self._lens(lens)
+        if positions is not None:
+            _vector_ok(positions, (n,), torch.int32, self.device, "positions")
+        _int32_ok(window, n_sink, n)
+        need = C.c_size_t()
+        _ok(self.lib.d2o_pages_attend_workspace_bytes(self._ref, n, self._bound, C.byref(need)), "d2o_pages_attend_workspace_bytes")
+
+        def call(stream):
+            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+            return self.lib.d2o_pages_attend(self._ref, qv, n, first.data_ptr(), at, None if positions is None else positions.data_ptr(),
+                                             self._bound, window, n_sink, ov, None if ws is None else ws.data_ptr(), need.value,
+                                             stream)
+        _ok(_enqueue(self.device, call), "d2o_pages_attend")
+
+
+def d2o_qk_norm_rope(Q, K, q_weight=None, k_weight=None, eps: float = 1e-6, positions=None, pos0: int = 0,
+                     rope_base: float = 10000.0, rot_dim=None, Q_out=None, K_out=None):
+    """Norms of queries and keys of every head, with the rotation by position: Q [B, Hq, n, d], K [B, Hkv, n, d] (any strides, d contiguous;
+    either may be None), weights [d] (None: ones), positions int32 [B, n] (None: pos0 + token), rot_dim: elements that are turned
+    (None: all).  Outputs are made here where None; Q_out may be Q itself and K_out K.  Returns (Q_out, K_out)."""
+    lib = load_library()
+    one = Q if Q is not None else K
+    _need(isinstance(one, torch.Tensor) and one.is_cuda and one.dim() == 4 and one.dtype in _DTYPE_CODES,
+          "Q and K: four-dimensional float32 or bfloat16 tensors on a GPU are needed")
+    B, _, n, d = one.shape
+    dev, dt = one.device, one.dtype
+    views, outs, heads = [], [], []
+    for x, y, w, what in ((Q, Q_out, q_weight, "Q"), (K, K_out, k_weight, "K")):
+        if x is None:
+            _need(y is None, f"{what}_out belongs to {what}")
+            views += [_NULL_VIEW, _NULL_VIEW]
+            outs.append(None)
+            heads.append(0)
+            continue
+        _need(isinstance(x, torch.Tensor) and x.dim() == 4, f"{what}: a tensor [B, heads, n, d] is needed")
+        _tensor_ok(x, (B, x.shape[1], n, d), dt, dev, what)
+        if y is None:
+            y = torch.empty(x.shape, dtype=dt, device=dev)
+        _tensor_ok(y, x.shape, dt, dev, what + "_out")
+        if w is not None:
+            _vector_ok(w, (d,), dt, dev, what.lower() + "_weight")
+        views += [_view_of(x), _view_of(y)]
+        outs.append(y)
+        heads.append(x.shape[1])
+    if positions is not None:
+        _vector_ok(positions, (B, n), torch.int32, dev, "positions")
+    rot_dim = d if rot_dim is None else rot_dim
+    _int32_ok(B, n, pos0, rot_dim)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _ok(_enqueue(dev, lambda stream: lib.d2o_qk_norm_rope(
+        B, n, heads[0], heads[1], d, _DTYPE_CODES[dt], views[0], views[2], ptr(q_weight), ptr(k_weight), eps, rot_dim,
+        ptr(positions), pos0, rope_base, views[1], views[3], stream)), "d2o_qk_norm_rope")
+    return outs[0], outs[1]
+
+
+def d2o_pages_map(page_table, lens, change, free_pages, free_state, page_size: int, max_tokens=None, first=None, slots=None,
+                  positions=None, lens_out=None, free_state_out=None):
+    """Block tables and slots from lengths: sequence b of lens[b] entries gains change[b] tokens (or loses -change[b]), all or none;
+    pages come from the ring free_pages (int32 [pages of the pool], free_state int32 [2]: place of the first, how many) and go
+    back to its end.  page_table int32 [B, max_pages], lens, change int32 [B].  Written: page_table, free_pages, lens_out and
+    free_state_out (None: lens and free_state themselves), first int32 [B + 1], slots int64 and positions int32 [max_tokens] (made
+    here where None).  Returns (lens_out, first, slots, positions)."""
+    lib = load_library()
+    _need(isinstance(page_table, torch.Tensor) and page_table.is_cuda and page_table.dim() == 2,
+          "page_table: an int32 tensor [B, max_pages] on a GPU is needed")
+    B, max_pages = page_table.shape
+    dev, i32 = page_table.device, torch.int32
+    _vector_ok(page_table, (B, max_pages), i32, dev, "page_table")
+    _need(isinstance(free_pages, torch.Tensor) and free_pages.dim() == 1, "free_pages: an int32 tensor [pages] is needed")
+    if max_tokens is None:
+        _need(isinstance(slots, torch.Tensor) and slots.dim() == 1, "max_tokens, or slots, an int64 tensor [tokens], is needed")
+        max_tokens = slots.shape[0]
+    _int32_ok(B, max_pages, max_tokens, page_size, free_pages.shape[0])
+    _need(max_tokens >= 0, "max_tokens: not negative")
+    lens_out = lens if lens_out is None else lens_out
+    free_state_out = free_state if free_state_out is None else free_state_out
+    first = torch.empty(B + 1, dtype=i32, device=dev) if first is None else first
+    slots = torch.empty(max_tokens, dtype=torch.int64, device=dev) if slots is None else slots
+    positions = torch.empty(max_tokens, dtype=i32, device=dev) if positions is None else positions
+    for t, n, dt, what in ((lens, B, i32, "lens"), (change, B, i32, "change"), (lens_out, B, i32, "lens_out"),
+                           (free_pages, free_pages.shape[0], i32, "free_pages"), (free_state, 2, i32, "free_state"),
+                           (free_state_out, 2, i32, "free_state_out"), (first, B + 1, i32, "first"),
+                           (slots, max_tokens, torch.int64, "slots"), (positions, max_tokens, i32, "positions")):
+        _vector_ok(t, (n,), dt, dev, what)
+    need = C.c_size_t()
+    _ok(lib.d2o_pages_map_workspace_bytes(B, max_pages, max_tokens, C.byref(need)), "d2o_pages_map_workspace_bytes")
+
+    def call(stream):
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+        return lib.d2o_pages_map(B, page_size, free_pages.shape[0], max_pages, page_table.data_ptr(), lens.data_ptr(),
+                                 change.data_ptr(), free_pages.data_ptr(), free_state.data_ptr(), max_tokens,
+                                 lens_out.data_ptr(), free_state_out.data_ptr(), first.data_ptr(), slots.data_ptr(),
+                                 positions.data_ptr(), None if ws is None else ws.data_ptr(), need.value, stream)
+    _ok(_enqueue(dev, call), "d2o_pages_map")
+    return lens_out, first, slots, positions
 
 
 KERNEL_IDS = {"attn_fwd": 0, "colsum": 1, "select": 2, "match_filter": 3, "match_refine": 4,

@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["d2o_host.hip", "prefill_f32.hip", "prefill_bf16.hip", "tokens.hip", "decode.hip", "decode_split.hip", "append.hip", "qkv.hip", "fp8.hip",
-           "window.hip", "pages_step.hip", "pages_evict.hip"]
+           "window.hip", "pages_step.hip", "pages_evict.hip", "pages_fp4.hip", "pages_rows.hip",
+           "pages_map.hip", "qk_norm.hip"]
 LIB = os.environ.get("D2O_LIB", os.path.join(HERE, "libd2o.so"))
 # Matrix-core results straight into vector registers: the kernels of tokens.hip post-process
 # every accumulator element on the vector ALU, and a copy out of the accumulation registers per

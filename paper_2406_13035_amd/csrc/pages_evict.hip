@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "fp4.h"
 #include "pages.h"
 
 namespace d2o {
@@ -362,7 +363,11 @@ __device__ __forceinline__ void put_row(const FillArgs& a, int bh, int b, int hk
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     uint8_t* dst = which ? a.pool.v_at(page, hk, s) : a.pool.k_at(page, hk, s);
-    if constexpr (sizeof(CT) == 1) {
+    if constexpr (std::is_same_v<CT, Code4>) {
+      int e;
+      reinterpret_cast<uint32_t*>(dst)[c] = fp4_encode_block(t[which], e);
+      if (c % 4 == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at * (D / kBlock4) + c / 4] = int8_t(e);
+    } else if constexpr (sizeof(CT) == 1) {
       float f[kE], m = 0.f;
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
@@ -407,7 +412,21 @@ struct EvictArgs {
   int32_t* guarded;  // [B][Hkv][slices] its protected entries
   uint32_t* cand;    // [B][Hkv][slices * extra][3] its lowest entries, as many as the sequence gives up: score's key, position's, entry | protected << 31
   int32_t max_len, budget, recent, n_sink, most, slices, extra;
+  int32_t exps;      // bytes of powers of two of a row: 0, 1, 2 or 4
 };
+
+// A row's powers of two as one number.
+__device__ __forceinline__ uint32_t load_exps(const int8_t* p, int64_t at, int exps) {
+  return exps == 4 ? reinterpret_cast<const uint32_t*>(p)[at] : exps == 2 ? reinterpret_cast<const uint16_t*>(p)[at] : exps == 1 ? uint8_t(p[at]) : 0u;
+}
+__device__ __forceinline__ void store_exps(int8_t* p, int64_t at, int exps, uint32_t v) {
+  if (exps == 4)
+    reinterpret_cast<uint32_t*>(p)[at] = v;
+  else if (exps == 2)
+    reinterpret_cast<uint16_t*>(p)[at] = uint16_t(v);
+  else if (exps == 1)
+    p[at] = int8_t(v);
+}
 constexpr int kInline = 512;  // moves of a head that the workgroup which chose them makes itself (256 rows of 32 heads: 15.7 us,
                               // in a launch of their own 18)
 
@@ -420,7 +439,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int hk, con
     u32x4 k[N], v[N];
     float score[N];
     int32_t pos[N], to[N], pt[N];
-    int8_t ke[N], ve[N];
+    uint32_t ke[N], ve[N];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const bool is = i + u * step < pairs;
@@ -435,8 +454,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int hk, con
       v[u] = reinterpret_cast<const u32x4*>(a.pool.v_at(page, hk, src))[c];
       score[u] = a.pool.score[at];
       pos[u] = a.pool.pos[at];
-      ke[u] = a.pool.k_exp ? a.pool.k_exp[at] : 0;
-      ve[u] = a.pool.k_exp ? a.pool.v_exp[at] : 0;
+      ke[u] = load_exps(a.pool.k_exp, at, a.exps);
+      ve[u] = load_exps(a.pool.v_exp, at, a.exps);
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -447,10 +466,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int hk, con
         const int64_t at = a.pool.at(pt[u], hk, to[u]);
         a.pool.score[at] = score[u];
         a.pool.pos[at] = pos[u];
-        if (a.pool.k_exp) {
-          a.pool.k_exp[at] = ke[u];
-          a.pool.v_exp[at] = ve[u];
-        }
+        store_exps(a.pool.k_exp, at, a.exps, ke[u]);
+        store_exps(a.pool.v_exp, at, a.exps, ve[u]);
       }
     }
   }
@@ -1002,7 +1019,9 @@ extern "C" int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, in
     else
       write(t, ct, std::integral_constant<int, 128>{});
   };
-  if (pages->cache_fp8)
+  if (pages->cache_fp4)
+    rows(uint16_t{}, Code4{});
+  else if (pages->cache_fp8)
     rows(uint16_t{}, uint8_t{});
   else if (pages->dtype == D2O_BF16)
     rows(uint16_t{}, uint16_t{});
@@ -1038,7 +1057,8 @@ extern "C" int d2o_pages_evict(const d2o_pages* pages, const int32_t* lens, int3
   a.guarded = a.newest + round256(size_t(bh) * a.slices * sizeof(int32_t)) / sizeof(int32_t);
   a.cand = reinterpret_cast<uint32_t*>(a.guarded + round256(size_t(bh) * a.slices * sizeof(int32_t)) / sizeof(int32_t));
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const int lanes = pages->head_dim * (pages->cache_fp8 ? 1 : pages->dtype == D2O_BF16 ? 2 : 4) / 16;
+  a.exps = pages->cache_fp4 ? pages->head_dim / kBlock4 : pages->cache_fp8;
+  const int lanes = pages->cache_fp4 ? pages->head_dim / 32 : pages->head_dim * (pages->cache_fp8 ? 1 : pages->dtype == D2O_BF16 ? 2 : 4) / 16;
   const dim3 heads{unsigned(bh)};
   // More than the registers of a workgroup hold: in slices where few go (one of 8 x 26214 entries 24 us, by a workgroup per head that reads them
   // again for every use 44; of 8 x 131072 25 and 184; 256 of 8 x 26214 42 and 100), by that workgroup where slices would leave as many candidates.

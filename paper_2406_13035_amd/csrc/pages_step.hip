@@ -2,7 +2,7 @@
 // over the entries that its window shows, and the softmax rows are added to the entries' scores.
 #include <algorithm>
 
-#include "pages.h"
+#include "pages_step.h"
 
 namespace d2o {
 
@@ -20,8 +20,8 @@ bool rows_apart(const d2o_view& v, const int32_t (&counts)[3], int d) {
   return true;
 }
 bool pages_apart(const d2o_pages* p) {
-  const int32_t counts[3] = {p->n_pages, p->n_kv_heads, p->page_size};
-  return rows_apart(p->K, counts, p->head_dim) && rows_apart(p->V, counts, p->head_dim);
+  const int32_t counts[3] = {p->n_pages, p->n_kv_heads, p->page_size}, row = p->cache_fp4 ? p->head_dim / 2 : p->head_dim;
+  return rows_apart(p->K, counts, row) && rows_apart(p->V, counts, row);
 }
 
 int check_pages(const d2o_pages* p, PagePool* out) {
@@ -32,13 +32,16 @@ int check_pages(const d2o_pages* p, PagePool* out) {
   if (p->head_dim != 64 && p->head_dim != 128) return D2O_ERR_UNSUPPORTED;
   if (p->n_q_heads / p->n_kv_heads > 16) return D2O_ERR_UNSUPPORTED;
   if (p->cache_fp8 != 0 && p->cache_fp8 != 1) return D2O_ERR_INVALID_ARG;
-  if (p->cache_fp8 && p->dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
+  if ((p->cache_fp4 != 0 && p->cache_fp4 != 1) || (p->cache_fp4 && p->cache_fp8)) return D2O_ERR_INVALID_ARG;
+  const bool coded = p->cache_fp8 || p->cache_fp4;
+  if (coded && p->dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
   if (p->page_size < 1 || p->page_size > 1024 || (p->page_size & (p->page_size - 1))) return D2O_ERR_INVALID_ARG;
   if (int64_t(p->max_pages) * p->page_size > 0x7FFF0000) return D2O_ERR_INVALID_ARG;
   if (int64_t(p->batch) * p->n_q_heads > 0x3FFFFFFF) return D2O_ERR_INVALID_ARG;
-  const int es = p->cache_fp8 ? 1 : p->dtype == D2O_BF16 ? 2 : 4;
+  const int es = coded ? 1 : p->dtype == D2O_BF16 ? 2 : 4;
   if (!dense_view_ok(p->K, es, true) || !dense_view_ok(p->V, es, true)) return D2O_ERR_INVALID_ARG;
-  if (p->cache_fp8 && (!p->K_exp || !p->V_exp)) return D2O_ERR_INVALID_ARG;
+  if (coded && (!p->K_exp || !p->V_exp)) return D2O_ERR_INVALID_ARG;
+  if (p->cache_fp4 && (reinterpret_cast<uintptr_t>(p->K_exp) | reinterpret_cast<uintptr_t>(p->V_exp)) & 3) return D2O_ERR_INVALID_ARG;
   if (!p->page_table || (reinterpret_cast<uintptr_t>(p->page_table) | reinterpret_cast<uintptr_t>(p->score) |
                          reinterpret_cast<uintptr_t>(p->pos)) & 3)
     return D2O_ERR_INVALID_ARG;
@@ -51,8 +54,8 @@ int check_pages(const d2o_pages* p, PagePool* out) {
   out->v_page = p->V.stride_b * es;
   out->v_head = p->V.stride_h * es;
   out->v_row = p->V.stride_n * es;
-  out->k_exp = p->cache_fp8 ? p->K_exp : nullptr;
-  out->v_exp = p->cache_fp8 ? p->V_exp : nullptr;
+  out->k_exp = coded ? p->K_exp : nullptr;
+  out->v_exp = coded ? p->V_exp : nullptr;
   out->score = p->score;
   out->pos = p->pos;
   out->table = p->page_table;
@@ -64,80 +67,6 @@ int check_pages(const d2o_pages* p, PagePool* out) {
 }
 
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 4;       // wavefronts of a workgroup
-constexpr int kTile = 16;       // entries of a tile: the rows of one matrix operand
-constexpr int kRowBcast = 0x150;  // lane i of each row of 16 lanes to all of the row (data-parallel primitive, + i)
-
-struct StepArgs {
-  PagePool pool;
-  View q, kn, vn, out;
-  const int32_t* lens;
-  const int32_t* positions;
-  float* logits;   // [B][Hq][pad] base-2 logits of the entries that are seen (scores kept)
-  float* part_o;   // [B * Hkv][splits][G][D] outputs of a share, not normalised
-  float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum (outputs and sums: times 2^-TileList::bias)
-  int32_t Hq, G, max_len, window, n_sink, pad, splits, joins;  // joins: workgroups of step_finish that join outputs
-};
-
-// The tiles of a sequence that hold what a step sees: those of the first tokens, then those from the window's start.  (Where the
-// pages keep positions, entries lie in any order and all tiles are looked at.)
-struct TileList {
-  int n, sink_tiles, rest0, tiles, share;  // entries, tiles of the first tokens, first tile behind them, tiles in all, tiles per workgroup
-  int64_t last;                            // the new token's position
-  int bias;                                // n < 2^bias
-  __device__ __forceinline__ TileList(const StepArgs& a, int b, int least) {
-    n = min(a.lens[b], a.max_len);
-    if (n <= 0) {
-      n = tiles = share = sink_tiles = rest0 = bias = 0;
-      last = 0;
-      return;
-    }
-    last = a.positions ? a.positions[b] : n - 1;
-    bias = 32 - __clz(n);
-    const int all = (n + kTile - 1) / kTile;
-    sink_tiles = rest0 = 0;
-    if (a.window != 0 && !a.pool.pos) {
-      const int64_t lo = last - a.window + 1;  // first entry of the window
-      sink_tiles = (min(a.n_sink, n) + kTile - 1) / kTile;
-      rest0 = int(min(max(lo / kTile, int64_t(sink_tiles)), int64_t(all)));
-      if (lo < 0) rest0 = sink_tiles;
-    }
-    tiles = sink_tiles + all - rest0;
-    if (tiles == 0) {  // nothing is seen: the last tile, whose entries are all masked
-      rest0 = all - 1;
-      tiles = 1;
-    }
-    share = ((tiles + a.splits - 1) / a.splits + least - 1) / least * least;  // whole rounds of the wavefronts
-  }
-  __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
-  __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }
-  // Whether the window shows entry s, whose position is `pos` where the pages keep positions.
-  __device__ __forceinline__ bool sees(const StepArgs& a, int s, int32_t pos) const {
-    const int p = a.pool.pos ? pos : s;
-    return a.window == 0 || p > last - a.window || p < a.n_sink;
-  }
-};
-
-template <int L>
-__device__ __forceinline__ float row_bcast(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kRowBcast + L, 0xF, 0xF, true));
-}
-// v + the same of the lanes 16 and 32 away: every lane gets the sum over the four rows of 16.
-__device__ __forceinline__ float sum_rows(float v) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-  v = __int_as_float(a[0]) + __int_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-  return __int_as_float(b[0]) + __int_as_float(b[1]);
-}
-
-__device__ __forceinline__ float max_rows(float v) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-  v = fmaxf(__int_as_float(a[0]), __int_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-  return fmaxf(__int_as_float(b[0]), __int_as_float(b[1]));
-}
 
 // What a lane holds of rows of type CT with D elements.  K: lane l has row l % 16 of a tile, chunks of 16 bytes that the four rows of
 // lanes take in turn; V: the 16 lanes of a row of lanes share a row of V, D / 16 elements each.
@@ -248,82 +177,6 @@ struct Rows<uint8_t, D> {
     }
   }
 };
-
-// out[h] of a (sequence, KV head) from joined partials.
-template <typename T>
-__device__ __forceinline__ void store_out(const StepArgs& a, int b, int hq, int col, float o) {
-  (static_cast<T*>(a.out.ptr) + b * a.out.sb + hq * a.out.sh)[col] = Elem<T>::from_f32(o);
-}
-
-// The new token's row into its page: two wavefronts, one for K and one for V.
-template <typename T, typename CT, int D>
-__device__ __forceinline__ void store_new(const StepArgs& a, int b, int hk, int page, int s, int64_t position) {
-  const int tid = threadIdx.x;
-  const int64_t at = a.pool.at(page, hk, s);
-  if (tid < 128) {
-    const int which = tid >> 6, lane = tid & 63;
-    const View& x = which ? a.vn : a.kn;
-    const T* src = static_cast<const T*>(x.ptr) + b * x.sb + hk * x.sh;
-    CT* dst = reinterpret_cast<CT*>(which ? a.pool.v_at(page, hk, s) : a.pool.k_at(page, hk, s));
-    if constexpr (sizeof(CT) == 1) {
-      float m = 0.f;
-      for (int i = lane; i < D; i += 64) m = fmaxf(m, fp8_magnitude(Elem<T>::to_f32(src[i])));
-      const int e = fp8_row_exponent(wave_max(m));
-      for (int i = lane; i < D; i += 64) dst[i] = fp8_code(Elem<T>::to_f32(src[i]), e);
-      if (lane == 0) (which ? a.pool.v_exp : a.pool.k_exp)[at] = int8_t(e);
-    } else {
-      for (int i = lane; i < D; i += 64) dst[i] = src[i];
-    }
-  }
-  if (tid == 0) {
-    if (a.pool.score) a.pool.score[at] = 0.f;
-    if (a.pool.pos) a.pool.pos[at] = int32_t(position);
-  }
-}
-
-// Adds the softmax rows of a (sequence, KV head) to the scores of entries i0, i0 + step, .. (in the order of the tiles) below `end`, N of them
-// (Eq. 6); the group's query heads in rising order.  What is read - logits, pages, old scores - is on its way before `totals` forms M and
-// inv, maximum and reciprocal sum (of exp2(x - M)) of each head.
-template <int N, int GM, typename F>
-__device__ __forceinline__ void add_scores(const StepArgs& a, const TileList& list, int b, int hk, int i0, int step, int end,
-                                           const float* M, const float* inv, const F& totals) {
-  const float* lg = a.logits + (int64_t(b) * a.Hq + hk * a.G) * a.pad;
-  int s[N], page[N];
-  float x[GM][N], old[N];
-  int64_t at[N];
-  int32_t pos[N] = {};
-  const bool by_pos = a.window != 0 && a.pool.pos;
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const int i = i0 + u * step;
-    s[u] = i < end ? list.slot(i / kTile) + i % kTile : list.n;
-    page[u] = s[u] < list.n ? a.pool.page_of(b, s[u]) : -1;
-  }
-#pragma unroll
-  for (int h = 0; h < GM; ++h)
-    if (h < a.G) {
-#pragma unroll
-      for (int u = 0; u < N; ++u) x[h][u] = lg[int64_t(h) * a.pad + min(s[u], list.n - 1)];
-    }
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    at[u] = page[u] >= 0 ? a.pool.at(page[u], hk, s[u]) : 0;
-    old[u] = a.pool.score[at[u]];
-    if (by_pos) pos[u] = a.pool.pos[at[u]];
-  }
-  totals();
-  float add[N] = {};
-#pragma unroll
-  for (int h = 0; h < GM; ++h)
-    if (h < a.G) {
-#pragma unroll
-      for (int u = 0; u < N; ++u) add[u] += __builtin_amdgcn_exp2f(x[h][u] - M[h]) * inv[h];
-    }
-  // (only what is seen: the logit of -infinity of an entry that is not would become NaN beside a NaN or an infinity of its head)
-#pragma unroll
-  for (int u = 0; u < N; ++u)
-    if (page[u] >= 0 && list.sees(a, s[u], pos[u]) && add[u] != 0.f) a.pool.score[at[u]] = old[u] + add[u];
-}
 
 // One workgroup per (sequence, KV head, share of its tiles).  U tiles of 16 entries per wavefront and round: the logits of all
 // query heads of the group come from the matrix core (heads are its columns, padded to 16), straight from rows in registers: lane l
@@ -595,64 +448,6 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   }
 }
 
-// Joins the shares of the heads that have several: the first `joins` workgroups the outputs, one query head each, the others the scores.
-constexpr int kFinish = 256, kFinishEntries = 1024;  // threads; entries of a workgroup that adds scores
-template <typename T, int D, int GM>
-__global__ __launch_bounds__(kFinish) void step_finish(StepArgs a, int least) {
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  // maximum and sum of a query head over the shares: a wavefront, a lane per share
-  auto total = [&](const float* ml, int ns, float& M, float& L) __attribute__((always_inline)) {
-    M = -3.402823466e38f;
-    for (int i = lane; i < ns; i += 64) M = fmaxf(M, ml[int64_t(i) * a.G * 2]);
-    M = wave_max(M);
-    L = 0.f;
-    for (int i = lane; i < ns; i += 64) L = fmaf(ml[int64_t(i) * a.G * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M), L);
-    L = wave_sum(L);
-  };
-  if (int(blockIdx.x) < a.joins) {
-    constexpr int kCols = D / 4, kParts = kFinish / kCols;  // four columns per thread, the shares among kParts groups of threads
-    __shared__ f32x4 so[kParts][kCols];
-    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, bh = b * a.pool.Hkv + hq / a.G, h = hq % a.G;
-    const TileList list(a, b, least);
-    const int ns = list.shares();
-    if (ns <= 1) return;
-    const float* ml = a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2;
-    float M, L;
-    total(ml, ns, M, L);
-    const int col = tid % kCols, part = tid / kCols;
-    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (int64_t(bh) * a.splits * a.G + h) * D) + col;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int i = part; i < ns; i += kParts) o += po[int64_t(i) * a.G * kCols] * __builtin_amdgcn_exp2f(ml[int64_t(i) * a.G * 2] - M);
-    so[part][col] = o;
-    __syncthreads();
-    if (tid < D) {
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < kParts; ++i) sum += so[i][tid / 4][tid % 4];
-      store_out<T>(a, b, hq, tid, L == 0.f ? 0.f : sum / L);
-    }
-    return;
-  }
-  __shared__ float sM[16], sinv[16];
-  const int per = (a.pad + kFinishEntries - 1) / kFinishEntries, x = blockIdx.x - a.joins, bh = x / per, b = bh / a.pool.Hkv, hk = bh % a.pool.Hkv;
-  const TileList list(a, b, least);
-  const int first = x % per * kFinishEntries, ns = list.shares();
-  if (first >= list.tiles * kTile || ns <= 1) return;
-  const int end = min(first + kFinishEntries, list.tiles * kTile);
-  add_scores<kFinishEntries / kFinish, GM>(a, list, b, hk, first + tid, kFinish, end, sM, sinv, [&]() __attribute__((always_inline)) {
-    for (int h = w; h < a.G; h += kFinish / 64) {
-      float M, L;
-      total(a.part_ml + (int64_t(bh) * a.splits * a.G + h) * 2, ns, M, L);
-      if (lane == 0) {
-        sM[h] = M;
-        sinv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
-      }
-    }
-    __syncthreads();
-  });
-}
-
 // Tiles per wavefront and round: two, where their rows take 16 KB at most.
 // (8-bit rows in fours: 39 instead of 36 us for 4 x 32 heads x 4100 entries; bf16 rows of 128 singly: 109 instead of 105 us for 8 heads of 131072.)
 template <typename CT, int D, int GM>
@@ -688,19 +483,6 @@ template <typename T, typename CT>
 void launch_step(StepArgs& a, int batch, int D, hipStream_t s) {
   if (D == 64) launch_step<T, CT, 64>(a, batch, s);
   else launch_step<T, CT, 128>(a, batch, s);
-}
-
-// Shares per head, for at most `tiles` tiles each: workgroups of 64 tiles, about four per CU (a workgroup's ends cost as much as a dozen
-// tiles: 128 heads of 258 tiles of 8-bit rows 36 us in eight shares, 30 in four), but for two per CU shares as small as two rounds of a workgroup.
-int step_splits(int64_t bh, int64_t tiles) {
-  const int64_t large = std::min<int64_t>(1024 / bh, tiles / 64), small = std::min<int64_t>(512 / bh, tiles / (2 * kWaves));
-  return int(std::max<int64_t>(1, std::max(large, small)));
-}
-// Tiles that a sequence of max_len entries shows at most.
-int64_t most_tiles(const d2o_pages* p, int32_t max_len, int32_t window, int32_t n_sink) {
-  const int64_t all = (int64_t(max_len) + kTile - 1) / kTile;
-  if (window == 0 || p->pos) return all;
-  return std::min(all, (int64_t(window) + n_sink) / kTile + 3);
 }
 
 }  // namespace
@@ -763,7 +545,9 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   a.window = window;
   a.n_sink = n_sink;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (pages->cache_fp8)
+  if (pages->cache_fp4)
+    launch_step4(a, pages->batch, pages->head_dim, s);
+  else if (pages->cache_fp8)
     launch_step<uint16_t, uint8_t>(a, pages->batch, pages->head_dim, s);
   else if (pages->dtype == D2O_BF16)
     launch_step<uint16_t, uint16_t>(a, pages->batch, pages->head_dim, s);

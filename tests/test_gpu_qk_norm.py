@@ -1,0 +1,133 @@
+"""Norms of queries and keys with the rotation by position (d2o_qk_norm_rope) against the formula in 64 bits."""
+import pytest
+import torch
+
+from paper_2406_13035_amd import binding
+
+from . import serving_ref as ref
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def inputs(dtype, B, Hq, Hkv, n, d, seed=0, scale=1.0, packed=False):
+    g = torch.Generator().manual_seed(seed)
+    xs = []
+    for h in (Hq, Hkv):
+        if packed:
+            xs.append((torch.randn((B, n, h, d), generator=g) * scale).to(dtype).transpose(1, 2))
+        else:
+            xs.append((torch.randn((B, h, n, d), generator=g) * scale).to(dtype))
+    ws = [(1.0 + 0.3 * torch.randn(d, generator=g)).to(dtype) for _ in range(2)]
+    return xs, ws
+
+
+def on_gpu(x):
+    y = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda:0")
+    return y.copy_(x)
+
+
+def check(got, x, w, eps, rot, positions, base):
+    want, tol = ref.norm_ref(x, w, eps, rot, positions, base)
+    err = (got.cpu().double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def run(dtype, B, Hq, Hkv, n, d, rot=None, far=1000, base=10000.0, eps=1e-6, seed=0, scale=1.0, packed=False, weights=True, in_place=False,
+        positions=True, pos0=0):
+    rot = d if rot is None else rot
+    (Q, K), (wq, wk) = inputs(dtype, B, Hq, Hkv, n, d, seed, scale, packed)
+    wq, wk = (wq, wk) if weights else (None, None)
+    at = None
+    if positions:
+        g = torch.Generator().manual_seed(seed + 5)
+        at = torch.randint(-far, far + 1, (B, n), generator=g, dtype=torch.int64).to(torch.int32)
+    Qg, Kg = on_gpu(Q), on_gpu(K)
+    outs = (Qg, Kg) if in_place else (None, None)
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    q, k = binding.d2o_qk_norm_rope(Qg, Kg, cu(wq), cu(wk), eps, cu(at), pos0, base, rot, *outs)
+    torch.cuda.synchronize()
+    at = at if at is not None else (pos0 + torch.arange(n)).expand(B, n)
+    check(q, Q, wq, eps, rot, at, base)
+    check(k, K, wk, eps, rot, at, base)
+    if in_place:
+        assert q is Qg and k is Kg
+    else:
+        assert torch.equal(Qg.cpu(), Q) and torch.equal(Kg.cpu(), K)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Hq,Hkv,n", [(1, 1, 1, 1), (1, 4, 2, 7), (3, 5, 1, 33), (2, 8, 8, 100), (64, 32, 8, 1), (1, 3, 3, 1025)], ids=str)
+def test_sizes(dtype, d, B, Hq, Hkv, n):
+    run(dtype, B, Hq, Hkv, n, d, seed=n + Hq)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d,rot", [(64, 0), (64, 16), (64, 48), (128, 32), (128, 112), (128, 64)])
+def test_part_of_a_row_is_turned(dtype, d, rot):
+    run(dtype, 2, 3, 2, 21, d, rot, seed=rot)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("far,base", [(1 << 20, 10000.0), ((1 << 31) - 2, 500000.0), ((1 << 24) + 1, 1.5)])
+def test_far_positions(dtype, far, base):
+    run(dtype, 2, 3, 2, 40, 128, far=far, base=base)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_forms(dtype):
+    run(dtype, 2, 4, 2, 19, 128, packed=True)
+    run(dtype, 2, 4, 2, 19, 64, in_place=True)
+    run(dtype, 1, 4, 2, 37, 128, packed=True, in_place=True, weights=False)
+    run(dtype, 2, 4, 2, 19, 128, positions=False, pos0=77)
+    run(dtype, 2, 4, 2, 19, 128, positions=False, pos0=-(1 << 31))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_queries_or_keys_alone(dtype):
+    (Q, K), (wq, wk) = inputs(dtype, 2, 5, 3, 9, 64)
+    at = torch.arange(9).expand(2, 9)
+    q, none = binding.d2o_qk_norm_rope(Q.cuda(), None, wq.cuda())
+    assert none is None
+    check(q, Q, wq, 1e-6, 64, at, 10000.0)
+    none, k = binding.d2o_qk_norm_rope(None, K.cuda(), None, wk.cuda())
+    assert none is None
+    check(k, K, wk, 1e-6, 64, at, 10000.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_magnitudes(dtype):
+    """Rows whose squares leave 32 bits on either side, beside ordinary ones; rows of zeros are zero."""
+    for scale in (1e-38, 1e-20, 1e-4, 1e15, 1e19, 1e30, 5e37):
+        run(dtype, 1, 2, 1, 12, 128, scale=scale)
+    (Q, K), (wq, wk) = inputs(dtype, 1, 4, 2, 16, 64)
+    Q[0, 1] *= 2.0 ** 120
+    Q[0, 2, 3] = 0.0
+    Q[0, 3] *= 2.0 ** -100
+    q, _ = binding.d2o_qk_norm_rope(Q.cuda(), K.cuda(), wq.cuda(), wk.cuda())
+    check(q, Q, wq, 1e-6, 64, torch.arange(16).expand(1, 16), 10000.0)
+    assert bool((q[0, 2, 3] == 0).all())
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    (Q, K), (wq, wk) = inputs(BF16, 1, 4, 2, 40, 128)
+    Q[0, 1, 5, 7], Q[0, 2, 6, 100] = float("inf"), float("nan")
+    q, k = binding.d2o_qk_norm_rope(Q.cuda(), K.cuda(), wq.cuda(), wk.cuda())
+    bad = torch.zeros(Q.shape, dtype=torch.bool)
+    bad[0, 1, 5], bad[0, 2, 6] = True, True
+    at = torch.arange(40).expand(1, 40)
+    want, tol = ref.norm_ref(Q, wq, 1e-6, 128, at, 10000.0)
+    err = (q.cpu().double() - want).abs()
+    assert bool((err <= tol)[~bad].all()) and bool(q.cpu()[0, 2, 6].isnan().all()) and bool(q.cpu()[0, 1, 5, 7].isnan())
+    check(k, K, wk, 1e-6, 128, at, 10000.0)
+
+
+def test_rows_with_gaps_and_what_lies_between_them():
+    g = torch.Generator().manual_seed(3)
+    wide = torch.randn((2, 3, 11, 96), generator=g).to(BF16)
+    Q = wide[..., 8:72]
+    out = torch.full((2, 3, 11, 96), 5.0, dtype=BF16, device="cuda:0")
+    binding.d2o_qk_norm_rope(wide.cuda()[..., 8:72], None, Q_out=out[..., 16:80])
+    check(out[..., 16:80], Q, None, 1e-6, 64, torch.arange(11).expand(2, 11), 10000.0)
+    assert bool((out[..., :16] == 5).all()) and bool((out[..., 80:] == 5).all())
