@@ -459,7 +459,7 @@ int d2o_pages_put(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_toke
 int d2o_pages_get(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_tokens, const int64_t* slots, void* stream);
 
 /* Attention of several new tokens per sequence over pages of 4-bit rows (cache_fp4), which hold them already.  q, out: [n_tokens][Hq][d] packed (stride_n
- * between tokens, stride_h between heads, stride_b unused); rows first[b] .. first[b + 1] - 1 (device [B + 1], taken within [0, n_tokens]) are the last tokens of
+ * between tokens, stride_h between heads, stride_b unused); rows first[b] .. first[b + 1] - 1 (device [B + 1], nowhere falling, taken within [0, n_tokens]) are the last tokens of
  * sequence b, the newest of them its entry lens[b] - 1.  Each sees the entries up to its own that have a position > its own - window or < n_sink (window = 0: all);
  * positions: device [n_tokens], NULL: the entry's number.  lens and max_len as for d2o_pages_step (a sequence that claims more is cut to it); tokens without an entry, or
  * that see none, get zeros.  Rows of out that belong to no sequence are left as they were.  Scores are neither read nor added to.  A weight

@@ -6,28 +6,28 @@ namespace d2o {
 namespace {
 
 // Query tokens of a batch's sequences stand one behind the other (attend); a sequence's (token, query head of a KV head's group) pairs, in
-// this order, are the columns of its products, sixteen to a workgroup.
+// this order, are the columns of its products, up to kGroup to a workgroup.
 struct AttendArgs : StepArgs {
   const int32_t* first;  // [B + 1] first query token of every sequence
   int32_t n_tokens, batch, groups;  // rows of q; groups of columns, at most
   __device__ __forceinline__ int token0(int b) const { return min(max(first[b], 0), n_tokens); }
   __device__ __forceinline__ int tokens(int b) const { return max(token0(b + 1) - token0(b), 0); }
 };
-constexpr int kCols = 16;
-constexpr int kUnits4 = 1;                        // pairs of tiles of a wavefront's round
-constexpr int kLeast4 = kWaves * 2 * kUnits4;  // tiles of a workgroup's round
+constexpr int kCols = 16;         // columns of a matrix product
+constexpr int kGroup = 32;        // columns of a workgroup at most
+constexpr int kLeast4 = kWaves * 2;  // tiles of a workgroup's round: a pair for each wavefront
 
 // Which columns a workgroup has.  Step: the group's query heads of sequence b.
 struct Columns {
   int b, base, count;  // sequence, first pair, pairs of the sequence from there on (0: none)
 };
-// The index-th group of kCols columns of the batch; all threads of the workgroup.
+// The index-th group of kGroup columns of the batch; all threads of the workgroup.
 __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) {
   __shared__ int sum[kWaves], found[3];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int per = (a.batch + 64 * kWaves - 1) / (64 * kWaves), b0 = tid * per, b1 = min(b0 + per, a.batch);
   int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (a.tokens(b) * a.G + kCols - 1) / kCols;
+  for (int b = b0; b < b1; ++b) mine += (a.tokens(b) * a.G + kGroup - 1) / kGroup;
   int inc = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -41,11 +41,11 @@ __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) 
   int at = inc - mine;
   if (index >= at && index < inc)
     for (int b = b0; b < b1; ++b) {
-      const int pairs = a.tokens(b) * a.G, n = (pairs + kCols - 1) / kCols;
+      const int pairs = a.tokens(b) * a.G, n = (pairs + kGroup - 1) / kGroup;
       if (index < at + n) {
         found[0] = b;
-        found[1] = (index - at) * kCols;
-        found[2] = pairs - found[1];
+        found[1] = (index - at) * kGroup;
+        found[2] = min(pairs - found[1], kGroup);
         break;
       }
       at += n;
@@ -67,18 +67,23 @@ __device__ __forceinline__ int row_min(int v) {
   for (int o = 1; o < 16; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
   return v;
 }
-// Column c's sight, and the tiles that any of the columns sees.  Returns false where there are none.
-__device__ __forceinline__ bool sight_of(const AttendArgs& a, const Columns& col, int c, int least, Sight& mine, TileList& list) {
-  const int m = a.tokens(col.b), len = min(a.lens[col.b], a.max_len);
-  const int token = (col.base + c) / a.G, last_token = (col.base + min(col.count, kCols) - 1) / a.G;
-  const bool is = c < col.count;
-  mine.last = is ? max(len - m + token, -1) : -1;
-  mine.lo = window_start(a.positions && is ? a.positions[a.token0(col.b) + token] : mine.last, a.window);
-  list.n = max(len - m + last_token + 1, 0);
+// The sights of columns c, c + 16, .. (N of them), and the tiles that any of the columns sees; false where there are none.
+template <int N>
+__device__ __forceinline__ bool sights_of(const AttendArgs& a, const Columns& col, int c, Sight (&mine)[N], TileList& list) {
+  const int m = a.tokens(col.b), len = min(a.lens[col.b], a.max_len), token0 = a.token0(col.b);
+  int lo = INT32_MAX;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = i * kCols + c, token = (col.base + at) / a.G;
+    const bool is = at < col.count;
+    mine[i].last = is ? max(len - m + token, -1) : -1;
+    mine[i].lo = window_start(a.positions && is ? a.positions[token0 + token] : mine[i].last, a.window);
+    lo = min(lo, is ? mine[i].lo : INT32_MAX);
+  }
+  list.n = max(len - m + (col.base + col.count - 1) / a.G + 1, 0);
   list.last = 0;
   if (list.n == 0) return false;
-  const int lo = a.window == 0 ? 0 : __builtin_amdgcn_readfirstlane(row_min(is ? mine.lo : INT32_MAX));
-  list.choose(a, lo, least);
+  list.choose(a, a.window == 0 ? 0 : __builtin_amdgcn_readfirstlane(row_min(lo)), kLeast4);
   return true;
 }
 
@@ -92,358 +97,610 @@ struct Row4 {
   static __device__ __forceinline__ uint32_t word(const KReg& k, int i) { return k[i]; }
 };
 
-// One workgroup per (sequence, KV head, 16 columns, share of the tiles they see).  As in the step over wider rows the logits S^T = K Q^T come from
-// the matrix core, entries by columns, and leave in each lane of row of lanes g one column and the entries 4 g .. 4 g + 3 of a tile.  Of two tiles these
-// are eight entries, which is what the lane has to hold of P as the left operand of P V (16 x 16 x 32): P goes from registers to the matrix core with no
-// exchange.  The right operand wants eight entries of one element of V: a lane converts the D / 16 elements it has of each of the eight rows to
-// bf16 (exact), two elements of one row at a time, and swaps halves between rows (a conversion and a permutation for two values).
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+// Where a pair of tiles lies, the same for all lanes.
+struct Pair {
+  int s0[2];      // first entries
+  int page[2];    // (pages of whole tiles)
+  bool there[2];  // within the share, and on a page
+};
+// How rows are found.  ROWS: each by its own page number.  TILES, PAIRS: a tile, or a pair of them, lies in one page, whose number and address are the same for
+// all lanes and live in scalar registers; a lane adds a displacement of 32 bits that never changes (see the step over wider rows).
+enum Finds { ROWS, TILES, PAIRS };
+
+// One share of the tiles that a workgroup's columns see, by its four wavefronts in turn, pairs of tiles at a time; N groups of 16 columns.  As in the
+// step over wider rows the logits S^T = K Q^T come from the matrix core, entries by columns, and leave in each lane of row of lanes g one column and the
+// entries 4 g .. 4 g + 3 of a tile.  Of two tiles these are eight entries, which is what the lane has to hold of P as the left operand of P V (16 x 16 x 32): P goes from registers to
+// the matrix core with no exchange.  The right operand wants eight entries of one element of V: a lane converts the D / 16 elements it has of each of the eight rows
+// to bf16 (exact), two elements of one row at a time, and swaps halves between rows: a conversion and a permutation for two values, once for all N groups.
 // P as two bf16 terms, which hold 16 bits: a weight is off by 2^-16 of itself at most.  Codes are always finite and powers of two may stand for NaN: where
 // columns see different entries, NaN is left out of the product, in which 0 * NaN would reach columns that do not see it, and added to those that do.
-// WIDE: a tile lies in one page (see the step over wider rows).
-template <int D, bool WIDE, bool STEP>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void attend_part4(AttendArgs a) {
+template <int D, Finds F, bool STEP, int N>
+struct Share {
   typedef Row4<D> R;
-  constexpr int E = R::kE, kExps = D / kBlock4, U = kUnits4;
-  __shared__ float so[kWaves][kCols][D];
-  __shared__ float sml[kWaves][kCols][2];
-  __shared__ float sM[kCols], sinv[kCols];
-  const int Hkv = a.pool.Hkv;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
-  Columns col;
-  Sight mine;
-  TileList list;
-  int hk, share, part;  // part: which partial result, in units of shares
-  if constexpr (STEP) {
-    share = blockIdx.x;
-    col.b = blockIdx.y / Hkv;
-    hk = blockIdx.y % Hkv;
-    col.base = 0;
-    col.count = a.G;
-    part = blockIdx.y * a.splits + share;
-    list = TileList(a, col.b, kLeast4);
-    if (list.n == 0) {
-      if (share == 0)
-        for (int i = tid; i < a.G * D; i += 64 * kWaves) store_out<uint16_t>(a, col.b, hk * a.G + i / D, i % D, 0.f);
-      return;
+  static constexpr int E = R::kE, kExps = D / kBlock4, kSteps = R::kSteps;
+  // Several groups: the next pair's rows are on their way and its keys converted beside the products of the present one (two wavefronts per SIMD).  One: few
+  // registers, so that four wavefronts per SIMD hide the loads.
+  static constexpr bool kAhead = !STEP;
+  const AttendArgs& a;
+  const Columns& col;
+  const TileList& list;
+  const int hk, t0, t1;
+  const Sight (&mine)[N];
+  const int w, lane, c, g;
+  const int all_last, all_lo;
+  // rows on their way
+  typename R::KReg k[2], vx[2];
+  typename R::VReg v[2][4];
+  int ke[2];
+  uint32_t absent[2];  // (ROWS) bit i: entry i of the tile has no page
+  // results: maximum (of the base-2 logits), sum and outputs, register i of om: column 4 g + i, element c * E + index
+  float m[N], l[N];
+  f32x4 om[N][E];
+
+  __device__ __forceinline__ Pair pair_at(int t) const {
+    const auto table = (const __attribute__((address_space(4))) int32_t*)(a.pool.table + int64_t(col.b) * a.pool.max_pages);
+    t = min(t, t0 + ((t1 - 1 - t0) & ~1));  // (behind the share: its last pair again)
+    Pair p;
+    p.s0[0] = list.slot(t);
+    p.there[0] = true;
+    p.there[1] = t + 1 < t1;
+    p.s0[1] = F == PAIRS ? p.s0[0] + kTile : list.slot(min(t + 1, t1 - 1));
+#pragma unroll
+    for (int i = 0; i < (F == ROWS ? 0 : F == TILES ? 2 : 1); ++i) {
+      const int page = table[p.s0[i] >> a.pool.shift];
+      const bool is = uint32_t(page) < uint32_t(a.pool.n_pages);
+      p.page[i] = is ? page : 0;  // (no page: the pool's first, whose values are not used; rows behind the end lie in the page)
+      p.there[i] = p.there[i] && is;
+      if (F == PAIRS) {
+        p.page[1] = p.page[0];
+        p.there[1] = p.there[1] && is;
+      }
     }
-    mine.last = c < a.G ? list.n - 1 : -1;
-    mine.lo = window_start(list.last, a.window);
-  } else {
-    const int index = blockIdx.x / a.splits / Hkv;
-    share = blockIdx.x % a.splits;
-    hk = blockIdx.x / a.splits % Hkv;
-    part = blockIdx.x;
-    col = find_columns(a, index);
-    if (col.count <= 0) return;
-    if (!sight_of(a, col, c, kLeast4, mine, list)) {
-      if (share == 0)
-        for (int i = tid; i < min(col.count, kCols) * D; i += 64 * kWaves) {
-          const int r = col.base + i / D;
-          (static_cast<uint16_t*>(a.out.ptr) + int64_t(a.token0(col.b) + r / a.G) * a.out.sn + int64_t(hk * a.G + r % a.G) * a.out.sh)[i % D] = 0;
-        }
-      return;
+    return p;
+  }
+  // Byte `row * stride` of page `page` behind base (strides: launch_*4 sees to it that pages' have 32 bits and rows' 21).
+  static __device__ __forceinline__ const uint8_t* at_row(const uint8_t* base, int page, int64_t page_stride, int row, int64_t row_stride) {
+    return base + (uint64_t(uint32_t(page)) * uint32_t(page_stride) + uint32_t(row) * uint32_t(row_stride));
+  }
+  __device__ __forceinline__ const int8_t* exps_at(const int8_t* base, int page, int row) const {
+    return base + ((int64_t(page) * a.pool.Hkv + hk) << a.pool.shift) * kExps + row * kExps;
+  }
+  __device__ __forceinline__ void load_k(const Pair& p) {
+    const int rmask = (1 << a.pool.shift) - 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (F != ROWS) {
+        const int row = p.s0[i] & rmask;
+        const uint8_t* kp = at_row(a.pool.K + hk * a.pool.k_head, p.page[i], a.pool.k_page, row, a.pool.k_row);
+        k[i] = *reinterpret_cast<const typename R::KReg*>(kp + (uint32_t(c) * uint32_t(a.pool.k_row) + g * (D / 8)));
+        ke[i] = exps_at(a.pool.k_exp, p.page[i], row)[uint32_t(c * kExps + g * kExps / 4)];
+      } else {
+        // (rows that are not there: the first row of the pool, whose values are not used)
+        const int s = p.s0[i] + c, pk = s < list.n ? a.pool.page_of(col.b, s) : -1;
+        k[i] = *reinterpret_cast<const typename R::KReg*>((pk >= 0 ? a.pool.k_at(pk, hk, s) : a.pool.K) + g * (D / 8));
+        ke[i] = a.pool.k_exp[(pk >= 0 ? a.pool.at(pk, hk, s) : 0) * kExps + g * kExps / 4];
+      }
     }
   }
-  const int b = col.b, cols = min(col.count, kCols);
+  __device__ __forceinline__ void load_v(const Pair& p) {
+    const int rmask = (1 << a.pool.shift) - 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      absent[i] = 0;
+      if constexpr (F != ROWS) {
+        const int row = p.s0[i] & rmask;
+        const uint8_t* vp = at_row(a.pool.V + hk * a.pool.v_head, p.page[i], a.pool.v_page, row, a.pool.v_row);
+        const uint32_t voff = uint32_t(4 * g) * uint32_t(a.pool.v_row) + c * (E / 2);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const auto* at_v = reinterpret_cast<const typename R::VReg*>(vp + uint32_t(r) * uint32_t(a.pool.v_row) + voff);
+          v[i][r] = STEP ? __builtin_nontemporal_load(at_v) : *at_v;
+        }
+        vx[i] = *reinterpret_cast<const typename R::KReg*>(exps_at(a.pool.v_exp, p.page[i], row) + uint32_t(4 * g * kExps));
+      } else {
+        const int s = p.s0[i] + c, pk = s < list.n ? a.pool.page_of(col.b, s) : -1;
+        absent[i] = ~uint32_t(__ballot(pk >= 0)) & 0xFFFFu;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int sv = p.s0[i] + 4 * g + r, pv = __shfl(pk, 4 * g + r, 64);
+          v[i][r] = *reinterpret_cast<const typename R::VReg*>((pv >= 0 ? a.pool.v_at(pv, hk, sv) : a.pool.V) + c * (E / 2));
+          const int8_t* ex = a.pool.v_exp + (pv >= 0 ? a.pool.at(pv, hk, sv) : 0) * kExps;
+          if constexpr (D == 128)
+            vx[i][r] = *reinterpret_cast<const uint32_t*>(ex);
+          else
+            vx[i][r / 2] = (r % 2 ? vx[i][r / 2] : 0u) | uint32_t(*reinterpret_cast<const uint16_t*>(ex)) << (16 * (r % 2));
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void convert_k(int i, bf16x8 (&to)[kSteps]) const {
+    const float scale = fp4_scale(ke[i]);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) to[j] = __builtin_bit_cast(bf16x8, fp4_decode8(k[i][j], scale));
+  }
+  // elements 2 y and 2 y + 1 of the lane's
+  __device__ __forceinline__ void convert_v(int y, bf16x8 (&to)[2], const int (&ve)[2][4]) const {
+      u32x4 even, odd;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        auto two = [&](int r) {
+          const float scale = fp4_scale(ve[i / 2][r]);
+          const uint32_t codes = v[i / 2][r];
+          // (which byte has to be a constant)
+          const bf16x2 x = y == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)
+                           : y == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)
+                           : y == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+          return __builtin_bit_cast(uint32_t, x);
+        };
+        const uint32_t x0 = two(i % 2 * 2), x1 = two(i % 2 * 2 + 1);
+        even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100);
+        odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302);
+      }
+      to[0] = __builtin_bit_cast(bf16x8, even);
+      to[1] = __builtin_bit_cast(bf16x8, odd);
+  }
+
+  // Probabilities are formed as 2^-bias * p, so that no mean of values of any size overflows.  The step, whose logits and sums make scores, forms
+  // (s - maximum) - bias; otherwise the products start from -bias in their own units and one multiply-add is left, and the sums of P, as it enters
+  // the products, come from the matrix core too (P times ones).
+  __device__ __forceinline__ void run(const bf16x8 (&q)[N][kSteps], float* lg) {
+    const float scale2 = kLog2e / sqrtf(float(D));
+    const float bias = list.bias, start = STEP ? 0.f : -bias / scale2;
+    const bool by_pos = a.window != 0 && a.pool.pos;
+    const int n = list.n;
+    f32x4 lm[N];   // (not STEP) sums of P: register i: column 4 g + i
+    float ref[N];  // what P is relative to, as an exponent
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      ref[x] = m[x] = -3.402823466e38f;
+      l[x] = 0.f;
+      lm[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < E; ++e) om[x][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int t = t0 + w * 2;
+    bf16x8 kop[2][kSteps];
+    Pair now = pair_at(t), next = now;
+    if (kAhead && t < t1) {
+      load_k(now);
+      load_v(now);
+      next = pair_at(t + kLeast4);
+      convert_k(0, kop[0]);
+      convert_k(1, kop[1]);
+      load_k(next);
+    }
+    while (t < t1) {
+      if constexpr (!kAhead) {
+        now = pair_at(t);
+        load_k(now);
+        load_v(now);
+      }
+      bool whole[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        whole[i] = now.there[i] && absent[i] == 0 && now.s0[i] + kTile - 1 <= all_last && !by_pos &&
+                   (now.s0[i] >= all_lo || now.s0[i] + kTile <= a.n_sink);
+      int ve[2][4];
+      uint32_t bad = 0, is = 0xFFu;  // bits 4 i + r: a power of two that stands for NaN; an entry of the sequence, on a page
+      const bool all = whole[0] && whole[1];
+      auto powers = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if constexpr (D == 128)
+              ve[i][r] = __builtin_amdgcn_sbfe(int(vx[i][r]), 8 * (c >> 2), 8);
+            else
+              ve[i][r] = __builtin_amdgcn_sbfe(int(vx[i][r / 2]), 16 * (r % 2) + 8 * (c >> 3), 8);
+          }
+        if (!all) {
+          is = 0;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              // (no branches: where a lane's vector was changed behind some, one compiler kept the old element)
+              const bool in = now.there[i] & (now.s0[i] + 4 * g + r < n) & !(absent[i] >> (4 * g + r) & 1), nan = in & (ve[i][r] == kNan4) & !whole[i];
+              bad |= uint32_t(nan) << (4 * i + r);
+              is |= uint32_t(in) << (4 * i + r);
+              ve[i][r] = whole[i] ? ve[i][r] : in & !nan ? min(ve[i][r], 125) : 0;
+            }
+        }
+      };
+      if constexpr (kAhead) powers();  // (else behind the products, which wait for the keys alone)
+      const Pair after = kAhead ? pair_at(t + 2 * kLeast4) : now;
+      f32x4 s[N][2];
+#pragma unroll
+      for (int x = 0; x < N; ++x) s[x][0] = s[x][1] = f32x4{start, start, start, start};
+      bf16x8 vop[E / 2][2];
+      if constexpr (kAhead) {
+#pragma unroll
+        for (int y = 0; y < E / 2; ++y) convert_v(y, vop[y], ve);
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < N; ++x) s[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[i][j], q[x][j], s[x][i], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          convert_k(i, kop[i]);
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int x = 0; x < N; ++x) s[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[i][j], q[x][j], s[x][i], 0, 0, 0);
+        }
+      }
+      if constexpr (kAhead) {
+        // one product, then as much of the conversion as runs beside it
+#pragma unroll
+        for (int i = 0; i < 2 * kSteps * N; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, (9 * E + 8) / (2 * kSteps * N), 0);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) asm volatile("" : "+v"(vop[e / 2][e % 2]));  // (converted here, not later)
+        load_v(next);  // (behind the last pair that one again: a branch would have the registers copied, and so waited for)
+      }
+      if constexpr (!kAhead) powers();
+      if constexpr (STEP) s[0][0] *= scale2, s[0][1] *= scale2;
+      uint32_t seen[N];  // bit 4 i + r: column x of the lane's sees entry 4 g + r of tile i
+#pragma unroll
+      for (int x = 0; x < N; ++x) seen[x] = 0xFFu;
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = now.s0[i] + 4 * g + r;
+            int at = e;
+            if (by_pos) {
+              const int p = e < n ? a.pool.page_of(col.b, e) : -1;
+              at = p >= 0 ? a.pool.pos[a.pool.at(p, hk, e)] : 0;
+            }
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+              const bool ok = bool(is >> (4 * i + r) & 1) & (e <= mine[x].last) & ((at >= mine[x].lo) | (at < a.n_sink));
+              const float logit = s[x][i][r];
+              s[x][i][r] = ok ? logit : -INFINITY;
+              seen[x] &= ~(uint32_t(!ok) << (4 * i + r));
+            }
+          }
+      }
+      if constexpr (STEP) {
+        if (lg && c < col.count) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (t + i < t1) *reinterpret_cast<f32x4*>(lg + now.s0[i] + 4 * g) = s[0][i];
+        }
+      }
+      float mx[N];
+      bool grown = false;
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        mx[x] = m[x];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx[x] = fmaxf(mx[x], s[x][i / 4][i % 4]);
+        grown |= mx[x] > m[x];
+      }
+      if (__any(grown)) {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          mx[x] = max_rows(mx[x]);
+          m[x] = mx[x];
+          const float to = STEP ? m[x] : fmaf(m[x], scale2, bias), f = __builtin_amdgcn_exp2f(ref[x] - to);
+          ref[x] = to;
+          l[x] *= f;
+          const f32x4 fh = {__shfl(f, 4 * g, 64), __shfl(f, 4 * g + 1, 64), __shfl(f, 4 * g + 2, 64), __shfl(f, 4 * g + 3, 64)};
+#pragma unroll
+          for (int e = 0; e < E; ++e) om[x][e] *= fh;
+          lm[x] *= fh;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        u32x4 hi2, lo2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float p[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float logit = s[x][i / 2][i % 2 * 2 + y];
+            p[y] = __builtin_amdgcn_exp2f(STEP ? (logit - ref[x]) - bias : fmaf(logit, scale2, -ref[x]));
+            if constexpr (STEP) l[x] += p[y];
+          }
+          const bf16x2 h = __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2);
+          // p - h in one instruction each.  (Minus zero beside minus one: the pair 0, -1.0 in this order would be written as the constant -1.0, which
+          // the instruction reads as a float's bits.)
+          const f32x2 rest = {__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, 0x8000BF80u), p[0], false),
+                              __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, 0xBF808000u), p[1], false)};
+          hi2[i] = __builtin_bit_cast(uint32_t, h);
+          lo2[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+        }
+        const bf16x8 hi = __builtin_bit_cast(bf16x8, hi2), lo = __builtin_bit_cast(bf16x8, lo2);
+        if constexpr (kAhead) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) om[x][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, vop[e / 2][e % 2], om[x][e], 0, 0, 0);
+          const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+          lm[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, ones, lm[x], 0, 0, 0);
+          lm[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, ones, lm[x], 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < E; ++e) om[x][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, vop[e / 2][e % 2], om[x][e], 0, 0, 0);
+        } else {
+          static_assert(kAhead || N == 1, "V is converted where it is used");
+#pragma unroll
+          for (int y = 0; y < E / 2; ++y) {
+            bf16x8 two[2];
+            convert_v(y, two, ve);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              om[x][2 * y + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, two[i], om[x][2 * y + i], 0, 0, 0);
+              om[x][2 * y + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, two[i], om[x][2 * y + i], 0, 0, 0);
+            }
+          }
+        }
+      }
+      if constexpr (kAhead) {
+        convert_k(0, kop[0]);
+        convert_k(1, kop[1]);
+        // the first columns' probabilities; the next ones' beside the products of those before, the next keys' conversion beside the last
+        __builtin_amdgcn_sched_group_barrier(0x002, 33, 1);
+#pragma unroll
+        for (int i = 0; i < N * (2 * E + 2); ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(0x002, 2, 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(kop[i][j]));
+        load_k(after);
+      }
+      if (__any(bad != 0)) {
+        // columns that see an entry whose block is NaN: counted by a product of ones
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          u32x4 sees, nan;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sees[i] = (seen[x] >> (2 * i) & 1 ? 0x3F80u : 0u) | (seen[x] >> (2 * i + 1) & 1 ? 0x3F800000u : 0u);
+            nan[i] = (bad >> (2 * i) & 1 ? 0x3F80u : 0u) | (bad >> (2 * i + 1) & 1 ? 0x3F800000u : 0u);
+          }
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, sees), __builtin_bit_cast(bf16x8, nan), zero, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float poison = met[i] > 0.f ? __uint_as_float(0x7FC00000u) : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) om[x][e][i] += poison;
+          }
+        }
+      }
+      t += kLeast4;
+      now = next;
+      next = after;
+    }
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      m[x] = ref[x];
+      l[x] = sum_rows(l[x]);
+      if constexpr (!STEP) {  // the lane of column c: register c % 4 of a lane of row c / 4
+        const float y = c % 4 == 0 ? lm[x][0] : c % 4 == 1 ? lm[x][1] : c % 4 == 2 ? lm[x][2] : lm[x][3];
+        l[x] = __shfl(y, (c >> 2) * 16 + c, 64);
+      }
+    }
+  }
+};
+
+template <int D>
+struct AttendShared {
+  float o[kWaves][kCols][D];
+  float ml[kWaves][kCols][2];
+  float M[kCols], inv[kCols];
+};
+
+__device__ __forceinline__ uint16_t* out_row(const AttendArgs& a, const Columns& col, int hk, int at) {
+  const int r = col.base + at;
+  return static_cast<uint16_t*>(a.out.ptr) + int64_t(a.token0(col.b) + r / a.G) * a.out.sn + int64_t(hk * a.G + r % a.G) * a.out.sh;
+}
+
+// A workgroup's share: its columns in N groups of 16.  `part`: which partial result.
+template <int D, Finds F, bool STEP, int N>
+__device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns& col, const TileList& list, const Sight (&mine)[N], int hk, int share,
+                                             int part, AttendShared<D>& sh) {
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4, b = col.b;
   const int t0 = share * list.share, t1 = min(t0 + list.share, list.tiles);
   if (t0 >= t1) return;
-  const int n = list.n;
+  constexpr int E = D / 16, kSteps = D / 32;
   if constexpr (STEP) {
     // the workgroup of the last tile stores the new token, and reads it back as it was encoded
     if (a.kn.ptr && t1 == list.tiles && a.lens[b] <= a.max_len) {
-      const int page = a.pool.page_of(b, n - 1);
-      if (page >= 0) store_new<uint16_t, Code4, D>(a, b, hk, page, n - 1, list.last);
+      const int page = a.pool.page_of(b, list.n - 1);
+      if (page >= 0) store_new<uint16_t, Code4, D>(a, b, hk, page, list.n - 1, list.last);
       __threadfence_block();
       __syncthreads();
     }
   }
-  // where every column sees a tile as a whole: entries up to the first column's last, from the last column's window on
+  // where every column sees a tile as a whole: entries up to the first column's last, from the latest window on
   int all_last, all_lo = INT32_MIN;
-  if constexpr (!STEP) {
-    all_last = __builtin_amdgcn_readfirstlane(__shfl(mine.last, 0, 64));
-    if (a.window != 0) {
-      all_lo = __builtin_amdgcn_readfirstlane(~row_min(c < cols ? ~mine.lo : INT32_MAX));  // the latest start
-    }
+  if constexpr (STEP) {
+    all_last = list.n - 1;
+    all_lo = mine[0].lo;
   } else {
-    all_last = n - 1;
-    all_lo = mine.lo;
+    all_last = __builtin_amdgcn_readfirstlane(mine[0].last);
+    if (a.window != 0) {
+      int latest = INT32_MAX;  // (complement: the minimum of ~lo)
+#pragma unroll
+      for (int x = 0; x < N; ++x) latest = min(latest, x * kCols + c < col.count ? ~mine[x].lo : INT32_MAX);
+      all_lo = __builtin_amdgcn_readfirstlane(~row_min(latest));
+    }
   }
-  const bool by_pos = a.window != 0 && a.pool.pos;
-  bf16x8 q[R::kSteps];
-  {
+  bf16x8 q[N][kSteps];
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
     const uint16_t* row = nullptr;
-    if (c < cols) {
-      const int r = col.base + c;
+    if (x * kCols + c < col.count) {
+      const int r = col.base + x * kCols + c;
       if constexpr (STEP)
         row = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + (hk * a.G + r) * a.q.sh;
       else
         row = static_cast<const uint16_t*>(a.q.ptr) + int64_t(a.token0(b) + r / a.G) * a.q.sn + int64_t(hk * a.G + r % a.G) * a.q.sh;
     }
 #pragma unroll
-    for (int i = 0; i < R::kSteps; ++i)
-      q[i] = row ? *reinterpret_cast<const bf16x8*>(row + g * (D / 4) + i * 8) : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+    for (int i = 0; i < kSteps; ++i)
+      q[x][i] = row ? *reinterpret_cast<const bf16x8*>(row + g * (D / 4) + i * 8) : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   }
-  const float scale2 = kLog2e / sqrtf(float(D));
-  const float bias = list.bias;  // probabilities are formed as 2^-bias * p, so that no mean of values of any size overflows
-  float m = -3.402823466e38f, l = 0.f;
-  f32x4 om[E] = {};  // register i: column 4 g + i, element c * E + index
   float* lg = STEP && a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
-  const auto table = (const __attribute__((address_space(4))) int32_t*)(a.pool.table + int64_t(b) * a.pool.max_pages);
-  const int rmask = (1 << a.pool.shift) - 1;
-  const uint32_t koff = uint32_t(c) * uint32_t(a.pool.k_row) + g * (D / 8), voff = uint32_t(4 * g) * uint32_t(a.pool.v_row) + c * (E / 2);
-  for (int t = t0 + w * 2 * U; t < t1; t += kLeast4) {
-    typename R::KReg k[2 * U], vx[2 * U];
-    typename R::VReg v[2 * U][4];
-    int ke[2 * U], s0[2 * U];
-    bool there[2 * U], whole[2 * U];
-    uint32_t absent[2 * U];  // (not WIDE) bit i: entry i of the tile has no page
-#pragma unroll
-    for (int u = 0; u < 2 * U; ++u) {
-      s0[u] = list.slot(min(t + u, t1 - 1));
-      there[u] = t + u < t1;
-      absent[u] = 0;
-      if constexpr (WIDE) {
-        const int page = table[s0[u] >> a.pool.shift];
-        there[u] = there[u] && uint32_t(page) < uint32_t(a.pool.n_pages);
-        const int p = uint32_t(page) < uint32_t(a.pool.n_pages) ? page : 0;
-        const int64_t at = ((int64_t(p) * Hkv + hk) << a.pool.shift) + (s0[u] & rmask);
-        const uint8_t* kp = a.pool.K + p * a.pool.k_page + hk * a.pool.k_head + (s0[u] & rmask) * a.pool.k_row;
-        const uint8_t* vp = a.pool.V + p * a.pool.v_page + hk * a.pool.v_head + (s0[u] & rmask) * a.pool.v_row;
-        k[u] = *reinterpret_cast<const typename R::KReg*>(kp + koff);
-        ke[u] = (a.pool.k_exp + at * kExps)[uint32_t(c * kExps + g * kExps / 4)];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[u][r] = __builtin_nontemporal_load(reinterpret_cast<const typename R::VReg*>(vp + r * a.pool.v_row + voff));
-        vx[u] = *reinterpret_cast<const typename R::KReg*>(a.pool.v_exp + at * kExps + uint32_t(4 * g * kExps));
-      } else {
-        // (rows that are not there: the first row of the pool, whose values are not used)
-        const int s = s0[u] + c, pk = s < n ? a.pool.page_of(b, s) : -1;
-        absent[u] = ~uint32_t(__ballot(pk >= 0)) & 0xFFFFu;
-        const uint8_t* kr = pk >= 0 ? a.pool.k_at(pk, hk, s) : a.pool.K;
-        k[u] = *reinterpret_cast<const typename R::KReg*>(kr + g * (D / 8));
-        ke[u] = a.pool.k_exp[(pk >= 0 ? a.pool.at(pk, hk, s) : 0) * kExps + g * kExps / 4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int sv = s0[u] + 4 * g + r, pv = __shfl(pk, 4 * g + r, 64);
-          const uint8_t* vr = pv >= 0 ? a.pool.v_at(pv, hk, sv) : a.pool.V;
-          v[u][r] = *reinterpret_cast<const typename R::VReg*>(vr + c * (E / 2));
-          const int8_t* ex = a.pool.v_exp + (pv >= 0 ? a.pool.at(pv, hk, sv) : 0) * kExps;
-          if constexpr (D == 128)
-            vx[u][r] = *reinterpret_cast<const uint32_t*>(ex);
-          else
-            vx[u][r / 2] = (r % 2 ? vx[u][r / 2] : 0u) | uint32_t(*reinterpret_cast<const uint16_t*>(ex)) << (16 * (r % 2));
-        }
-      }
-      whole[u] = there[u] && absent[u] == 0 && s0[u] + kTile - 1 <= all_last && !by_pos &&
-                 (s0[u] >= all_lo || s0[u] + kTile <= a.n_sink);
-    }
-#pragma unroll
-    for (int u2 = 0; u2 < U; ++u2) {
-      f32x4 s[2];
-      int ve[2][4];
-      uint32_t bad = 0;      // bit 4 i + r: a power of two that stands for NaN
-      uint32_t seen = 0xFFu;  // bit 4 i + r: this lane's column sees entry 4 g + r of tile i
-      float mx = m;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int u = 2 * u2 + i;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        const float scale = fp4_scale(ke[u]);
-#pragma unroll
-        for (int j = 0; j < R::kSteps; ++j)
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp4_decode8(k[u][j], scale)), q[j], x, 0, 0, 0);
-        s[i] = x * scale2;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if constexpr (D == 128)
-            ve[i][r] = __builtin_amdgcn_sbfe(int(vx[u][r]), 8 * (c >> 2), 8);
-          else
-            ve[i][r] = __builtin_amdgcn_sbfe(int(vx[u][r / 2]), 16 * (r % 2) + 8 * (c >> 3), 8);
-        }
-        if (!whole[u]) {
-          int32_t at[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            at[r] = s0[u] + 4 * g + r;
-            if (by_pos) {
-              const int p = at[r] < n ? a.pool.page_of(b, at[r]) : -1;
-              at[r] = p >= 0 ? a.pool.pos[a.pool.at(p, hk, at[r])] : 0;
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            // (no branches: where a lane's vector was changed behind some, one compiler kept the old element)
-            const int e = s0[u] + 4 * g + r;
-            const bool is = there[u] & (e < n) & !(absent[u] >> (4 * g + r) & 1);
-            const bool ok = is & (e <= mine.last) & ((at[r] >= mine.lo) | (at[r] < a.n_sink)), nan = is & (ve[i][r] == kNan4);
-            const float logit = s[i][r];
-            s[i][r] = ok ? logit : -INFINITY;
-            seen &= ~(uint32_t(!ok) << (4 * i + r));
-            bad |= uint32_t(nan) << (4 * i + r);
-            ve[i][r] = is & !nan ? min(ve[i][r], 125) : 0;
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[i][r]);
-        if (lg && c < cols && t + u < t1) *reinterpret_cast<f32x4*>(lg + list.slot(t + u) + 4 * g) = s[i];
-      }
-      mx = max_rows(mx);
-      if (__any(mx > m)) {
-        const float f = __builtin_amdgcn_exp2f(m - mx);
-        m = mx;
-        l *= f;
-        const f32x4 fh = {__shfl(f, 4 * g, 64), __shfl(f, 4 * g + 1, 64), __shfl(f, 4 * g + 2, 64), __shfl(f, 4 * g + 3, 64)};
-#pragma unroll
-        for (int e = 0; e < E; ++e) om[e] *= fh;
-      }
-      bf16x8 hi, lo;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f((s[i / 4][i % 4] - m) - bias);
-        l += p;
-        hi[i] = __bf16(p);
-        lo[i] = __bf16(p - float(hi[i]));
-      }
-#pragma unroll
-      for (int y = 0; y < E / 2; ++y) {  // elements 2 y and 2 y + 1 of the lane's
-        u32x4 even, odd;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int u = 2 * u2 + i / 2, r = i % 2 * 2;
-          auto two = [&](int rr) {
-            const float scale = fp4_scale(ve[i / 2][rr]);
-            const uint32_t codes = v[u][rr];
-            // (which byte has to be a constant)
-            const bf16x2 x = y == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)
-                             : y == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)
-                             : y == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)
-                                      : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
-            return __builtin_bit_cast(uint32_t, x);
-          };
-          const uint32_t x0 = two(r), x1 = two(r + 1);
-          even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100);
-          odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302);
-        }
-        om[2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, __builtin_bit_cast(bf16x8, even), om[2 * y], 0, 0, 0);
-        om[2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, __builtin_bit_cast(bf16x8, even), om[2 * y], 0, 0, 0);
-        om[2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, __builtin_bit_cast(bf16x8, odd), om[2 * y + 1], 0, 0, 0);
-        om[2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, __builtin_bit_cast(bf16x8, odd), om[2 * y + 1], 0, 0, 0);
-      }
-      if (__any(bad != 0)) {
-        // columns that see an entry whose block is NaN: counted by a product of ones
-        u32x4 sees, nan;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sees[i] = (seen >> (2 * i) & 1 ? 0x3F80u : 0u) | (seen >> (2 * i + 1) & 1 ? 0x3F800000u : 0u);
-          nan[i] = (bad >> (2 * i) & 1 ? 0x3F80u : 0u) | (bad >> (2 * i + 1) & 1 ? 0x3F800000u : 0u);
-        }
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, sees), __builtin_bit_cast(bf16x8, nan), zero, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (met[i] > 0.f)
-#pragma unroll
-            for (int e = 0; e < E; ++e) om[e][i] = __uint_as_float(0x7FC00000u);
-      }
-    }
-  }
-  // join the wavefronts
-  l = sum_rows(l);
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) so[w][4 * g + i][c * E + e] = om[e][i];
-  if (lane < kCols) {
-    sml[w][lane][0] = m;
-    sml[w][lane][1] = l;
-  }
-  __threadfence_block();  // (the logits, which the whole workgroup reads where it is a head's only one)
-  __syncthreads();
+  Share<D, F, STEP, N> work{a, col, list, hk, t0, t1, mine, w, lane, c, g, all_last, all_lo};
+  work.run(q, lg);
   const bool single = list.shares() == 1;
-  for (int i = tid; i < cols * D; i += 64 * kWaves) {
-    const int h = i / D, x0 = i % D;
-    float M = sml[0][h][0];
+  // join the wavefronts, 16 columns at a time
 #pragma unroll
-    for (int x = 1; x < kWaves; ++x) M = fmaxf(M, sml[x][h][0]);
-    float L = 0.f, o = 0.f;
+  for (int x = 0; x < N; ++x) {
+    if (x) __syncthreads();
 #pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
-      const float fx = __builtin_amdgcn_exp2f(sml[x][h][0] - M);
-      L = fmaf(sml[x][h][1], fx, L);
-      o = fmaf(so[x][h][x0], fx, o);
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh.o[w][4 * g + i][c * E + e] = work.om[x][e][i];
+    if (lane < kCols) {
+      sh.ml[w][lane][0] = work.m[x];
+      sh.ml[w][lane][1] = work.l[x];
     }
-    const int64_t at = int64_t(part) * (STEP ? a.G : kCols) + h;
-    if (single) {
-      const float y = L == 0.f ? 0.f : o / L;
-      if constexpr (STEP) {
-        store_out<uint16_t>(a, b, hk * a.G + h, x0, y);
-      } else {
-        const int r = col.base + h;
-        (static_cast<uint16_t*>(a.out.ptr) + int64_t(a.token0(b) + r / a.G) * a.out.sn + int64_t(hk * a.G + r % a.G) * a.out.sh)[x0] =
-            Elem<uint16_t>::from_f32(y);
+    __threadfence_block();  // (the logits, which the whole workgroup reads where it is a head's only one)
+    __syncthreads();
+    const int cols = min(col.count - x * kCols, kCols);
+    for (int i = tid; i < cols * D; i += 64 * kWaves) {
+      const int h = i / D, at = i % D;
+      float M = sh.ml[0][h][0];
+#pragma unroll
+      for (int y = 1; y < kWaves; ++y) M = fmaxf(M, sh.ml[y][h][0]);
+      float L = 0.f, o = 0.f;
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) {
+        const float f = __builtin_amdgcn_exp2f(sh.ml[y][h][0] - M);
+        L = fmaf(sh.ml[y][h][1], f, L);
+        o = fmaf(sh.o[y][h][at], f, o);
       }
-    } else {
-      a.part_o[at * D + x0] = o;
-    }
-    if (x0 == 0) {
+      const int64_t row = int64_t(part) * (STEP ? a.G : kGroup) + x * kCols + h;
       if (single) {
-        sM[h] = M;
-        sinv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
+        const float y = L == 0.f ? 0.f : o / L;
+        if constexpr (STEP)
+          store_out<uint16_t>(a, b, hk * a.G + h, at, y);
+        else
+          out_row(a, col, hk, x * kCols + h)[at] = Elem<uint16_t>::from_f32(y);
       } else {
-        a.part_ml[at * 2] = M;
-        a.part_ml[at * 2 + 1] = L;
+        a.part_o[row * D + at] = o;
+      }
+      if (at == 0) {
+        if (single) {
+          sh.M[h] = M;
+          sh.inv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
+        } else {
+          a.part_ml[row * 2] = M;
+          a.part_ml[row * 2 + 1] = L;
+        }
       }
     }
   }
-  if (lg && single) {
-    __syncthreads();
-    for (int i = tid; i < list.tiles * kTile; i += 64 * kWaves)
-      add_scores<1, kCols>(a, list, b, hk, i, 0, list.tiles * kTile, sM, sinv, [] {});
+  if constexpr (STEP) {
+    if (lg && single) {
+      __syncthreads();
+      for (int i = tid; i < list.tiles * kTile; i += 64 * kWaves)
+        add_scores<1, kCols>(a, list, b, hk, i, 0, list.tiles * kTile, sh.M, sh.inv, [] {});
+    }
   }
 }
 
-// Joins the shares of 16 columns: a workgroup per (group of columns, KV head), a wavefront per column at a time.
-template <int D>
-__global__ __launch_bounds__(64 * kWaves) void attend_join4(AttendArgs a, int least) {
-  const int index = blockIdx.x / a.pool.Hkv, hk = blockIdx.x % a.pool.Hkv;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// The step: a workgroup per (share, sequence and KV head), whose columns are the group's query heads.
+template <int D, Finds F>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void step_part4(AttendArgs a) {
+  __shared__ AttendShared<D> sh;
+  const int b = blockIdx.y / a.pool.Hkv, hk = blockIdx.y % a.pool.Hkv;
+  const TileList list(a, b, kLeast4);
+  if (list.n == 0) {
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < a.G * D; i += 64 * kWaves) store_out<uint16_t>(a, b, hk * a.G + i / D, i % D, 0.f);
+    return;
+  }
+  const Sight mine[1] = {{int(threadIdx.x & 15) < a.G ? list.n - 1 : -1, window_start(list.last, a.window)}};
+  attend_share<D, F, true, 1>(a, Columns{b, 0, a.G}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
+}
+
+// Several tokens per sequence: a workgroup per (group of columns, KV head, share).
+template <int D, Finds F>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void attend_part4(AttendArgs a) {
+  __shared__ AttendShared<D> sh;
+  // the last groups of a sequence see most: first
+  const int index = a.groups - 1 - int(blockIdx.x / a.splits) / a.pool.Hkv, hk = blockIdx.x / a.splits % a.pool.Hkv, share = blockIdx.x % a.splits;
+  const int part = (index * a.pool.Hkv + hk) * a.splits + share;
   const Columns col = find_columns(a, index);
   if (col.count <= 0) return;
-  Sight mine;
+  auto go = [&](auto groups) __attribute__((always_inline)) {
+    constexpr int N = decltype(groups)::value;
+    Sight mine[N];
+    TileList list;
+    if (sights_of<N>(a, col, threadIdx.x & 15, mine, list)) {
+      attend_share<D, F, false, N>(a, col, list, mine, hk, share, part, sh);
+    } else if (share == 0) {
+      for (int i = threadIdx.x; i < col.count * D; i += 64 * kWaves) out_row(a, col, hk, i / D)[i % D] = 0;
+    }
+  };
+  if (col.count > kCols)
+    go(std::integral_constant<int, kGroup / kCols>{});
+  else
+    go(std::integral_constant<int, 1>{});
+}
+
+// Joins the shares: a workgroup per (16 columns of a group, KV head), a wavefront per column at a time.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves) void attend_join4(AttendArgs a) {
+  constexpr int kParts = kGroup / kCols;
+  const int x = blockIdx.x % kParts, hk = blockIdx.x / kParts % a.pool.Hkv, index = blockIdx.x / kParts / a.pool.Hkv;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const Columns col = find_columns(a, index);
+  if (col.count <= x * kCols) return;
+  Sight mine[kParts];
   TileList list;
-  if (!sight_of(a, col, lane & 15, least, mine, list)) return;
+  if (!sights_of<kParts>(a, col, lane & 15, mine, list)) return;
   const int ns = list.shares();
   if (ns <= 1) return;
-  for (int h = w; h < min(col.count, kCols); h += kWaves) {
-    const int64_t at0 = int64_t(blockIdx.x) * a.splits * kCols + h;  // (share s: + s * kCols)
+  for (int h = x * kCols + w; h < min(col.count, (x + 1) * kCols); h += kWaves) {
+    const int64_t at0 = (int64_t(index) * a.pool.Hkv + hk) * a.splits * kGroup + h;  // (share s: + s * kGroup)
     const float* ml = a.part_ml + at0 * 2;
     float M = -3.402823466e38f, L = 0.f;
-    for (int s = lane; s < ns; s += 64) M = fmaxf(M, ml[int64_t(s) * kCols * 2]);
+    for (int s = lane; s < ns; s += 64) M = fmaxf(M, ml[int64_t(s) * kGroup * 2]);
     M = wave_max(M);
-    for (int s = lane; s < ns; s += 64) L = fmaf(ml[int64_t(s) * kCols * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(s) * kCols * 2] - M), L);
+    for (int s = lane; s < ns; s += 64) L = fmaf(ml[int64_t(s) * kGroup * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M), L);
     L = wave_sum(L);
     float o[D / 64] = {};
 #pragma unroll 4
     for (int s = 0; s < ns; ++s) {
-      const float f = __builtin_amdgcn_exp2f(ml[int64_t(s) * kCols * 2] - M);
+      const float f = __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M);
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) o[x] = fmaf(a.part_o[(at0 + int64_t(s) * kCols) * D + x * 64 + lane], f, o[x]);
+      for (int y = 0; y < D / 64; ++y) o[y] = fmaf(a.part_o[(at0 + int64_t(s) * kGroup) * D + y * 64 + lane], f, o[y]);
     }
-    const int r = col.base + h;
-    uint16_t* out = static_cast<uint16_t*>(a.out.ptr) + int64_t(a.token0(col.b) + r / a.G) * a.out.sn + int64_t(hk * a.G + r % a.G) * a.out.sh;
+    uint16_t* out = out_row(a, col, hk, h);
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x) out[x * 64 + lane] = Elem<uint16_t>::from_f32(L == 0.f ? 0.f : o[x] / L);
+    for (int y = 0; y < D / 64; ++y) out[y * 64 + lane] = Elem<uint16_t>::from_f32(L == 0.f ? 0.f : o[y] / L);
   }
 }
 
-bool wide_pages(const PagePool& p) {
-  // pages that hold whole tiles, displacements that fit, powers of two that can be read sixteen bytes at a time
-  return p.shift >= 4 && p.k_row < (1 << 24) && p.v_row < (1 << 24) && !(reinterpret_cast<uintptr_t>(p.v_exp) & 15);
+// Rows by pairs of tiles where a page holds whole pairs, and displacements, strides and alignment are as at_row and the loads of powers of two take them.
+Finds finds_of(const PagePool& p) {
+  const bool scalar = p.k_row < (1 << 21) && p.v_row < (1 << 21) && p.k_page < (int64_t(1) << 32) && p.v_page < (int64_t(1) << 32) &&
+                      !(reinterpret_cast<uintptr_t>(p.v_exp) & 15);
+  return !scalar || p.shift < 4 ? ROWS : p.shift == 4 ? TILES : PAIRS;
 }
 
 template <int D>
 void launch_step4(AttendArgs& a, int batch, hipStream_t s) {
   const int bh = batch * a.pool.Hkv;
-  const auto part = wide_pages(a.pool) ? attend_part4<D, true, true> : attend_part4<D, false, true>;
+  const Finds f = finds_of(a.pool);
+  const auto part = f == PAIRS ? step_part4<D, PAIRS> : f == TILES ? step_part4<D, TILES> : step_part4<D, ROWS>;
   part<<<dim3(a.splits, bh), 64 * kWaves, 0, s>>>(a);
   if (a.splits == 1) return;
   a.joins = batch * a.Hq;
@@ -453,21 +710,22 @@ void launch_step4(AttendArgs& a, int batch, hipStream_t s) {
 
 template <int D>
 void launch_attend4(const AttendArgs& a, hipStream_t s) {
-  const auto part = wide_pages(a.pool) ? attend_part4<D, true, false> : attend_part4<D, false, false>;
+  const Finds f = finds_of(a.pool);
   const unsigned heads = unsigned(a.groups) * a.pool.Hkv;
+  const auto part = f == PAIRS ? attend_part4<D, PAIRS> : f == TILES ? attend_part4<D, TILES> : attend_part4<D, ROWS>;
   part<<<dim3(heads * a.splits), 64 * kWaves, 0, s>>>(a);
-  if (a.splits > 1) attend_join4<D><<<dim3(heads), 64 * kWaves, 0, s>>>(a, kLeast4);
+  if (a.splits > 1) attend_join4<D><<<dim3(heads * (kGroup / kCols)), 64 * kWaves, 0, s>>>(a);
 }
 
 // Groups of columns of n_tokens query tokens, at most: every sequence may leave its last one unfinished.
 int64_t column_groups(const d2o_pages* p, int32_t n_tokens) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
-  return std::min(int64_t(n_tokens) * ((G + kCols - 1) / kCols), int64_t(n_tokens) * G / kCols + p->batch);
+  return std::min(int64_t(n_tokens), int64_t(n_tokens) * G / kGroup + p->batch);
 }
 size_t attend_bytes(const d2o_pages* p, int32_t max_len, int32_t n_tokens, int* splits) {
   const int64_t heads = column_groups(p, n_tokens) * p->n_kv_heads;
   *splits = step_splits(heads, most_tiles(p, max_len, 0, 0));
-  const size_t rows = size_t(heads) * *splits * kCols;
+  const size_t rows = size_t(heads) * *splits * kGroup;
   return *splits > 1 ? round256(rows * p->head_dim * sizeof(float)) + round256(rows * 2 * sizeof(float)) : 0;
 }
 
@@ -477,7 +735,7 @@ int check_attend(const d2o_pages* p, PagePool* pool, int32_t n_tokens, int32_t m
   if (!p->cache_fp4) return D2O_ERR_UNSUPPORTED;
   if (n_tokens < 0 || max_len < 1) return D2O_ERR_INVALID_ARG;
   // products of tokens and heads that are formed in 32 bits, and the grid
-  if (int64_t(n_tokens) * p->n_q_heads > 0x3FFFFFFF || column_groups(p, n_tokens) * p->n_kv_heads > 0x3FFFFF) return D2O_ERR_UNSUPPORTED;
+  if (int64_t(n_tokens) * p->n_q_heads > 0x3FFFFFFF || column_groups(p, n_tokens) * p->n_kv_heads > 0xFFFFF) return D2O_ERR_UNSUPPORTED;
   return D2O_OK;
 }
 
@@ -530,13 +788,14 @@ extern "C" int d2o_pages_attend(const d2o_pages* pages, d2o_view q, int32_t n_to
   a.groups = int(column_groups(pages, n_tokens));
   const int64_t heads = int64_t(a.groups) * pages->n_kv_heads;
   a.part_o = static_cast<float*>(workspace);
-  a.part_ml = need ? a.part_o + round256(size_t(heads) * a.splits * kCols * pages->head_dim * sizeof(float)) / sizeof(float) : nullptr;
+  a.part_ml = need ? a.part_o + round256(size_t(heads) * a.splits * kGroup * pages->head_dim * sizeof(float)) / sizeof(float) : nullptr;
   a.splits = std::min(a.splits, step_splits(heads, most_tiles(pages, max_len, window, n_sink)));
   a.Hq = pages->n_q_heads;
   a.G = pages->n_q_heads / pages->n_kv_heads;
   a.max_len = max_len;
   a.window = window;
   a.n_sink = n_sink;
+  a.pairs = 1;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (pages->head_dim == 64)
     launch_attend4<64>(a, s);

