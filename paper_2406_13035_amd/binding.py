@@ -439,14 +439,26 @@ def _view_of(t: torch.Tensor, rows=True) -> d2o_view:
 
 def _tensor_ok(t, shape, dtype, device, what, whole=False):
     """`t` has this shape, type and device, and its last dimension (`whole`: all of it) is contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device
-            and (t.is_contiguous() if whole else t.stride(-1) == 1)):
-        raise D2OError(f"{what}: a tensor of shape {tuple(shape)} and type {dtype} on {device}, "
-                       f"{'contiguous' if whole else 'with its last dimension contiguous'}, is needed")
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.device == device
+                and (t.is_contiguous() if whole else t.stride(-1) == 1)):
+            return
+    except AttributeError:
+        pass
+    raise D2OError(f"{what}: a tensor of shape {tuple(shape)} and type {dtype} on {device}, "
+                   f"{'contiguous' if whole else 'with its last dimension contiguous'}, is needed")
 
 
 def _vector_ok(t, shape, dtype, device, what):
     _tensor_ok(t, shape, dtype, device, what, whole=True)
+
+
+def _pointer(t, shape, dtype, device, what):
+    """Of a contiguous tensor of this shape, type and device; None stays None."""
+    if t is None:
+        return None
+    _tensor_ok(t, shape, dtype, device, what, True)
+    return t.data_ptr()
 
 
 def _int32_ok(*values):
@@ -594,53 +606,49 @@ class Pages:
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_evict(
             self._ref, self._lens(lens), self._bound, budget, recent, n_sink, *self._ws, stream)), "d2o_pages_evict")
 
-    def _packed(self, t, heads, what, n=None):
+    def _packed(self, t, shape, what):
         """A view of packed tokens [n, heads, d]."""
-        _need(isinstance(t, torch.Tensor) and t.dim() == 3, f"{what}: a tensor [tokens, heads, d] is needed")
-        _tensor_ok(t, (t.shape[0] if n is None else n, heads, self.head_dim), self.dtype, self.device, what)
-        return d2o_view(t.data_ptr(), 0, t.stride(1) if heads > 1 else 0, t.stride(0) if t.shape[0] > 1 else 0)
+        _tensor_ok(t, shape, self.dtype, self.device, what)
+        token, head, _ = t.stride()
+        return d2o_view(t.data_ptr(), 0, head if shape[1] > 1 else 0, token if shape[0] > 1 else 0)
 
-    def _slots(self, K, V, slots):
-        k = self._packed(K, self.n_kv_heads, "K")
-        n = K.shape[0]
-        _vector_ok(slots, (n,), torch.int64, self.device, "slots")
-        return k, self._packed(V, self.n_kv_heads, "V", n), n, slots.data_ptr()
+    def _rows(self, K, V, slots):
+        _need(isinstance(slots, torch.Tensor) and slots.dim() == 1, "slots: an int64 tensor [tokens] is needed")
+        n = slots.shape[0]
+        shape = (n, self.n_kv_heads, self.head_dim)
+        return self._packed(K, shape, "K"), self._packed(V, shape, "V"), n, _pointer(slots, (n,), torch.int64, self.device, "slots")
 
     def d2o_pages_put(self, K, V, slots, positions=None):
         """Tokens' rows K, V [n, Hkv, d] into slots (int64 [n], as d2o_pages_map gives them; outside the pool: left out), with score 0 and, where
         the pages keep positions, positions (int32 [n])."""
-        k, v, n, at = self._slots(K, V, slots)
-        if positions is not None:
-            _vector_ok(positions, (n,), torch.int32, self.device, "positions")
-        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_put(
-            self._ref, k, v, n, at, None if positions is None else positions.data_ptr(), stream)), "d2o_pages_put")
+        k, v, n, at = self._rows(K, V, slots)
+        pos = _pointer(positions, (n,), torch.int32, self.device, "positions")
+        _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_put(self._ref, k, v, n, at, pos, stream)), "d2o_pages_put")
 
     def d2o_pages_get(self, slots, K, V):
         """Rows of slots (int64 [n]) as values into K, V [n, Hkv, d]; rows of slots outside the pool stay as they were."""
-        k, v, n, at = self._slots(K, V, slots)
+        k, v, n, at = self._rows(K, V, slots)
         _ok(_enqueue(self.device, lambda stream: self.lib.d2o_pages_get(self._ref, k, v, n, at, stream)), "d2o_pages_get")
 
     def d2o_pages_attend(self, q, first, lens, out, positions=None, window=0, n_sink=0):
         """Attention of several new tokens per sequence, whose rows the pages (of 4-bit rows) hold already: q, out [n, Hq, d] packed;
         first int32 [B + 1]: rows first[b] .. first[b + 1] - 1 are the last tokens of sequence b; lens int32 [B], those included;
         positions int32 [n], None: the entries' numbers."""
-        qv = self._packed(q, self.n_q_heads, "q")
-        n = q.shape[0]
-        ov = self._packed(out, self.n_q_heads, "out", n)
-        _vector_ok(first, (self.batch + 1,), torch.int32, self.device, "first")
-        at = self._lens(lens)
-        if positions is not None:
-            _vector_ok(positions, (n,), torch.int32, self.device, "positions")
+        _need(isinstance(q, torch.Tensor) and q.dim() == 3, "q: a tensor [tokens, Hq, d] is needed")
+        n, dev = q.shape[0], self.device
+        shape = (n, self.n_q_heads, self.head_dim)
+        qv, ov = self._packed(q, shape, "q"), self._packed(out, shape, "out")
+        start, at = _pointer(first, (self.batch + 1,), torch.int32, dev, "first"), self._lens(lens)
+        pos = _pointer(positions, (n,), torch.int32, dev, "positions")
         _int32_ok(window, n_sink, n)
         need = C.c_size_t()
         _ok(self.lib.d2o_pages_attend_workspace_bytes(self._ref, n, self._bound, C.byref(need)), "d2o_pages_attend_workspace_bytes")
 
         def call(stream):
-            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-            return self.lib.d2o_pages_attend(self._ref, qv, n, first.data_ptr(), at, None if positions is None else positions.data_ptr(),
-                                             self._bound, window, n_sink, ov, None if ws is None else ws.data_ptr(), need.value,
-                                             stream)
-        _ok(_enqueue(self.device, call), "d2o_pages_attend")
+            ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+            return self.lib.d2o_pages_attend(self._ref, qv, n, start, at, pos, self._bound, window, n_sink, ov,
+                                             None if ws is None else ws.data_ptr(), need.value, stream)
+        _ok(_enqueue(dev, call), "d2o_pages_attend")
 
 
 def d2o_qk_norm_rope(Q, K, q_weight=None, k_weight=None, eps: float = 1e-6, positions=None, pos0: int = 0,
@@ -654,33 +662,32 @@ def d2o_qk_norm_rope(Q, K, q_weight=None, k_weight=None, eps: float = 1e-6, posi
           "Q and K: four-dimensional float32 or bfloat16 tensors on a GPU are needed")
     B, _, n, d = one.shape
     dev, dt = one.device, one.dtype
-    views, outs, heads = [], [], []
-    for x, y, w, what in ((Q, Q_out, q_weight, "Q"), (K, K_out, k_weight, "K")):
+
+    def both(x, out, w, what):
         if x is None:
-            _need(y is None, f"{what}_out belongs to {what}")
-            views += [_NULL_VIEW, _NULL_VIEW]
-            outs.append(None)
-            heads.append(0)
-            continue
+            _need(out is None, f"{what}_out belongs to {what}")
+            return 0, _NULL_VIEW, _NULL_VIEW, None, None
         _need(isinstance(x, torch.Tensor) and x.dim() == 4, f"{what}: a tensor [B, heads, n, d] is needed")
-        _tensor_ok(x, (B, x.shape[1], n, d), dt, dev, what)
-        if y is None:
-            y = torch.empty(x.shape, dtype=dt, device=dev)
-        _tensor_ok(y, x.shape, dt, dev, what + "_out")
-        if w is not None:
-            _vector_ok(w, (d,), dt, dev, what.lower() + "_weight")
-        views += [_view_of(x), _view_of(y)]
-        outs.append(y)
-        heads.append(x.shape[1])
-    if positions is not None:
-        _vector_ok(positions, (B, n), torch.int32, dev, "positions")
+        shape = x.shape
+        h = shape[1]
+        _tensor_ok(x, (B, h, n, d), dt, dev, what)
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=dev)
+        elif out is not x:
+            _tensor_ok(out, shape, dt, dev, what + "_out")
+        views = []
+        for t in (x, out):
+            s = t.stride()  # (a dimension of size one may have any stride: it takes no part)
+            views.append(d2o_view(t.data_ptr(), s[0] if B > 1 else 0, s[1] if h > 1 else 0, s[2] if n > 1 else 0))
+        return h, views[0], views[1], out, _pointer(w, (d,), dt, dev, "weights of " + what)
+    hq, q, qo, Q_out, wq = both(Q, Q_out, q_weight, "Q")
+    hk, k, ko, K_out, wk = both(K, K_out, k_weight, "K")
+    pos = _pointer(positions, (B, n), torch.int32, dev, "positions")
     rot_dim = d if rot_dim is None else rot_dim
     _int32_ok(B, n, pos0, rot_dim)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     _ok(_enqueue(dev, lambda stream: lib.d2o_qk_norm_rope(
-        B, n, heads[0], heads[1], d, _DTYPE_CODES[dt], views[0], views[2], ptr(q_weight), ptr(k_weight), eps, rot_dim,
-        ptr(positions), pos0, rope_base, views[1], views[3], stream)), "d2o_qk_norm_rope")
-    return outs[0], outs[1]
+        B, n, hq, hk, d, _DTYPE_CODES[dt], q, k, wq, wk, eps, rot_dim, pos, pos0, rope_base, qo, ko, stream)), "d2o_qk_norm_rope")
+    return Q_out, K_out
 
 
 def d2o_pages_map(page_table, lens, change, free_pages, free_state, page_size: int, max_tokens=None, first=None, slots=None,
@@ -695,32 +702,31 @@ def d2o_pages_map(page_table, lens, change, free_pages, free_state, page_size: i
           "page_table: an int32 tensor [B, max_pages] on a GPU is needed")
     B, max_pages = page_table.shape
     dev, i32 = page_table.device, torch.int32
-    _vector_ok(page_table, (B, max_pages), i32, dev, "page_table")
     _need(isinstance(free_pages, torch.Tensor) and free_pages.dim() == 1, "free_pages: an int32 tensor [pages] is needed")
     if max_tokens is None:
         _need(isinstance(slots, torch.Tensor) and slots.dim() == 1, "max_tokens, or slots, an int64 tensor [tokens], is needed")
         max_tokens = slots.shape[0]
-    _int32_ok(B, max_pages, max_tokens, page_size, free_pages.shape[0])
+    n_pages = free_pages.shape[0]
+    _int32_ok(B, max_pages, max_tokens, page_size, n_pages)
     _need(max_tokens >= 0, "max_tokens: not negative")
     lens_out = lens if lens_out is None else lens_out
     free_state_out = free_state if free_state_out is None else free_state_out
     first = torch.empty(B + 1, dtype=i32, device=dev) if first is None else first
     slots = torch.empty(max_tokens, dtype=torch.int64, device=dev) if slots is None else slots
     positions = torch.empty(max_tokens, dtype=i32, device=dev) if positions is None else positions
-    for t, n, dt, what in ((lens, B, i32, "lens"), (change, B, i32, "change"), (lens_out, B, i32, "lens_out"),
-                           (free_pages, free_pages.shape[0], i32, "free_pages"), (free_state, 2, i32, "free_state"),
-                           (free_state_out, 2, i32, "free_state_out"), (first, B + 1, i32, "first"),
-                           (slots, max_tokens, torch.int64, "slots"), (positions, max_tokens, i32, "positions")):
-        _vector_ok(t, (n,), dt, dev, what)
+    per, rows = (B,), (max_tokens,)
+    args = (B, page_size, n_pages, max_pages, _pointer(page_table, (B, max_pages), i32, dev, "page_table"),
+            _pointer(lens, per, i32, dev, "lens"), _pointer(change, per, i32, dev, "change"),
+            _pointer(free_pages, (n_pages,), i32, dev, "free_pages"), _pointer(free_state, (2,), i32, dev, "free_state"), max_tokens,
+            _pointer(lens_out, per, i32, dev, "lens_out"), _pointer(free_state_out, (2,), i32, dev, "free_state_out"),
+            _pointer(first, (B + 1,), i32, dev, "first"), _pointer(slots, rows, torch.int64, dev, "slots"),
+            _pointer(positions, rows, i32, dev, "positions"))
     need = C.c_size_t()
     _ok(lib.d2o_pages_map_workspace_bytes(B, max_pages, max_tokens, C.byref(need)), "d2o_pages_map_workspace_bytes")
 
     def call(stream):
         ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-        return lib.d2o_pages_map(B, page_size, free_pages.shape[0], max_pages, page_table.data_ptr(), lens.data_ptr(),
-                                 change.data_ptr(), free_pages.data_ptr(), free_state.data_ptr(), max_tokens,
-                                 lens_out.data_ptr(), free_state_out.data_ptr(), first.data_ptr(), slots.data_ptr(),
-                                 positions.data_ptr(), None if ws is None else ws.data_ptr(), need.value, stream)
+        return lib.d2o_pages_map(*args, None if ws is None else ws.data_ptr(), need.value, stream)
     _ok(_enqueue(dev, call), "d2o_pages_map")
     return lens_out, first, slots, positions
 
