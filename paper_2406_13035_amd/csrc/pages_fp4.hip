@@ -10,24 +10,31 @@ namespace {
 struct AttendArgs : StepArgs {
   const int32_t* first;  // [B + 1] first query token of every sequence
   int32_t n_tokens, batch, groups;  // rows of q; groups of columns, at most
-  __device__ __forceinline__ int token0(int b) const { return min(max(first[b], 0), n_tokens); }
-  __device__ __forceinline__ int tokens(int b) const { return max(token0(b + 1) - token0(b), 0); }
+  uint32_t over_g;                  // ceil(2^32 / G): x / G is the upper half of x * over_g for x < 2^28
+  __device__ __forceinline__ int token_of(int pair) const { return G == 1 ? pair : int(__umulhi(uint32_t(pair), over_g)); }
 };
-constexpr int kCols = 16;         // columns of a matrix product
-constexpr int kGroup = 32;        // columns of a workgroup at most
+constexpr int kCols = 16;            // columns of a matrix product
+constexpr int kGroup = 32;           // columns of a workgroup at most
 constexpr int kLeast4 = kWaves * 2;  // tiles of a workgroup's round: a pair for each wavefront
 
 // Which columns a workgroup has.  Step: the group's query heads of sequence b.
 struct Columns {
-  int b, base, count;  // sequence, first pair, pairs of the sequence from there on (0: none)
+  int b, base, count;       // sequence, first pair, pairs (0: none)
+  int token0, tokens, len;  // (attend) the sequence's first query token, how many it has, its entries
 };
-// The index-th group of kGroup columns of the batch; all threads of the workgroup.
+// The index-th group of kGroup columns of the batch (of a sequence's, which see more and more, the last one first); all threads of the workgroup.
 __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) {
-  __shared__ int sum[kWaves], found[3];
+  __shared__ int sum[kWaves], found[6];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int per = (a.batch + 64 * kWaves - 1) / (64 * kWaves), b0 = tid * per, b1 = min(b0 + per, a.batch);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (a.tokens(b) * a.G + kGroup - 1) / kGroup;
+  auto token0 = [&](int b) { return min(max(a.first[b], 0), a.n_tokens); };
+  int mine = 0, len = 0, start = 0, end = 0;
+  for (int b = b0; b < b1; ++b) {
+    start = token0(b);
+    end = token0(b + 1);
+    len = a.lens[b];  // (of the last one; there is one nearly always)
+    mine += (max(end - start, 0) * a.G + kGroup - 1) / kGroup;
+  }
   int inc = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -41,17 +48,27 @@ __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) 
   int at = inc - mine;
   if (index >= at && index < inc)
     for (int b = b0; b < b1; ++b) {
-      const int pairs = a.tokens(b) * a.G, n = (pairs + kGroup - 1) / kGroup;
+      if (per > 1) {
+        start = token0(b);
+        end = token0(b + 1);
+        len = a.lens[b];
+      }
+      const int tokens = max(end - start, 0), pairs = tokens * a.G, n = (pairs + kGroup - 1) / kGroup;
       if (index < at + n) {
+        const int base = (n - 1 - (index - at)) * kGroup;
         found[0] = b;
-        found[1] = (index - at) * kGroup;
-        found[2] = min(pairs - found[1], kGroup);
+        found[1] = base;
+        found[2] = min(pairs - base, kGroup);
+        found[3] = start;
+        found[4] = tokens;
+        found[5] = min(len, a.max_len);
         break;
       }
       at += n;
     }
   __syncthreads();
-  return {__builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[2])};
+  auto scalar = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
+  return {scalar(0), scalar(1), scalar(2), scalar(3), scalar(4), scalar(5)};
 }
 
 // What a column sees: entries up to `last`, of these the ones with a position from `lo` on or below n_sink.
@@ -70,17 +87,17 @@ __device__ __forceinline__ int row_min(int v) {
 // The sights of columns c, c + 16, .. (N of them), and the tiles that any of the columns sees; false where there are none.
 template <int N>
 __device__ __forceinline__ bool sights_of(const AttendArgs& a, const Columns& col, int c, Sight (&mine)[N], TileList& list) {
-  const int m = a.tokens(col.b), len = min(a.lens[col.b], a.max_len), token0 = a.token0(col.b);
+  const int before = col.len - col.tokens;
   int lo = INT32_MAX;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = i * kCols + c, token = (col.base + at) / a.G;
+    const int at = i * kCols + c, token = a.token_of(col.base + at);
     const bool is = at < col.count;
-    mine[i].last = is ? max(len - m + token, -1) : -1;
-    mine[i].lo = window_start(a.positions && is ? a.positions[token0 + token] : mine[i].last, a.window);
+    mine[i].last = is ? max(before + token, -1) : -1;
+    mine[i].lo = window_start(a.window != 0 && a.positions && is ? a.positions[col.token0 + token] : mine[i].last, a.window);
     lo = min(lo, is ? mine[i].lo : INT32_MAX);
   }
-  list.n = max(len - m + (col.base + col.count - 1) / a.G + 1, 0);
+  list.n = max(before + a.token_of(col.base + col.count - 1) + 1, 0);
   list.last = 0;
   if (list.n == 0) return false;
   list.choose(a, a.window == 0 ? 0 : __builtin_amdgcn_readfirstlane(row_min(lo)), kLeast4);
@@ -248,7 +265,7 @@ struct Share {
   // the products, come from the matrix core too (P times ones).
   __device__ __forceinline__ void run(const bf16x8 (&q)[N][kSteps], float* lg) {
     const float scale2 = kLog2e / sqrtf(float(D));
-    const float bias = list.bias, start = STEP ? 0.f : -bias / scale2;
+    const float bias = list.bias, start = STEP ? 0.f : -bias / scale2, slack = STEP ? float(kSlack) : kSlack / scale2;
     const bool by_pos = a.window != 0 && a.pool.pos;
     const int n = list.n;
     f32x4 lm[N];   // (not STEP) sums of P: register i: column 4 g + i
@@ -385,7 +402,7 @@ struct Share {
         mx[x] = m[x];
 #pragma unroll
         for (int i = 0; i < 8; ++i) mx[x] = fmaxf(mx[x], s[x][i / 4][i % 4]);
-        grown |= mx[x] > m[x];
+        grown |= mx[x] > m[x] + slack;
       }
       if (__any(grown)) {
 #pragma unroll
@@ -500,12 +517,19 @@ template <int D>
 struct AttendShared {
   float o[kWaves][kCols][D];
   float ml[kWaves][kCols][2];
-  float M[kCols], inv[kCols];
+  float M[kCols], inv[kCols], sum[kCols];  // of the whole workgroup
+  float f[kWaves][kCols];                  // what a wavefront's outputs count for
 };
 
-__device__ __forceinline__ uint16_t* out_row(const AttendArgs& a, const Columns& col, int hk, int at) {
-  const int r = col.base + at;
-  return static_cast<uint16_t*>(a.out.ptr) + int64_t(a.token0(col.b) + r / a.G) * a.out.sn + int64_t(hk * a.G + r % a.G) * a.out.sh;
+// Four elements of an output.
+__device__ __forceinline__ void store_out4(uint16_t* to, const f32x4& o) {
+  *reinterpret_cast<u32x2*>(to) = u32x2{uint32_t(Elem<uint16_t>::from_f32(o[0])) | uint32_t(Elem<uint16_t>::from_f32(o[1])) << 16,
+                                        uint32_t(Elem<uint16_t>::from_f32(o[2])) | uint32_t(Elem<uint16_t>::from_f32(o[3])) << 16};
+}
+// Displacement of column `at` in q or out.
+__device__ __forceinline__ int64_t column_at(const AttendArgs& a, const View& v, const Columns& col, int hk, int at) {
+  const int r = col.base + at, token = a.token_of(r);
+  return int64_t(col.token0 + token) * v.sn + int64_t(hk * a.G + r - token * a.G) * v.sh;
 }
 
 // A workgroup's share: its columns in N groups of 16.  `part`: which partial result.
@@ -544,11 +568,10 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
   for (int x = 0; x < N; ++x) {
     const uint16_t* row = nullptr;
     if (x * kCols + c < col.count) {
-      const int r = col.base + x * kCols + c;
       if constexpr (STEP)
-        row = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + (hk * a.G + r) * a.q.sh;
+        row = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + (hk * a.G + c) * a.q.sh;
       else
-        row = static_cast<const uint16_t*>(a.q.ptr) + int64_t(a.token0(b) + r / a.G) * a.q.sn + int64_t(hk * a.G + r % a.G) * a.q.sh;
+        row = static_cast<const uint16_t*>(a.q.ptr) + column_at(a, a.q, col, hk, x * kCols + c);
     }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
@@ -563,9 +586,10 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
   for (int x = 0; x < N; ++x) {
     if (x) __syncthreads();
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sh.o[w][4 * g + i][c * E + e] = work.om[x][e][i];
+      for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<f32x4*>(&sh.o[w][4 * g + i][c * E + e]) = f32x4{work.om[x][e][i], work.om[x][e + 1][i], work.om[x][e + 2][i], work.om[x][e + 3][i]};
     if (lane < kCols) {
       sh.ml[w][lane][0] = work.m[x];
       sh.ml[w][lane][1] = work.l[x];
@@ -573,36 +597,41 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
     __threadfence_block();  // (the logits, which the whole workgroup reads where it is a head's only one)
     __syncthreads();
     const int cols = min(col.count - x * kCols, kCols);
-    for (int i = tid; i < cols * D; i += 64 * kWaves) {
-      const int h = i / D, at = i % D;
-      float M = sh.ml[0][h][0];
+    if (tid < cols) {  // a thread per column: what each wavefront's outputs count for
+      float M = sh.ml[0][tid][0], f[kWaves], L = 0.f;
 #pragma unroll
-      for (int y = 1; y < kWaves; ++y) M = fmaxf(M, sh.ml[y][h][0]);
-      float L = 0.f, o = 0.f;
+      for (int y = 1; y < kWaves; ++y) M = fmaxf(M, sh.ml[y][tid][0]);
 #pragma unroll
       for (int y = 0; y < kWaves; ++y) {
-        const float f = __builtin_amdgcn_exp2f(sh.ml[y][h][0] - M);
-        L = fmaf(sh.ml[y][h][1], f, L);
-        o = fmaf(sh.o[y][h][at], f, o);
+        f[y] = __builtin_amdgcn_exp2f(sh.ml[y][tid][0] - M);
+        L = fmaf(sh.ml[y][tid][1], f[y], L);
       }
-      const int64_t row = int64_t(part) * (STEP ? a.G : kGroup) + x * kCols + h;
       if (single) {
-        const float y = L == 0.f ? 0.f : o / L;
-        if constexpr (STEP)
-          store_out<uint16_t>(a, b, hk * a.G + h, at, y);
-        else
-          out_row(a, col, hk, x * kCols + h)[at] = Elem<uint16_t>::from_f32(y);
+        sh.M[tid] = M;
+        sh.inv[tid] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
+        sh.sum[tid] = L;
       } else {
-        a.part_o[row * D + at] = o;
+        const int64_t row = int64_t(part) * (STEP ? a.G : kGroup) + x * kCols + tid;
+        a.part_ml[row * 2] = M;
+        a.part_ml[row * 2 + 1] = L;
       }
-      if (at == 0) {
-        if (single) {
-          sh.M[h] = M;
-          sh.inv[h] = L == 0.f ? 0.f : ldexpf(1.f / L, -list.bias);
-        } else {
-          a.part_ml[row * 2] = M;
-          a.part_ml[row * 2 + 1] = L;
-        }
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) sh.f[y][tid] = f[y];
+    }
+    __syncthreads();
+    const int at = tid % (D / 4) * 4;
+    for (int h = tid / (D / 4); h < cols; h += 64 * kWaves / (D / 4)) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) o += *reinterpret_cast<const f32x4*>(&sh.o[y][h][at]) * sh.f[y][h];
+      if (single) {
+        const float L = sh.sum[h];
+        o = L == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / L;
+        store_out4(STEP ? static_cast<uint16_t*>(a.out.ptr) + b * a.out.sb + (hk * a.G + h) * a.out.sh + at
+                        : static_cast<uint16_t*>(a.out.ptr) + column_at(a, a.out, col, hk, x * kCols + h) + at, o);
+      } else {
+        const int64_t row = int64_t(part) * (STEP ? a.G : kGroup) + x * kCols + h;
+        *reinterpret_cast<f32x4*>(a.part_o + row * D + at) = o;
       }
     }
   }
@@ -627,15 +656,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
     return;
   }
   const Sight mine[1] = {{int(threadIdx.x & 15) < a.G ? list.n - 1 : -1, window_start(list.last, a.window)}};
-  attend_share<D, F, true, 1>(a, Columns{b, 0, a.G}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
+  attend_share<D, F, true, 1>(a, Columns{b, 0, a.G, 0, 0, 0}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
 }
 
 // Several tokens per sequence: a workgroup per (group of columns, KV head, share).
 template <int D, Finds F>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void attend_part4(AttendArgs a) {
   __shared__ AttendShared<D> sh;
-  // the last groups of a sequence see most: first
-  const int index = a.groups - 1 - int(blockIdx.x / a.splits) / a.pool.Hkv, hk = blockIdx.x / a.splits % a.pool.Hkv, share = blockIdx.x % a.splits;
+  // neighbouring workgroups are of different KV heads: with eight of them (or a multiple) the groups of a sequence that read one head's rows share an L2
+  const int hk = blockIdx.x % a.pool.Hkv, share = blockIdx.x / a.pool.Hkv % a.splits, index = blockIdx.x / a.pool.Hkv / a.splits;
   const int part = (index * a.pool.Hkv + hk) * a.splits + share;
   const Columns col = find_columns(a, index);
   if (col.count <= 0) return;
@@ -646,7 +675,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     if (sights_of<N>(a, col, threadIdx.x & 15, mine, list)) {
       attend_share<D, F, false, N>(a, col, list, mine, hk, share, part, sh);
     } else if (share == 0) {
-      for (int i = threadIdx.x; i < col.count * D; i += 64 * kWaves) out_row(a, col, hk, i / D)[i % D] = 0;
+      for (int i = threadIdx.x; i < col.count * D; i += 64 * kWaves) static_cast<uint16_t*>(a.out.ptr)[column_at(a, a.out, col, hk, i / D) + i % D] = 0;
     }
   };
   if (col.count > kCols)
@@ -655,38 +684,40 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     go(std::integral_constant<int, 1>{});
 }
 
-// Joins the shares: a workgroup per (16 columns of a group, KV head), a wavefront per column at a time.
+// Joins the shares: a workgroup per (16 columns of a group, KV head), 16 lanes per column.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void attend_join4(AttendArgs a) {
-  constexpr int kParts = kGroup / kCols;
+  constexpr int kParts = kGroup / kCols, kE = D / 16;
   const int x = blockIdx.x % kParts, hk = blockIdx.x / kParts % a.pool.Hkv, index = blockIdx.x / kParts / a.pool.Hkv;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const Columns col = find_columns(a, index);
   if (col.count <= x * kCols) return;
   Sight mine[kParts];
   TileList list;
-  if (!sights_of<kParts>(a, col, lane & 15, mine, list)) return;
+  if (!sights_of<kParts>(a, col, threadIdx.x & 15, mine, list)) return;
   const int ns = list.shares();
   if (ns <= 1) return;
-  for (int h = x * kCols + w; h < min(col.count, (x + 1) * kCols); h += kWaves) {
-    const int64_t at0 = (int64_t(index) * a.pool.Hkv + hk) * a.splits * kGroup + h;  // (share s: + s * kGroup)
-    const float* ml = a.part_ml + at0 * 2;
-    float M = -3.402823466e38f, L = 0.f;
-    for (int s = lane; s < ns; s += 64) M = fmaxf(M, ml[int64_t(s) * kGroup * 2]);
-    M = wave_max(M);
-    for (int s = lane; s < ns; s += 64) L = fmaf(ml[int64_t(s) * kGroup * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M), L);
-    L = wave_sum(L);
-    float o[D / 64] = {};
+  const int h = x * kCols + int(threadIdx.x >> 4), c = threadIdx.x & 15;
+  const bool is = h < col.count;
+  const int64_t at0 = (int64_t(index) * a.pool.Hkv + hk) * a.splits * kGroup + (is ? h : x * kCols);  // (share s: + s * kGroup)
+  const float* ml = a.part_ml + at0 * 2;
+  float M = -3.402823466e38f, L = 0.f;
+  for (int s = c; s < ns; s += 16) M = fmaxf(M, ml[int64_t(s) * kGroup * 2]);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  for (int s = c; s < ns; s += 16) L = fmaf(ml[int64_t(s) * kGroup * 2 + 1], __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M), L);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) L += __shfl_xor(L, o, 64);
+  f32x4 o[kE / 4] = {};
 #pragma unroll 4
-    for (int s = 0; s < ns; ++s) {
-      const float f = __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M);
+  for (int s = 0; s < ns; ++s) {
+    const float f = __builtin_amdgcn_exp2f(ml[int64_t(s) * kGroup * 2] - M);
 #pragma unroll
-      for (int y = 0; y < D / 64; ++y) o[y] = fmaf(a.part_o[(at0 + int64_t(s) * kGroup) * D + y * 64 + lane], f, o[y]);
-    }
-    uint16_t* out = out_row(a, col, hk, h);
-#pragma unroll
-    for (int y = 0; y < D / 64; ++y) out[y * 64 + lane] = Elem<uint16_t>::from_f32(L == 0.f ? 0.f : o[y] / L);
+    for (int y = 0; y < kE / 4; ++y) o[y] += *reinterpret_cast<const f32x4*>(a.part_o + (at0 + int64_t(s) * kGroup) * D + c * kE + y * 4) * f;
   }
+  if (!is) return;
+  uint16_t* out = static_cast<uint16_t*>(a.out.ptr) + column_at(a, a.out, col, hk, h) + c * kE;
+#pragma unroll
+  for (int y = 0; y < kE / 4; ++y) store_out4(out + y * 4, L == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[y] / L);
 }
 
 // Rows by pairs of tiles where a page holds whole pairs, and displacements, strides and alignment are as at_row and the loads of powers of two take them.
@@ -705,7 +736,9 @@ void launch_step4(AttendArgs& a, int batch, hipStream_t s) {
   if (a.splits == 1) return;
   a.joins = batch * a.Hq;
   const int64_t scores = a.pool.score ? int64_t((a.pad + kFinishEntries - 1) / kFinishEntries) * bh : 0;
-  step_finish<uint16_t, D, 16><<<dim3(unsigned(a.joins + scores)), kFinish, 0, s>>>(a, kLeast4);
+  const auto finish = a.G == 1 ? step_finish<uint16_t, D, 1> : a.G == 2 ? step_finish<uint16_t, D, 2> : a.G <= 4 ? step_finish<uint16_t, D, 4>
+                      : a.G <= 8 ? step_finish<uint16_t, D, 8> : step_finish<uint16_t, D, 16>;
+  finish<<<dim3(unsigned(a.joins + scores)), kFinish, 0, s>>>(a, kLeast4);
 }
 
 template <int D>
@@ -722,9 +755,14 @@ int64_t column_groups(const d2o_pages* p, int32_t n_tokens) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   return std::min(int64_t(n_tokens), int64_t(n_tokens) * G / kGroup + p->batch);
 }
+// Shares of a group's tiles, for at most `tiles` tiles each: three workgroups per CU, of which two are there at a time, and shares of 32 tiles.  (Sixteen sequences
+// of up to 8192 entries, 8 KV heads, 1 to 48 tokens: 91 us with two per CU, 73 with three, 80 with four or eight.)
+int attend_splits(int64_t heads, int64_t tiles) { return int(std::max<int64_t>(1, std::min<int64_t>(768 / heads, tiles / 32))); }
+// Tiles of a share, so that `splits` of them hold the longest sequence: shorter ones take fewer.
+int share_tiles(int64_t tiles, int splits) { return int(((tiles + splits - 1) / splits + kLeast4 - 1) / kLeast4 * kLeast4); }
 size_t attend_bytes(const d2o_pages* p, int32_t max_len, int32_t n_tokens, int* splits) {
   const int64_t heads = column_groups(p, n_tokens) * p->n_kv_heads;
-  *splits = step_splits(heads, most_tiles(p, max_len, 0, 0));
+  *splits = attend_splits(heads, most_tiles(p, max_len, 0, 0));
   const size_t rows = size_t(heads) * *splits * kGroup;
   return *splits > 1 ? round256(rows * p->head_dim * sizeof(float)) + round256(rows * 2 * sizeof(float)) : 0;
 }
@@ -735,14 +773,14 @@ int check_attend(const d2o_pages* p, PagePool* pool, int32_t n_tokens, int32_t m
   if (!p->cache_fp4) return D2O_ERR_UNSUPPORTED;
   if (n_tokens < 0 || max_len < 1) return D2O_ERR_INVALID_ARG;
   // products of tokens and heads that are formed in 32 bits, and the grid
-  if (int64_t(n_tokens) * p->n_q_heads > 0x3FFFFFFF || column_groups(p, n_tokens) * p->n_kv_heads > 0xFFFFF) return D2O_ERR_UNSUPPORTED;
+  if (int64_t(n_tokens) * p->n_q_heads > 0xFFFFFFF || column_groups(p, n_tokens) * p->n_kv_heads > 0xFFFFF) return D2O_ERR_UNSUPPORTED;
   return D2O_OK;
 }
 
 }  // namespace
 
 void launch_step4(StepArgs& args, int batch, int D, hipStream_t s) {
-  AttendArgs a{args, nullptr, 0, 0, 0};
+  AttendArgs a{args, nullptr, 0, 0, 0, 0};
   if (D == 64)
     launch_step4<64>(a, batch, s);
   else
@@ -789,9 +827,12 @@ extern "C" int d2o_pages_attend(const d2o_pages* pages, d2o_view q, int32_t n_to
   const int64_t heads = int64_t(a.groups) * pages->n_kv_heads;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = need ? a.part_o + round256(size_t(heads) * a.splits * kGroup * pages->head_dim * sizeof(float)) / sizeof(float) : nullptr;
-  a.splits = std::min(a.splits, step_splits(heads, most_tiles(pages, max_len, window, n_sink)));
+  const int64_t tiles = pages->pos || positions ? most_tiles(pages, max_len, 0, 0) : most_tiles(pages, max_len, window, n_sink + kGroup);
+  a.splits = std::min(a.splits, attend_splits(heads, tiles));
+  a.share = share_tiles(tiles, a.splits);
   a.Hq = pages->n_q_heads;
   a.G = pages->n_q_heads / pages->n_kv_heads;
+  a.over_g = uint32_t(0xFFFFFFFFu / uint32_t(a.G)) + 1;  // (G = 1 is not divided by)
   a.max_len = max_len;
   a.window = window;
   a.n_sink = n_sink;

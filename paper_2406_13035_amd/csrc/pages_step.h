@@ -13,6 +13,9 @@ constexpr int kWaves = 4;       // wavefronts of a workgroup
 constexpr int kTile = 16;       // entries of a tile: the rows of one matrix operand
 constexpr int kRowBcast = 0x150;  // lane i of each row of 16 lanes to all of the row (data-parallel primitive, + i)
 
+// (4-bit rows) a maximum that grew by less than 2^kSlack stays what weights are relative to.
+constexpr int kSlack = 8;
+
 struct StepArgs {
   PagePool pool;
   View q, kn, vn, out;
@@ -23,6 +26,7 @@ struct StepArgs {
   float* part_ml;  // [B * Hkv][splits][G][2] its softmax maximum and sum (outputs and sums: times 2^-TileList::bias)
   int32_t Hq, G, max_len, window, n_sink, pad, splits, joins;  // joins: workgroups of step_finish that join outputs
   int32_t pairs;  // 1: tiles are looked at in pairs, entries 32 i .. 32 i + 31
+  int32_t share;  // tiles of a workgroup at least (0: a sequence's tiles are spread over all shares)
 };
 
 // The tiles of a sequence that hold what a step sees: those of the first tokens, then those from the window's start.  (Where the
@@ -30,7 +34,7 @@ struct StepArgs {
 struct TileList {
   int n, sink_tiles, rest0, tiles, share;  // entries, tiles of the first tokens, first tile behind them, tiles in all, tiles per workgroup
   int64_t last;                            // the new token's position
-  int bias;                                // n < 2^bias
+  int bias;                                // n < 2^bias (weights may be as large as 2^kSlack: n < 2^(bias - kSlack))
   __device__ __forceinline__ TileList() {}
   __device__ __forceinline__ TileList(const StepArgs& a, int b, int least) {
     n = min(a.lens[b], a.max_len);
@@ -44,7 +48,7 @@ struct TileList {
   }
   // The tiles of the n entries (n > 0) for windows that start at entry `lo` or later.
   __device__ __forceinline__ void choose(const StepArgs& a, int64_t lo, int least) {
-    bias = 32 - __clz(n);
+    bias = 32 - __clz(n) + (a.pairs ? kSlack : 0);
     const int all = (n + kTile - 1) / kTile;
     sink_tiles = rest0 = 0;
     if (a.window != 0 && !a.pool.pos) {
@@ -57,7 +61,7 @@ struct TileList {
       rest0 = all - 1;
       tiles = 1;
     }
-    share = ((tiles + a.splits - 1) / a.splits + least - 1) / least * least;  // whole rounds of the wavefronts
+    share = max(((tiles + a.splits - 1) / a.splits + least - 1) / least * least, a.share);  // whole rounds of the wavefronts
   }
   __device__ __forceinline__ int slot(int t) const { return (t < sink_tiles ? t : rest0 + t - sink_tiles) * kTile; }
   __device__ __forceinline__ int shares() const { return tiles ? (tiles + share - 1) / share : 0; }

@@ -545,6 +545,7 @@ extern "C" int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new
   a.window = window;
   a.n_sink = n_sink;
   a.pairs = pages->cache_fp4;
+  a.share = 0;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (pages->cache_fp4)
     launch_step4(a, pages->batch, pages->head_dim, s);
