@@ -116,6 +116,12 @@ struct Row4 {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
+// a * b as a number of its own, never part of a multiply-add: large logits that are equal have to stay equal when a maximum is taken from them.
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // Where a pair of tiles lies, the same for all lanes.
 struct Pair {
   int s0[2];      // first entries
@@ -261,11 +267,14 @@ struct Share {
   }
 
   // Probabilities are formed as 2^-bias * p, so that no mean of values of any size overflows.  The step, whose logits and sums make scores, forms
-  // (s - maximum) - bias; otherwise the products start from -bias in their own units and one multiply-add is left, and the sums of P, as it enters
+  // (s - maximum) - bias; otherwise the products start from a number that stands for it in their own units and one multiply-add is left, and the sums of P, as it enters
   // the products, come from the matrix core too (P times ones).
   __device__ __forceinline__ void run(const bf16x8 (&q)[N][kSteps], float* lg) {
     const float scale2 = kLog2e / sqrtf(float(D));
-    const float bias = list.bias, start = STEP ? 0.f : -bias / scale2, slack = STEP ? float(kSlack) : kSlack / scale2;
+    const float bias = list.bias, slack = STEP ? float(kSlack) : kSlack / scale2;
+    // (a power of two, so that sums of products that are exact stay so)
+    const float offset = STEP ? 0.f : ldexpf(1.f, ilogbf(bias / scale2) + 1), start = -offset;
+    bool large = false;  // (not STEP) exponents beyond 2^20, where an exact product less a rounded one is no longer small
     const bool by_pos = a.window != 0 && a.pool.pos;
     const int n = list.n;
     f32x4 lm[N];   // (not STEP) sums of P: register i: column 4 g + i
@@ -364,7 +373,10 @@ struct Share {
         load_v(next);  // (behind the last pair that one again: a branch would have the registers copied, and so waited for)
       }
       if constexpr (!kAhead) powers();
-      if constexpr (STEP) s[0][0] *= scale2, s[0][1] *= scale2;
+      if constexpr (STEP) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0][i / 4][i % 4] = product(s[0][i / 4][i % 4], scale2);
+      }
       uint32_t seen[N];  // bit 4 i + r: column x of the lane's sees entry 4 g + r of tile i
 #pragma unroll
       for (int x = 0; x < N; ++x) seen[x] = 0xFFu;
@@ -409,13 +421,31 @@ struct Share {
         for (int x = 0; x < N; ++x) {
           mx[x] = max_rows(mx[x]);
           m[x] = mx[x];
-          const float to = STEP ? m[x] : fmaf(m[x], scale2, bias), f = __builtin_amdgcn_exp2f(ref[x] - to);
+          const float to = STEP ? m[x] : product(m[x], scale2) + product(offset, scale2), f = __builtin_amdgcn_exp2f(ref[x] - to);
           ref[x] = to;
           l[x] *= f;
           const f32x4 fh = {__shfl(f, 4 * g, 64), __shfl(f, 4 * g + 1, 64), __shfl(f, 4 * g + 2, 64), __shfl(f, 4 * g + 3, 64)};
 #pragma unroll
           for (int e = 0; e < E; ++e) om[x][e] *= fh;
           lm[x] *= fh;
+        }
+        if constexpr (!STEP) {
+          bool far = false;
+#pragma unroll
+          for (int x = 0; x < N; ++x) far |= fabsf(ref[x]) > 1048576.f && ref[x] > -1e37f;
+          large = __any(far);
+        }
+      }
+      float times = scale2, less[N];
+#pragma unroll
+      for (int x = 0; x < N; ++x) less[x] = -ref[x];
+      if (large) {
+        times = 1.f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          less[x] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[x][i / 4][i % 4] = (product(s[x][i / 4][i % 4], scale2) - product(m[x], scale2)) - product(offset, scale2);
         }
       }
 #pragma unroll
@@ -427,7 +457,7 @@ struct Share {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const float logit = s[x][i / 2][i % 2 * 2 + y];
-            p[y] = __builtin_amdgcn_exp2f(STEP ? (logit - ref[x]) - bias : fmaf(logit, scale2, -ref[x]));
+            p[y] = __builtin_amdgcn_exp2f(STEP ? (logit - ref[x]) - bias : fmaf(logit, times, less[x]));
             if constexpr (STEP) l[x] += p[y];
           }
           const bf16x2 h = __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2);

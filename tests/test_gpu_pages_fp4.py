@@ -343,3 +343,61 @@ def test_attend_with_entries_that_have_no_page():
     for page in (4, 16, 64):
         attend_case(128, 4, 2, page, [3 * page + 1, 2 * page], [page, 3], spoil=spoil)
 
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("total", [14, 18, 22, 30, 60, 100])
+def test_logits_of_any_size(d, total):
+    """Logits that are products of a power of two and a code, exact in fp32: tokens attend to the highest entry they see, or to those that
+    share its value, alone.  Heads in turn: of such logits, of their negatives, of all-zero ones and of small ones."""
+    n, m, page = 700, 90, 64
+    g = torch.Generator().manual_seed(total)
+    code = torch.randint(0, 8, (n,), generator=g)
+    k = torch.zeros((n, 2, d))
+    k[:, :, 0] = ref.GRID[code].float()[:, None]
+    k[:, :, 32] = 6.0 * torch.where(torch.rand(n, generator=g) < 0.5, 1.0, -1.0)[:, None]
+    k[:, :, 1] = 6.0  # (every block's power of two is one)
+    v = ref.rounded4(torch.randn((n, 2, d), generator=g).to(BF16)).to(BF16)
+    t = ref.make_pages4(1, 2, d, page, -(-n // page), 1, score=False, pos=False)
+    p, r = pages_ref.entries(t, 0, n)
+    for x, y in (("k", k), ("v", v)):
+        t[x][p, :, r], t[x + "_exp"][p, :, r] = ref.encode4(y)
+    q = torch.zeros((m, 8, d))
+    for h, f in enumerate((2.0 ** total, -2.0 ** total, 0.0, 0.25, 2.0 ** total, -2.0 ** total, 0.0, 0.25)):
+        q[:, h, 0] = f
+        q[:, h, 32] = f / 2 ** 7 if h % 4 == 3 else 0.0
+    q = q.to(BF16)
+    out = torch.zeros((m, 8, d), dtype=BF16)
+    want, tol = ref.attend_ref(ref.values(t), q, [0, m], [n], None, 0, 0, 1 << 20, out)
+    # ties and gaps are exact, so the bound's share of the logits' magnitude does not apply to the large ones: their weights are equal or zero
+    exact = tol.clone()
+    for h in (0, 1, 2, 4, 5, 6):
+        exact[:, h] = (2.0 ** -8 * want.abs() + (2.0 ** -15 + n * 2.0 ** -23) * 6.0)[:, h]
+    gt = on_gpu(t)
+    pages = pages_of(gt, 8)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    og = out.cuda()
+    pages.d2o_pages_attend(q.cuda(), i32([0, m]), i32([n]), og)
+    within(og, want, exact)
+    one = torch.zeros((1, 8, d), dtype=BF16, device="cuda:0")
+    pages.d2o_pages_attend(q[-1:].cuda(), i32([0, 1]), i32([n]), one)
+    within(one, want[-1:], exact[-1:])
+    pages.d2o_pages_step(q[-1:].cuda(), None, None, i32([n]), one)
+    within(one, want[-1:], exact[-1:])
+
+
+def test_large_logits_beside_large_values():
+    """Means of values near the largest number where all logits are equal, and large: no sum overflows."""
+    n, m, d, page = 5000, 20, 128, 64
+    t = ref.make_pages4(1, 1, d, page, -(-n // page), 1, score=False, pos=False)
+    t["k"].fill_(0x22), t["k_exp"].zero_()              # all ones
+    t["v"].fill_(0x77), t["v_exp"].fill_(125)           # 6 * 2^125
+    gt = on_gpu(t)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    for size in (0.0, 2.0 ** 10, 2.0 ** 22, -2.0 ** 40, 2.0 ** 100):
+        q = torch.full((m, 1, d), size / d, dtype=BF16, device="cuda:0")
+        out = torch.zeros_like(q)
+        pages_of(gt, 1).d2o_pages_attend(q, i32([0, m]), i32([n]), out)
+        assert bool((out.float() == 6.0 * 2.0 ** 125).all()), size
+        one = torch.zeros((1, 1, d), dtype=BF16, device="cuda:0")
+        pages_of(gt, 1).d2o_pages_step(q[:1], None, None, i32([n]), one)
+        assert bool((one.float() == 6.0 * 2.0 ** 125).all()), size
