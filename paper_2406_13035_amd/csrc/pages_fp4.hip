@@ -111,10 +111,11 @@ struct Row4 {
   static constexpr int kSteps = D / 32, kE = D / 16;
   typedef std::conditional_t<D == 128, u32x4, u32x2> KReg;       // also the powers of two of four rows
   typedef std::conditional_t<D == 128, uint32_t, uint16_t> VReg;
-  static __device__ __forceinline__ uint32_t word(const KReg& k, int i) { return k[i]; }
 };
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+constexpr float kLowest = -3.402823466e38f;  // a maximum before the first logit
 
 // a * b as a number of its own, never part of a multiply-add: large logits that are equal have to stay equal when a maximum is taken from them.
 __device__ __forceinline__ float product(float a, float b) {
@@ -281,7 +282,7 @@ struct Share {
     float ref[N];  // what P is relative to, as an exponent
 #pragma unroll
     for (int x = 0; x < N; ++x) {
-      ref[x] = m[x] = -3.402823466e38f;
+      ref[x] = m[x] = kLowest;
       l[x] = 0.f;
       lm[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -432,7 +433,7 @@ struct Share {
         if constexpr (!STEP) {
           bool far = false;
 #pragma unroll
-          for (int x = 0; x < N; ++x) far |= fabsf(ref[x]) > 1048576.f && ref[x] > -1e37f;
+          for (int x = 0; x < N; ++x) far |= fabsf(ref[x]) > 1048576.f && m[x] != kLowest;
           large = __any(far);
         }
       }
@@ -730,7 +731,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join4(AttendArgs a) {
   const bool is = h < col.count;
   const int64_t at0 = (int64_t(index) * a.pool.Hkv + hk) * a.splits * kGroup + (is ? h : x * kCols);  // (share s: + s * kGroup)
   const float* ml = a.part_ml + at0 * 2;
-  float M = -3.402823466e38f, L = 0.f;
+  float M = kLowest, L = 0.f;
   for (int s = c; s < ns; s += 16) M = fmaxf(M, ml[int64_t(s) * kGroup * 2]);
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, 64));

@@ -99,7 +99,8 @@ __global__ __launch_bounds__(256) void norm_rope(NormArgs a) {
 #pragma unroll
       for (int o = 1; o < kLanes; o <<= 1) ss += __shfl_xor(ss, o, 64);
       float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-      if (__any(!(ss < 1e37f))) {  // squares that left 32 bits: once more in 64, before the factor as a float loses bits
+      const bool far = !(ss < 1e37f);
+      if (__any(far)) {  // squares that left 32 bits: such rows once more in 64, before the factor as a float loses bits
         double s = 0.0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s = fma(double(y[i]), double(y[i]), s);
@@ -107,8 +108,8 @@ __global__ __launch_bounds__(256) void norm_rope(NormArgs a) {
         for (int o = 1; o < kLanes; o <<= 1) s += __shfl_xor(s, o, 64);
         const double rd = 1.0 / sqrt(s * (1.0 / D) + double(a.eps));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = float(double(y[i]) * rd);
-        r = 1.f;
+        for (int i = 0; i < 16; ++i) y[i] = far ? float(double(y[i]) * rd) : y[i];
+        r = far ? 1.f : r;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = y[i] * r * (which ? wt[1][i] : wt[0][i]);

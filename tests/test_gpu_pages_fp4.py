@@ -393,7 +393,7 @@ def test_large_logits_beside_large_values():
     t["v"].fill_(0x77), t["v_exp"].fill_(125)           # 6 * 2^125
     gt = on_gpu(t)
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
-    for size in (0.0, 2.0 ** 10, 2.0 ** 22, -2.0 ** 40, 2.0 ** 100):
+    for size in (0.0, 2.0 ** 10, 2.0 ** 22, -2.0 ** 40, 2.0 ** 100, -2.0 ** 126):
         q = torch.full((m, 1, d), size / d, dtype=BF16, device="cuda:0")
         out = torch.zeros_like(q)
         pages_of(gt, 1).d2o_pages_attend(q, i32([0, m]), i32([n]), out)

@@ -131,3 +131,15 @@ def test_rows_with_gaps_and_what_lies_between_them():
     binding.d2o_qk_norm_rope(wide.cuda()[..., 8:72], None, Q_out=out[..., 16:80])
     check(out[..., 16:80], Q, None, 1e-6, 64, torch.arange(11).expand(2, 11), 10000.0)
     assert bool((out[..., :16] == 5).all()) and bool((out[..., 80:] == 5).all())
+
+
+def test_a_row_does_not_depend_on_those_beside_it():
+    """Rows beside infinities, NaN and numbers near the largest are, bit for bit, what they are alone."""
+    (Q, K), (wq, wk) = inputs(BF16, 1, 2, 1, 64, 128)
+    plain, _ = binding.d2o_qk_norm_rope(Q.cuda(), None, wq.cuda())
+    spoilt = Q.clone()
+    spoilt[0, :, 3::4] *= 2.0 ** 120
+    spoilt[0, 0, 7, 5], spoilt[0, 1, 11, 9] = float("inf"), float("nan")
+    got, _ = binding.d2o_qk_norm_rope(spoilt.cuda(), None, wq.cuda())
+    keep = [i for i in range(64) if i % 4 != 3]
+    assert torch.equal(got[:, :, keep], plain[:, :, keep])
