@@ -206,7 +206,7 @@ def test_fill(d, n, budget, recent, n_sink, page):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("page", [1, 64])
 @pytest.mark.parametrize("lens,budget,recent,n_sink", [([9, 8], 8, 2, 1), ([300, 100], 77, 20, 4), ([2304, 2100], 1100, 300, 4),
-                                                       ([18000, 17000], 16990, 100, 0)], ids=str)
+                                                       ([18000, 17000], 16990, 100, 0), ([20000, 19995], 19990, 100, 2)], ids=str)
 def test_evict(d, page, lens, budget, recent, n_sink):
     if page == 1 and lens[0] > 10000:
         lens = [n // 50 for n in lens]
@@ -401,3 +401,53 @@ def test_large_logits_beside_large_values():
         one = torch.zeros((1, 1, d), dtype=BF16, device="cuda:0")
         pages_of(gt, 1).d2o_pages_step(q[:1], None, None, i32([n]), one)
         assert bool((one.float() == 6.0 * 2.0 ** 125).all()), size
+
+
+def placed(t, how):
+    """The same tables at odd places: exponents from an address that is a multiple of 4 alone, or rows further apart than 2^21 bytes."""
+    out = on_gpu(t)
+    if how == "exponents":
+        for x in ("k_exp", "v_exp"):
+            room = torch.full((t[x].numel() + 16,), 99, dtype=torch.int8, device="cuda:0")
+            out[x] = room[4:4 + t[x].numel()].view(t[x].shape).copy_(t[x])
+            assert out[x].data_ptr() % 16 == 4
+        return out
+    pages, heads, page, wide = t["k"].shape
+    for x in ("k", "v"):
+        step = (1 << 21) + 64
+        room = torch.zeros(pages * page * step, dtype=torch.uint8, device="cuda:0")
+        out[x] = torch.as_strided(room, t[x].shape, (page * step, wide, step, 1))
+        out[x].copy_(t[x])
+    return out
+
+
+@pytest.mark.parametrize("how", ["exponents", "rows"])
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 64), (128, 16)])
+def test_odd_addresses_and_wide_strides(d, page, how):
+    lens, news = [3 * page + 5, page], [page + 3, 1]
+    t = ref.make_pages4(2, 2, d, page, 4, 5, score=True, pos=False, spare=0)
+    g = torch.Generator().manual_seed(2)
+    q = torch.randn((sum(news), 4, d), generator=g).to(BF16)
+    first = [0, news[0], sum(news)]
+    out = torch.zeros(q.shape, dtype=BF16)
+    want, tol = ref.attend_ref(ref.values(t), q, first, lens, None, 0, 0, 4 * page, out)
+    gt = placed(t, how)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    pages, og = pages_of(gt, 4), out.cuda()
+    pages.d2o_pages_attend(q.cuda(), i32(first), i32(lens), og)
+    within(og, want, tol)
+    bits_same(gt, t)
+    # a step that stores its tokens, and rows put and read back
+    kn, vn = (torch.randn((2, 2, d), generator=g).to(BF16) for _ in range(2))
+    n = torch.tensor([x + 1 for x in lens], dtype=torch.int32)
+    want, tol, new, add, add_tol = ref.step_ref4(t, q[:2], kn, vn, n, None, 0, 0, 4 * page)
+    o = torch.zeros((2, 4, d), dtype=BF16, device="cuda:0")
+    pages.d2o_pages_step(q[:2].cuda(), kn.cuda(), vn.cuda(), n.cuda(), o)
+    within(o, want, tol)
+    same_values(gt, new)
+    slots = torch.tensor([5, page + 1, -1], device="cuda:0")
+    K, V = (torch.randn((3, 2, d), generator=g).to(BF16).cuda() for _ in range(2))
+    pages.d2o_pages_put(K, V, slots)
+    Ko, Vo = torch.zeros_like(K), torch.zeros_like(V)
+    pages.d2o_pages_get(slots, Ko, Vo)
+    assert torch.equal(Ko[:2].cpu().double(), ref.rounded4(K[:2].cpu())) and torch.equal(Vo[:2].cpu().double(), ref.rounded4(V[:2].cpu()))
