@@ -1,5 +1,6 @@
 // Attention over a cache in pages whose rows are held in 4 bits: one query token per sequence (d2o_pages_step) and several
 // (d2o_pages_attend).
+#include "pages_columns.h"
 #include "pages_step.h"
 
 namespace d2o {
@@ -61,7 +62,7 @@ __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) 
         found[2] = min(pairs - base, kGroup);
         found[3] = start;
         found[4] = tokens;
-        found[5] = min(len, a.max_len);
+        found[5] = entries_of(len, a.max_len);
         break;
       }
       at += n;
@@ -87,17 +88,16 @@ __device__ __forceinline__ int row_min(int v) {
 // The sights of columns c, c + 16, .. (N of them), and the tiles that any of the columns sees; false where there are none.
 template <int N>
 __device__ __forceinline__ bool sights_of(const AttendArgs& a, const Columns& col, int c, Sight (&mine)[N], TileList& list) {
-  const int before = col.len - col.tokens;
   int lo = INT32_MAX;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int at = i * kCols + c, token = a.token_of(col.base + at);
     const bool is = at < col.count;
-    mine[i].last = is ? max(before + token, -1) : -1;
+    mine[i].last = is ? last_seen(col.len, col.tokens, token) : -1;
     mine[i].lo = window_start(a.window != 0 && a.positions && is ? a.positions[col.token0 + token] : mine[i].last, a.window);
     lo = min(lo, is ? mine[i].lo : INT32_MAX);
   }
-  list.n = max(before + a.token_of(col.base + col.count - 1) + 1, 0);
+  list.n = last_seen(col.len, col.tokens, a.token_of(col.base + col.count - 1)) + 1;
   list.last = 0;
   if (list.n == 0) return false;
   list.choose(a, a.window == 0 ? 0 : __builtin_amdgcn_readfirstlane(row_min(lo)), kLeast4);
