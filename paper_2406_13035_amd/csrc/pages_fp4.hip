@@ -116,6 +116,7 @@ struct Row4 {
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 constexpr float kLowest = -3.402823466e38f;  // a maximum before the first logit
+constexpr float kFar = 1048576.f;            // exponents whose rounding is no longer small (2^-4)
 
 // a * b as a number of its own, never part of a multiply-add: large logits that are equal have to stay equal when a maximum is taken from them.
 __device__ __forceinline__ float product(float a, float b) {
@@ -268,13 +269,11 @@ struct Share {
   }
 
   // Probabilities are formed as 2^-bias * p, so that no mean of values of any size overflows.  The step, whose logits and sums make scores, forms
-  // (s - maximum) - bias; otherwise the products start from a number that stands for it in their own units and one multiply-add is left, and the sums of P, as it enters
+  // (s - maximum) - bias; otherwise one multiply-add is left, from a maximum that is rounded so that it stays exact with bias added, and the sums of P, as it enters
   // the products, come from the matrix core too (P times ones).
   __device__ __forceinline__ void run(const bf16x8 (&q)[N][kSteps], float* lg) {
     const float scale2 = kLog2e / sqrtf(float(D));
     const float bias = list.bias, slack = STEP ? float(kSlack) : kSlack / scale2;
-    // (a power of two, so that sums of products that are exact stay so)
-    const float offset = STEP ? 0.f : ldexpf(1.f, ilogbf(bias / scale2) + 1), start = -offset;
     bool large = false;  // (not STEP) exponents beyond 2^20, where an exact product less a rounded one is no longer small
     const bool by_pos = a.window != 0 && a.pool.pos;
     const int n = list.n;
@@ -341,7 +340,7 @@ struct Share {
       const Pair after = kAhead ? pair_at(t + 2 * kLeast4) : now;
       f32x4 s[N][2];
 #pragma unroll
-      for (int x = 0; x < N; ++x) s[x][0] = s[x][1] = f32x4{start, start, start, start};
+      for (int x = 0; x < N; ++x) s[x][0] = s[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
       bf16x8 vop[E / 2][2];
       if constexpr (kAhead) {
 #pragma unroll
@@ -422,7 +421,12 @@ struct Share {
         for (int x = 0; x < N; ++x) {
           mx[x] = max_rows(mx[x]);
           m[x] = mx[x];
-          const float to = STEP ? m[x] : product(m[x], scale2) + product(offset, scale2), f = __builtin_amdgcn_exp2f(ref[x] - to);
+          float to = m[x];
+          if constexpr (!STEP) {  // up to 2^20 with as many bits as the sum with bias has; beyond, where each logit is multiplied and rounded first, as those are
+            to = product(m[x], scale2);
+            to = fabsf(to) > kFar ? to : (to + bias) - bias;
+          }
+          const float f = __builtin_amdgcn_exp2f(ref[x] - to);
           ref[x] = to;
           l[x] *= f;
           const f32x4 fh = {__shfl(f, 4 * g, 64), __shfl(f, 4 * g + 1, 64), __shfl(f, 4 * g + 2, 64), __shfl(f, 4 * g + 3, 64)};
@@ -433,20 +437,20 @@ struct Share {
         if constexpr (!STEP) {
           bool far = false;
 #pragma unroll
-          for (int x = 0; x < N; ++x) far |= fabsf(ref[x]) > 1048576.f && m[x] != kLowest;
+          for (int x = 0; x < N; ++x) far |= fabsf(ref[x]) > kFar && m[x] != kLowest;
           large = __any(far);
         }
       }
       float times = scale2, less[N];
 #pragma unroll
-      for (int x = 0; x < N; ++x) less[x] = -ref[x];
+      for (int x = 0; x < N; ++x) less[x] = -(ref[x] + bias);
       if (large) {
         times = 1.f;
 #pragma unroll
         for (int x = 0; x < N; ++x) {
           less[x] = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[x][i / 4][i % 4] = (product(s[x][i / 4][i % 4], scale2) - product(m[x], scale2)) - product(offset, scale2);
+          for (int i = 0; i < 8; ++i) s[x][i / 4][i % 4] = (product(s[x][i / 4][i % 4], scale2) - ref[x]) - bias;
         }
       }
 #pragma unroll
