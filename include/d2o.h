@@ -400,8 +400,8 @@ int d2o_pages_fill(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n, co
  * lens counts the entries there are).  max_len: host bound of every lens[b], at most max_pages * page_size
  * (a sequence that claims more is cut to it).  lens[b] <= 0: nothing is stored, out rows are zero; so are rows that see no entry (or only
  * logits of minus infinity).  Values may be as large as their type allows; a weight below 2^-126 times twice the
- * entries of the largest may count as zero, and means end at 2^-149 times twice the entries.  4-bit rows: a weight holds 16 bits (8 where it is below 2^-118
- * times 512 times the entries of the largest), and 512 times the entries stand in the place of twice.
+ * entries of the largest may count as zero, and means end at 2^-149 times twice the entries.  4-bit rows: a weight holds 24 bits (fewer where it is below
+ * 2^-102 times 512 times the entries of the largest), and 512 times the entries stand in the place of twice.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_len beyond the page table, workspace too small), HIP. */
 int d2o_pages_step(const d2o_pages* pages, d2o_view q, d2o_view k_new, d2o_view v_new, const int32_t* lens,
                    const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,
@@ -463,8 +463,8 @@ int d2o_pages_get(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_toke
  * between tokens, stride_h between heads, stride_b unused); rows first[b] .. first[b + 1] - 1 (device [B + 1], nowhere falling, taken within [0, n_tokens]) are the last tokens of
  * sequence b, the newest of them its entry lens[b] - 1.  Each sees the entries up to its own that have a position > its own - window or < n_sink (window = 0: all);
  * positions: device [n_tokens], NULL: the entry's number.  lens and max_len as for d2o_pages_step (a sequence that claims more is cut to it); tokens without an entry, or
- * that see none, get zeros.  Rows of out that belong to no sequence are left as they were.  Scores are neither read nor added to.  Weights
- * are as for a step over 4-bit rows, sums hold 24 bits; NaN of a row reaches the tokens that see it and no others; out may be q itself.
+ * that see none, get zeros.  Rows of out that belong to no sequence are left as they were.  Scores are neither read nor added to.  Weights end
+ * as those of a step over 4-bit rows and hold 16 bits (8 where they are below 2^-118 times 512 times the entries of the largest), sums 24; NaN of a row reaches the tokens that see it and no others; out may be q itself.
  * Errors: INVALID_ARG, UNSUPPORTED (rows that are not of 4 bits; too many tokens for a launch), CAPACITY (max_len beyond the page table; workspace smaller than
  * d2o_pages_attend_workspace_bytes says, which grows with n_tokens up to a bound and falls again; where it says 0, NULL will do), HIP. */
 int d2o_pages_attend_workspace_bytes(const d2o_pages* pages, int32_t n_tokens, int32_t max_len, size_t* bytes);

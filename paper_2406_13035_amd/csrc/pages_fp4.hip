@@ -72,6 +72,14 @@ __device__ __forceinline__ Columns find_columns(const AttendArgs& a, int index) 
   return {scalar(0), scalar(1), scalar(2), scalar(3), scalar(4), scalar(5)};
 }
 
+// Heads of a step's group that have room in the sixteen columns PARTS times, and the head of column c (kCols: none).
+template <int PARTS>
+constexpr int kPart = kCols / PARTS;
+template <int PARTS>
+__device__ __forceinline__ int head_of(int c) {
+  return c < PARTS * kPart<PARTS> ? c % kPart<PARTS> : kCols;
+}
+
 // What a column sees: entries up to `last`, of these the ones with a position from `lo` on or below n_sink.
 struct Sight {
   int last;  // -1: nothing
@@ -139,9 +147,14 @@ enum Finds { ROWS, TILES, PAIRS };
 // entries 4 g .. 4 g + 3 of a tile.  Of two tiles these are eight entries, which is what the lane has to hold of P as the left operand of P V (16 x 16 x 32): P goes from registers to
 // the matrix core with no exchange.  The right operand wants eight entries of one element of V: a lane converts the D / 16 elements it has of each of the eight rows
 // to bf16 (exact), two elements of one row at a time, and swaps halves between rows: a conversion and a permutation for two values, once for all N groups.
-// P as two bf16 terms, which hold 16 bits: a weight is off by 2^-16 of itself at most.  Codes are always finite and powers of two may stand for NaN: where
+// P goes in as bf16 terms.  The step takes three, which hold all 24 bits: a group of up to five heads stands in the sixteen columns three times, each time for one
+// term of the same P, so that one product does for all three and the join adds the parts up (16 x 8192 entries, 8 KV heads of 4: 32 us as with two terms; three products 34);
+// one of up to eight twice, for two products (4 KV heads of 8: 23.8 us, with scores 29.8; three products 24.4 and 33.6; two terms 22.9 and 29.0); larger ones take three
+// products (2 KV heads of 16: 18.4 us, with scores 29.2; two terms 17.8 and 26.6).  Attention of several tokens, whose columns are all different, takes two, which hold
+// 16 bits: a weight is off by 2^-16 of itself at most (three: 1587 -> 1920 us for 2048 tokens on 32768, and bf16 outputs no closer to those of 64 bits in four digits).
+// Codes are always finite and powers of two may stand for NaN: where
 // columns see different entries, NaN is left out of the product, in which 0 * NaN would reach columns that do not see it, and added to those that do.
-template <int D, Finds F, bool STEP, int N>
+template <int D, Finds F, bool STEP, int N, int PARTS>
 struct Share {
   typedef Row4<D> R;
   static constexpr int E = R::kE, kExps = D / kBlock4, kSteps = R::kSteps;
@@ -455,7 +468,7 @@ struct Share {
       }
 #pragma unroll
       for (int x = 0; x < N; ++x) {
-        u32x4 hi2, lo2;
+        u32x4 hi2, lo2, third2;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float p[2];
@@ -465,15 +478,25 @@ struct Share {
             p[y] = __builtin_amdgcn_exp2f(STEP ? (logit - ref[x]) - bias : fmaf(logit, times, less[x]));
             if constexpr (STEP) l[x] += p[y];
           }
-          const bf16x2 h = __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2);
-          // p - h in one instruction each.  (Minus zero beside minus one: the pair 0, -1.0 in this order would be written as the constant -1.0, which
-          // the instruction reads as a float's bits.)
-          const f32x2 rest = {__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, 0x8000BF80u), p[0], false),
-                              __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, 0xBF808000u), p[1], false)};
+          // x - h in one instruction each (x itself in the columns that have come to their term).  (Minus zero beside minus one: the pair 0, -1.0 in this
+          // order would be written as the constant -1.0, which the instruction reads as a float's bits.)
+          auto less_term = [&](const f32x2& x, const bf16x2& h, bool is) __attribute__((always_inline)) {
+            const uint32_t one0 = is ? 0x8000BF80u : 0x80008000u, one1 = is ? 0xBF808000u : 0x80008000u;
+            return f32x2{__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, one0), x[0], false),
+                         __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, one1), x[1], false)};
+          };
+          const f32x2 all24 = {p[0], p[1]};
+          const bf16x2 h = __builtin_convertvector(all24, bf16x2);
+          const f32x2 rest = less_term(all24, h, PARTS == 1 || c >= kPart<PARTS>);
+          const bf16x2 l = __builtin_convertvector(rest, bf16x2);
           hi2[i] = __builtin_bit_cast(uint32_t, h);
-          lo2[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+          lo2[i] = __builtin_bit_cast(uint32_t, l);
+          if constexpr (STEP) {
+            third2[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(less_term(rest, l, PARTS < 3 || c >= 2 * kPart<PARTS>), bf16x2));
+            if (PARTS == 2) third2[i] = c >= kPart<PARTS> ? third2[i] : 0u;
+          }
         }
-        const bf16x8 hi = __builtin_bit_cast(bf16x8, hi2), lo = __builtin_bit_cast(bf16x8, lo2);
+        const bf16x8 hi = __builtin_bit_cast(bf16x8, hi2), lo = __builtin_bit_cast(bf16x8, lo2), third = __builtin_bit_cast(bf16x8, third2);
         if constexpr (kAhead) {
 #pragma unroll
           for (int e = 0; e < E; ++e) om[x][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, vop[e / 2][e % 2], om[x][e], 0, 0, 0);
@@ -488,11 +511,13 @@ struct Share {
           for (int y = 0; y < E / 2; ++y) {
             bf16x8 two[2];
             convert_v(y, two, ve);
+            auto add = [&](const bf16x8& term) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              om[x][2 * y + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, two[i], om[x][2 * y + i], 0, 0, 0);
-              om[x][2 * y + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, two[i], om[x][2 * y + i], 0, 0, 0);
-            }
+              for (int i = 0; i < 2; ++i) om[x][2 * y + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(term, two[i], om[x][2 * y + i], 0, 0, 0);
+            };
+            add(third);
+            if constexpr (PARTS < 3) add(lo);
+            if constexpr (PARTS < 2) add(hi);
           }
         }
       }
@@ -567,8 +592,9 @@ __device__ __forceinline__ int64_t column_at(const AttendArgs& a, const View& v,
   return int64_t(col.token0 + token) * v.sn + int64_t(hk * a.G + r - token * a.G) * v.sh;
 }
 
+
 // A workgroup's share: its columns in N groups of 16.  `part`: which partial result.
-template <int D, Finds F, bool STEP, int N>
+template <int D, Finds F, bool STEP, int N, int PARTS>
 __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns& col, const TileList& list, const Sight (&mine)[N], int hk, int share,
                                              int part, AttendShared<D>& sh) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4, b = col.b;
@@ -602,9 +628,10 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
 #pragma unroll
   for (int x = 0; x < N; ++x) {
     const uint16_t* row = nullptr;
-    if (x * kCols + c < col.count) {
+    const int head = head_of<PARTS>(c);  // (of the step)
+    if (x * kCols + head < col.count) {
       if constexpr (STEP)
-        row = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + (hk * a.G + c) * a.q.sh;
+        row = static_cast<const uint16_t*>(a.q.ptr) + b * a.q.sb + (hk * a.G + head) * a.q.sh;
       else
         row = static_cast<const uint16_t*>(a.q.ptr) + column_at(a, a.q, col, hk, x * kCols + c);
     }
@@ -613,7 +640,7 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
       q[x][i] = row ? *reinterpret_cast<const bf16x8*>(row + g * (D / 4) + i * 8) : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   }
   float* lg = STEP && a.pool.score ? a.logits + (int64_t(b) * a.Hq + hk * a.G + c) * a.pad : nullptr;
-  Share<D, F, STEP, N> work{a, col, list, hk, t0, t1, mine, w, lane, c, g, all_last, all_lo};
+  Share<D, F, STEP, N, PARTS> work{a, col, list, hk, t0, t1, mine, w, lane, c, g, all_last, all_lo};
   work.run(q, lg);
   const bool single = list.shares() == 1;
   // join the wavefronts, 16 columns at a time
@@ -658,7 +685,12 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
     for (int h = tid / (D / 4); h < cols; h += 64 * kWaves / (D / 4)) {
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int y = 0; y < kWaves; ++y) o += *reinterpret_cast<const f32x4*>(&sh.o[y][h][at]) * sh.f[y][h];
+      for (int y = 0; y < kWaves; ++y) {
+        f32x4 one = *reinterpret_cast<const f32x4*>(&sh.o[y][h][at]);
+#pragma unroll
+        for (int i = 1; i < PARTS; ++i) one += *reinterpret_cast<const f32x4*>(&sh.o[y][h + i * kPart<PARTS>][at]);
+        o += one * sh.f[y][h];
+      }
       if (single) {
         const float L = sh.sum[h];
         o = L == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / L;
@@ -681,7 +713,7 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
 
 // The step: a workgroup per (share, sequence and KV head), whose columns are the group's query heads.  8 heads x 131072 entries: 33 us, 4.3 TB/s, of which 24 are
 // the instructions that conversions and products take to issue.
-template <int D, Finds F>
+template <int D, Finds F, int PARTS>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void step_part4(AttendArgs a) {
   __shared__ AttendShared<D> sh;
   const int b = blockIdx.y / a.pool.Hkv, hk = blockIdx.y % a.pool.Hkv;
@@ -691,8 +723,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
       for (int i = threadIdx.x; i < a.G * D; i += 64 * kWaves) store_out<uint16_t>(a, b, hk * a.G + i / D, i % D, 0.f);
     return;
   }
-  const Sight mine[1] = {{int(threadIdx.x & 15) < a.G ? list.n - 1 : -1, window_start(list.last, a.window)}};
-  attend_share<D, F, true, 1>(a, Columns{b, 0, a.G, 0, 0, 0}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
+  const int c = threadIdx.x & 15;
+  const Sight mine[1] = {{head_of<PARTS>(c) < a.G ? list.n - 1 : -1, window_start(list.last, a.window)}};
+  attend_share<D, F, true, 1, PARTS>(a, Columns{b, 0, a.G, 0, 0, 0}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
 }
 
 // Several tokens per sequence: a workgroup per (group of columns, KV head, share).  2048 tokens on 32768 entries, 32 heads on 8: 1.55-1.6 ms, 0.68 PFLOP/s, three executed products
@@ -710,7 +743,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     Sight mine[N];
     TileList list;
     if (sights_of<N>(a, col, threadIdx.x & 15, mine, list)) {
-      attend_share<D, F, false, N>(a, col, list, mine, hk, share, part, sh);
+      attend_share<D, F, false, N, 1>(a, col, list, mine, hk, share, part, sh);
     } else if (share == 0) {
       for (int i = threadIdx.x; i < col.count * D; i += 64 * kWaves) static_cast<uint16_t*>(a.out.ptr)[column_at(a, a.out, col, hk, i / D) + i % D] = 0;
     }
@@ -764,11 +797,15 @@ Finds finds_of(const PagePool& p) {
   return !scalar || p.shift < 4 ? ROWS : p.shift == 4 ? TILES : PAIRS;
 }
 
+template <int D, int PARTS>
+auto step_kernel(Finds f) {
+  return f == PAIRS ? step_part4<D, PAIRS, PARTS> : f == TILES ? step_part4<D, TILES, PARTS> : step_part4<D, ROWS, PARTS>;
+}
 template <int D>
 void launch_step4(AttendArgs& a, int batch, hipStream_t s) {
   const int bh = batch * a.pool.Hkv;
   const Finds f = finds_of(a.pool);
-  const auto part = f == PAIRS ? step_part4<D, PAIRS> : f == TILES ? step_part4<D, TILES> : step_part4<D, ROWS>;
+  const auto part = a.G <= kPart<3> ? step_kernel<D, 3>(f) : a.G <= kPart<2> ? step_kernel<D, 2>(f) : step_kernel<D, 1>(f);
   part<<<dim3(a.splits, bh), 64 * kWaves, 0, s>>>(a);
   if (a.splits == 1) return;
   a.joins = batch * a.Hq;
