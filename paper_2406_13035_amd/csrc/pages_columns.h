@@ -15,4 +15,10 @@ constexpr int32_t last_seen(int32_t entries, int32_t tokens, int32_t token) {
   return last > -1 ? last : -1;
 }
 
+// Tiles of `tile` entries that a window and the first n_sink entries show of max_len entries at most, to `columns` neighbouring tokens.
+constexpr int64_t shown_tiles(int32_t max_len, int32_t window, int32_t n_sink, int32_t columns, int32_t tile) {
+  const int64_t all = (int64_t(max_len) + tile - 1) / tile, shown = (int64_t(window) + n_sink + columns) / tile + 3;
+  return shown < all ? shown : all;
+}
+
 }  // namespace d2o

@@ -1,6 +1,5 @@
 // Attention over a cache in pages whose rows are held in 4 bits: one query token per sequence (d2o_pages_step) and several
 // (d2o_pages_attend).
-#include "pages_columns.h"
 #include "pages_step.h"
 
 namespace d2o {
@@ -901,7 +900,7 @@ extern "C" int d2o_pages_attend(const d2o_pages* pages, d2o_view q, int32_t n_to
   const int64_t heads = int64_t(a.groups) * pages->n_kv_heads;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = need ? a.part_o + round256(size_t(heads) * a.splits * kGroup * pages->head_dim * sizeof(float)) / sizeof(float) : nullptr;
-  const int64_t tiles = pages->pos || positions ? most_tiles(pages, max_len, 0, 0) : most_tiles(pages, max_len, window, n_sink + kGroup);
+  const int64_t tiles = pages->pos || positions ? most_tiles(pages, max_len, 0, 0) : most_tiles(pages, max_len, window, n_sink, kGroup);
   a.splits = std::min(a.splits, attend_splits(heads, tiles));
   a.share = share_tiles(tiles, a.splits);
   a.Hq = pages->n_q_heads;

@@ -5,6 +5,7 @@
 
 #include "fp4.h"
 #include "pages.h"
+#include "pages_columns.h"
 
 namespace d2o {
 
@@ -240,11 +241,10 @@ int step_splits(int64_t bh, int64_t tiles) {
   const int64_t large = std::min<int64_t>(1024 / bh, tiles / 64), small = std::min<int64_t>(512 / bh, tiles / (2 * kWaves));
   return int(std::max<int64_t>(1, std::max(large, small)));
 }
-// Tiles that a sequence of max_len entries shows at most.
-int64_t most_tiles(const d2o_pages* p, int32_t max_len, int32_t window, int32_t n_sink) {
-  const int64_t all = (int64_t(max_len) + kTile - 1) / kTile;
-  if (window == 0 || p->pos) return all;
-  return std::min(all, (int64_t(window) + n_sink) / kTile + 3);
+// Tiles that a sequence of max_len entries shows at most, to `columns` neighbouring tokens.
+int64_t most_tiles(const d2o_pages* p, int32_t max_len, int32_t window, int32_t n_sink, int32_t columns = 0) {
+  if (window == 0 || p->pos) return (int64_t(max_len) + kTile - 1) / kTile;
+  return shown_tiles(max_len, window, n_sink, columns, kTile);
 }
 
 }  // namespace

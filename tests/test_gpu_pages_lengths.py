@@ -30,3 +30,9 @@ def test_lengths_of_any_value(d):
     pages_of(gt, 4, max_len).d2o_pages_attend(q.cuda(), i32(first), i32(lens), og)
     within(og, want, tol)
     bits_same(gt, t)
+
+
+@pytest.mark.parametrize("n_sink", [HIGH, HIGH - 31, HIGH - 32])
+def test_as_many_first_tokens_as_there_are_numbers(n_sink):
+    """A window beside first tokens without end hides nothing."""
+    attend_case(128, 8, 2, 64, [5000, 40], [40, 3], window=9, n_sink=n_sink)

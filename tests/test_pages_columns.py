@@ -30,7 +30,15 @@ int main() {
           wrong += got != want;
           outside += got < -1 || got >= max_len;  // (an entry behind the last one that the page table's row names)
         }
-  printf("%ld %ld\n", wrong, outside);
+  long shares = 0;
+  for (int32_t max_len : bounds)
+    for (int32_t window : {1, 64, high})
+      for (int32_t sink : {0, 4, high - 32, high - 31, high})
+        for (int32_t columns : {0, 32}) {
+          const __int128 all = (__int128(max_len) + 15) / 16, shown = (__int128(window) + sink + columns) / 16 + 3;
+          shares += d2o::shown_tiles(max_len, window, sink, columns, 16) != (shown < all ? shown : all);
+        }
+  printf("%ld %ld %ld\n", wrong, outside, shares);
 }
 """
 
@@ -45,6 +53,14 @@ def program(tmp_path_factory):
     return str(where / "columns")
 
 
+def counts(program):
+    return list(map(int, subprocess.run([program], check=True, capture_output=True, text=True).stdout.split()))
+
+
 def test_lengths_of_any_value(program):
-    wrong, outside = map(int, subprocess.run([program], check=True, capture_output=True, text=True).stdout.split())
+    wrong, outside, _ = counts(program)
     assert outside == 0 and wrong == 0
+
+
+def test_first_tokens_up_to_the_largest_number(program):
+    assert counts(program)[2] == 0
