@@ -466,7 +466,7 @@ int d2o_pages_get(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_toke
  * that see none, get zeros.  Rows of out that belong to no sequence are left as they were.  Scores are neither read nor added to.  Weights end
  * as those of a step over 4-bit rows and hold 16 bits (8 where they are below 2^-118 times 512 times the entries of the largest), sums 24; NaN of a row reaches the tokens that see it and no others; out may be q itself.
  * Errors: INVALID_ARG, UNSUPPORTED (rows that are not of 4 bits; too many tokens for a launch), CAPACITY (max_len beyond the page table; workspace smaller than
- * d2o_pages_attend_workspace_bytes says, which grows with n_tokens up to a bound and falls again; where it says 0, NULL will do), HIP. */
+ * this call needs; what d2o_pages_attend_workspace_bytes says is enough for it and for every call with as many tokens and entries or fewer, and where it says 0, NULL will do), HIP. */
 int d2o_pages_attend_workspace_bytes(const d2o_pages* pages, int32_t n_tokens, int32_t max_len, size_t* bytes);
 int d2o_pages_attend(const d2o_pages* pages, d2o_view q, int32_t n_tokens, const int32_t* first, const int32_t* lens,
                      const int32_t* positions, int32_t max_len, int32_t window, int32_t n_sink, d2o_view out,

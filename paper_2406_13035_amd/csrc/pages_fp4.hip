@@ -830,14 +830,27 @@ int64_t column_groups(const d2o_pages* p, int32_t n_tokens) {
 }
 // Shares of a group's tiles, for at most `tiles` tiles each: three workgroups per CU, of which two are there at a time, and shares of 32 tiles.  (Sixteen sequences
 // of up to 8192 entries, 8 KV heads, 1 to 48 tokens: 91 us with two per CU, 73 with three, 80 with four or eight.)
-int attend_splits(int64_t heads, int64_t tiles) { return int(std::max<int64_t>(1, std::min<int64_t>(768 / heads, tiles / 32))); }
+constexpr int64_t kWanted = 768, kLeastShare = 32;
+int attend_splits(int64_t heads, int64_t tiles) { return int(std::max<int64_t>(1, std::min(kWanted / heads, tiles / kLeastShare))); }
 // Tiles of a share, so that `splits` of them hold the longest sequence: shorter ones take fewer.
 int share_tiles(int64_t tiles, int splits) { return int(((tiles + splits - 1) / splits + kLeast4 - 1) / kLeast4 * kLeast4); }
+// Bytes of the partial results of `parts` workgroups.
+size_t part_bytes(const d2o_pages* p, int64_t parts) {
+  const size_t rows = size_t(parts) * kGroup;
+  return round256(rows * p->head_dim * sizeof(float)) + round256(rows * 2 * sizeof(float));
+}
+// What a call needs, and with how many shares.
 size_t attend_bytes(const d2o_pages* p, int32_t max_len, int32_t n_tokens, int* splits) {
   const int64_t heads = column_groups(p, n_tokens) * p->n_kv_heads;
   *splits = attend_splits(heads, most_tiles(p, max_len, 0, 0));
-  const size_t rows = size_t(heads) * *splits * kGroup;
-  return *splits > 1 ? round256(rows * p->head_dim * sizeof(float)) + round256(rows * 2 * sizeof(float)) : 0;
+  return *splits > 1 ? part_bytes(p, heads * *splits) : 0;
+}
+// What every call with as many tokens and entries or fewer needs: large ones have one share and need nothing, smaller ones several.  (heads * splits, where
+// splits > 1, is at most kWanted and at most heads times the shares that a group may have, which both do not fall as tokens or entries rise.)
+size_t attend_bytes_at_most(const d2o_pages* p, int32_t max_len, int32_t n_tokens) {
+  const int64_t heads = column_groups(p, n_tokens) * p->n_kv_heads, shares = most_tiles(p, max_len, 0, 0) / kLeastShare;
+  if (shares < 2 || p->n_kv_heads * 2 > kWanted) return 0;
+  return part_bytes(p, std::min(kWanted, heads * shares));
 }
 
 int check_attend(const d2o_pages* p, PagePool* pool, int32_t n_tokens, int32_t max_len) {
@@ -868,8 +881,7 @@ extern "C" int d2o_pages_attend_workspace_bytes(const d2o_pages* pages, int32_t 
   const int rc = check_attend(pages, nullptr, n_tokens, max_len);
   if (rc != D2O_OK) return rc;
   if (!bytes) return D2O_ERR_INVALID_ARG;
-  int splits;
-  *bytes = n_tokens == 0 ? 0 : attend_bytes(pages, max_len, n_tokens, &splits);
+  *bytes = n_tokens == 0 ? 0 : attend_bytes_at_most(pages, max_len, n_tokens);
   return D2O_OK;
 }
 
