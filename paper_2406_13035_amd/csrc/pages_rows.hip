@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void put_rows(RowArgs a) {
     }
     if (c == 0) {
       if (a.pool.score) a.pool.score[at] = 0.f;
-      if (a.pool.pos) a.pool.pos[at] = a.positions ? a.positions[t] : 0;
+      if (a.pool.pos) a.pool.pos[at] = a.positions[t];
     }
   }
 }
