@@ -131,7 +131,8 @@ int d2o_reset(d2o_ctx* ctx, void* stream);
  * X: device [batch * n][hidden]; W: device [(Hq + 2 Hkv) * d][hidden] (a row = one output
  * feature; queries first, then keys, then values), both contiguous and 16-byte aligned;
  * Q: [B][Hq][n][d], K, V: [B][Hkv][n][d] views.  Built for D2O_BF16, d = 128, hidden a multiple
- * of 32 (fp32 accumulation on the matrix cores).  Enqueues only.
+ * of 32 (fp32 accumulation on the matrix cores).  Results that are not rotated (as d2o_qk_norm_rope takes them): every
+ * token as a sequence of its own, batch = tokens and n = 1, with pos0 = 0, where the angle is zero.  Enqueues only.
  * Errors: INVALID_ARG, UNSUPPORTED (other dtype / head_dim / hidden), HIP. */
 int d2o_qkv_project(int32_t batch, int32_t n, int32_t hidden, int32_t n_q_heads, int32_t n_kv_heads,
                     int32_t head_dim, int32_t dtype, const void* X, const void* W, d2o_view Q,
@@ -346,7 +347,8 @@ int d2o_window_attend(int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_
                       d2o_view Q, d2o_view K, d2o_view V, const int32_t* lens, int32_t window, int32_t n_sink,
                       d2o_view O, void* workspace, size_t workspace_bytes, void* stream);
 
-/* A cache in pages.  Entry s of sequence b is row s % page_size of page page_table[b][s / page_size], for every
+/* A cache in pages.  (The calls read all of the structure, to cache_fp4: a program that was compiled before it ended there has to be
+ * compiled again.)  Entry s of sequence b is row s % page_size of page page_table[b][s / page_size], for every
  * KV head.  A page id outside [0, n_pages) stands for no page: entries there are as if absent (never attended to, written
  * or moved; evictions rank them below all others).  A page that a call writes (rows, scores, positions) must stand once in one
  * sequence's row of the table; pages that are only attended to, with no scores kept, may be shared. */
@@ -454,7 +456,8 @@ int d2o_pages_map(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max
  * slots: device [n_tokens], page * page_size + row of the page; a token whose slot lies outside the pool is left out.
  * put stores K and V in the rows' format, score 0, and positions[t] (device [n_tokens]; NULL only if the pages keep none).  Slots that are written are all different.
  * get reads rows back as values (8-bit and 4-bit rows: exactly what they stand for); K and V of tokens that are left out stay as they were.
- * pages->page_table is checked but not looked at.  Enqueues only, needs no workspace.  Errors: INVALID_ARG, UNSUPPORTED (also more than 2^26 tokens), HIP. */
+ * pages->page_table is checked but not looked at.  (Neither put nor d2o_pages_attend adds attention to scores: an eviction gives up first what came in by them alone.)
+ * Enqueues only, needs no workspace.  Errors: INVALID_ARG, UNSUPPORTED (also more than 2^26 tokens), HIP. */
 int d2o_pages_put(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_tokens, const int64_t* slots,
                   const int32_t* positions, void* stream);
 int d2o_pages_get(const d2o_pages* pages, d2o_view K, d2o_view V, int32_t n_tokens, const int64_t* slots, void* stream);

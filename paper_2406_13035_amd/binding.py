@@ -519,9 +519,9 @@ class Pages:
 
     K, V: pools [n_pages, Hkv, page_size, d], float32 or bfloat16, or uint8 codes with int8 K_exp, V_exp
     [n_pages, Hkv, page_size] (8-bit rows of bfloat16 tensors), or uint8 pairs of codes [n_pages, Hkv, page_size, d / 2] with
-    K_exp, V_exp [n_pages, Hkv, page_size, d / 32] (4-bit rows); page_table int32 [B, max_pages]; score float32 and pos int32
-    [n_pages, Hkv, page_size] where accumulated attention and token positions are kept.  max_len: the most entries a sequence
-    (or tokens a prompt) will have in any call, the page table's capacity if None.  Calls on one object
+    K_exp, V_exp [n_pages, Hkv, page_size, d / 32] (4-bit rows; the dimensions of K_exp tell the two apart); page_table int32
+    [B, max_pages]; score float32 and pos int32 [n_pages, Hkv, page_size] where accumulated attention and token positions are
+    kept.  max_len: the most entries a sequence (or tokens a prompt) will have in any call, the page table's capacity if None.  Calls on one object
     share its workspace: on streams (or in graphs) that overlap in time, use an object each, and keep it until they are done."""
 
     def __init__(self, K, V, page_table, n_q_heads, K_exp=None, V_exp=None, score=None, pos=None, max_len=None):
