@@ -710,8 +710,8 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const Columns&
   }
 }
 
-// The step: a workgroup per (share, sequence and KV head), whose columns are the group's query heads.  8 heads x 131072 entries: 33 us, 4.3 TB/s, of which 24 are
-// the instructions that conversions and products take to issue.
+// The step: a workgroup per (share, sequence and KV head), whose columns are the group's query heads.  8 heads x 131072 entries: 33 us, 4.3 TB/s; conversions and
+// products take 20 us to issue.
 template <int D, Finds F, int PARTS>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void step_part4(AttendArgs a) {
   __shared__ AttendShared<D> sh;
@@ -727,7 +727,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))
   attend_share<D, F, true, 1, PARTS>(a, Columns{b, 0, a.G, 0, 0, 0}, list, mine, hk, blockIdx.x, blockIdx.y * a.splits + blockIdx.x, sh);
 }
 
-// Several tokens per sequence: a workgroup per (group of columns, KV head, share).  2048 tokens on 32768 entries, 32 heads on 8: 1.55-1.6 ms, 0.68 PFLOP/s, three executed products
+// Several tokens per sequence: a workgroup per (group of columns, KV head, share).  2048 tokens on 32768 entries, 32 heads on 8: 1.58 ms, 0.67 PFLOP/s, three executed products
 // per two counted; 232 vector instructions and 50 products per pair of tiles and 32 columns, which on this card run beside each other only in part.
 template <int D, Finds F>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void attend_part4(AttendArgs a) {

@@ -161,8 +161,8 @@ __device__ __forceinline__ int owner(const int32_t* first, int row, int lo, int 
   return lo;
 }
 
-// Small batches: everything by one workgroup.  Bound by latency: the lengths, two scans, a page's number, the slot (64 sequences: 6.6 us; 256 with 300000 tokens, by two
-// launches, 6 and 8).
+// Small batches: everything by one workgroup.  Bound by latency: the lengths, two scans, a page's number, the slot (64 sequences: 6.7 us; 256 with 300000 tokens, by two
+// launches, 6 and 9).
 constexpr int kSmall = 1024, kSmallRows = 4096, kSmallParts = 1024;
 __global__ __launch_bounds__(kThreads) void map_small(MapArgs a) {
   __shared__ int32_t before[kSmall], after[kSmall], take[kSmall], give[kSmall], first[kSmall + 1];
